@@ -461,13 +461,210 @@ nsp_status nsp_sp_tree_worklist(const nsp_plan_params *prm, const int64_t *lengt
                                 int32_t *sp);
 
 /*
+ * Row operators of the step around the attention.  A packed batch's rows go
+ * through a norm before the projections, the query and key heads through a
+ * norm and the rotation by their positions before the prologue, and the last
+ * rows' logits into the log probabilities that are trained on or answered
+ * with.  All three are bound by memory: every call reads each input once and
+ * writes each output once, however the rows lie.
+ *
+ * They share the conventions above, with these differences:
+ *   - A tensor of rows is given as nsp_rows: row (t, h) of token t and head h
+ *     is `n` contiguous elements at data + t * token_stride + h * head_stride
+ *     (strides in elements, >= 0).  So the heads of one projection's output
+ *     are used where they lie.  Rows of an input may coincide (stride 0: a
+ *     broadcast input); those of an output may not (NSP_EINVAL).
+ *   - Data pointers must be aligned to their element; 16-byte alignment of
+ *     the rows is faster, not required.
+ *   - An output may be the very view of the input of the same shape (same
+ *     address and strides: in place, where the call says so); any other
+ *     overlap of an output's extent with that input's is NSP_EINVAL.
+ *   - Nothing is allocated and no work list is kept: every call can be
+ *     captured into a HIP graph at once.  A workspace is used from a call's
+ *     first kernel to its last: two calls that may run at the same time (also
+ *     two graphs) need two.
+ *   - Results are deterministic: no atomics, sums in a fixed order that
+ *     depends on the shapes and types only.
+ *   - n_tokens, and n_tokens * n_heads, up to 2^31 - 1; 0 tokens are a valid
+ *     call.
+ */
+typedef struct {
+  void *data;
+  int64_t token_stride, head_stride;
+} nsp_rows;
+
+typedef enum { NSP_ROTARY_HALF = 0, NSP_ROTARY_PAIRS = 1 } nsp_rotary_layout;
+
+/*
+ * Rotary positions of query and key heads (Background, Sequence Packing:
+ * position ids restart at every packed sequence), before nsp_ulysses_pack or
+ * the attention.  For token t and pair i < rot_dim / 2, with
+ * a = positions[t] * freqs[i] radians (the product and its reduction to a
+ * turn in 64 bits: positions of any context are as exact as the first):
+ *     (x1, x2) = (x[i], x[i + rot_dim / 2])   NSP_ROTARY_HALF
+ *                (x[2 i], x[2 i + 1])         NSP_ROTARY_PAIRS
+ *     y1 = scale (x1 cos a - x2 sin a),  y2 = scale (x2 cos a + x1 sin a)
+ * in float32, rounded once; elements rot_dim .. head_dim - 1 are copied.
+ * nsp_rotary_bwd is the gradient: the transposed rotation (angle -a, the same
+ * scale) of dq_out, dk_out into dq, dk.
+ *   dtype       of every tensor (NSP_BF16 or NSP_F32)
+ *   head_dim    1 .. 1024;  rot_dim even, 2 .. head_dim
+ *   freqs       DEVICE, rot_dim / 2 doubles, as nsp_rotary_frequencies (or
+ *               any other rule) gives them
+ *   scale       amplitude of the rotated part, finite
+ *   positions   DEVICE, n_tokens int64 (any value)
+ *   q, q_out    q_heads (>= 1) heads; in place allowed
+ *   k, k_out    k_heads (>= 0) heads; NULL with k_heads = 0; in place allowed
+ * q and k (and their outputs) may be parts of one tensor; writing into a part
+ * that another argument reads is the caller's race.
+ * Errors: NSP_EINVAL, NSP_EUNSUPPORTED (head_dim > 1024), NSP_EHIP.
+ */
+nsp_status nsp_rotary_fwd(nsp_rotary_layout layout, nsp_dtype dtype, int64_t n_tokens, int32_t head_dim,
+                          int32_t rot_dim, const double *freqs, float scale, const int64_t *positions,
+                          int32_t q_heads, const nsp_rows *q, const nsp_rows *q_out, int32_t k_heads,
+                          const nsp_rows *k, const nsp_rows *k_out, hipStream_t stream);
+nsp_status nsp_rotary_bwd(nsp_rotary_layout layout, nsp_dtype dtype, int64_t n_tokens, int32_t head_dim,
+                          int32_t rot_dim, const double *freqs, float scale, const int64_t *positions,
+                          int32_t q_heads, const nsp_rows *dq_out, const nsp_rows *dq, int32_t k_heads,
+                          const nsp_rows *dk_out, const nsp_rows *dk, hipStream_t stream);
+
+/*
+ * The angle per position of every pair, f_i = base^(-2 i / rot_dim), scaled
+ * for contexts longer than the trained one (host only):
+ *   NSP_ROTARY_PLAIN   f_i
+ *   NSP_ROTARY_LINEAR  f_i / factor (positions interpolated)
+ *   NSP_ROTARY_BASE    base replaced by base * factor^(r / (r - 2)), r =
+ *                      rot_dim >= 4: the slowest pair interpolated by factor,
+ *                      the fastest kept
+ *   NSP_ROTARY_PARTS   by the turns n_i = context * f_i / (2 pi) that a pair
+ *                      makes in the trained context: f_i (g + (1 - g) / factor),
+ *                      g = (n_i - low) / (high - low) clamped to 0 .. 1
+ *   factor    >= 1 (ignored by NSP_ROTARY_PLAIN); context > 0, 0 <= low < high
+ *             (read by NSP_ROTARY_PARTS only)
+ *   freqs     out, HOST, rot_dim / 2 doubles
+ *   scale     out (may be NULL): the amplitude that goes with interpolation by
+ *             parts, 0.1 ln(factor) + 1; 1 for the others
+ * Errors: NSP_EINVAL.
+ */
+typedef enum { NSP_ROTARY_PLAIN = 0, NSP_ROTARY_LINEAR = 1, NSP_ROTARY_BASE = 2, NSP_ROTARY_PARTS = 3 } nsp_rotary_scaling;
+nsp_status nsp_rotary_frequencies(int32_t rot_dim, double base, nsp_rotary_scaling scaling, double factor,
+                                  double context, double low, double high, double *freqs, float *scale);
+
+typedef enum { NSP_NORM_LAYER = 0, NSP_NORM_RMS = 1 } nsp_norm_kind;
+
+/*
+ * Norm of rows of n elements, (n_tokens x n_heads) of them, in float32:
+ *     NSP_NORM_LAYER   m = mean(x), v = mean((x - m)^2)
+ *     NSP_NORM_RMS     m = 0,       v = mean(x^2)
+ *     rstd = 1 / sqrt(v + eps),  y = (x - m) rstd w + b   (rounded once)
+ * The same w and b for every row: hidden rows (n_heads = 1), or each head's
+ * (n_heads heads of a projection's output).
+ *   dtype       of x and y; w_dtype of w and b (each NSP_BF16 or NSP_F32)
+ *   n           1 .. 65536
+ *   w, b        n contiguous elements; NULL: ones, zeros
+ *   eps         finite, >= 0
+ *   y           in place allowed
+ *   mean, rstd  float32 [n_tokens * n_heads] in row order (t, then h), for the
+ *               backward; either may be NULL (mean is not written by NSP_NORM_RMS)
+ * Errors: NSP_EINVAL, NSP_EUNSUPPORTED (n > 65536), NSP_EHIP.
+ */
+nsp_status nsp_norm_fwd(nsp_norm_kind kind, nsp_dtype dtype, nsp_dtype w_dtype, int64_t n_tokens, int32_t n_heads,
+                        int32_t n, const nsp_rows *x, const void *w, const void *b, float eps, const nsp_rows *y,
+                        float *mean, float *rstd, hipStream_t stream);
+
+/* Bytes of device workspace nsp_norm_bwd needs (0 for invalid sizes): the
+ * partial sums of dw and db; at most 8192 n + 1024 for any number of rows. */
+size_t nsp_norm_bwd_workspace(int64_t n_tokens, int32_t n_heads, int32_t n);
+
+/*
+ * Gradient of the norm, with h = dy w, xh = (x - m) rstd and means over the row:
+ *     dx = rstd (h - mean(h) - xh mean(h xh))    (NSP_NORM_RMS: without mean(h))
+ *     dw = sum over rows of dy xh,  db = sum over rows of dy
+ * the sums over rows in float32, in a fixed order, rounded once to w_dtype.
+ *   x, w        as in the forward; mean, rstd its outputs (mean is not read by
+ *               NSP_NORM_RMS and may be NULL)
+ *   dx          may be dy's or x's very view
+ *   dw, db      n elements of w_dtype; either may be NULL (not computed)
+ *   workspace   nsp_norm_bwd_workspace bytes, 256-byte aligned (NULL if neither
+ *               dw nor db is wanted); contents on entry are ignored
+ * With no rows dw and db are zeros.
+ * Errors: NSP_EINVAL, NSP_EUNSUPPORTED, NSP_EWORKSPACE, NSP_EHIP.
+ */
+nsp_status nsp_norm_bwd(nsp_norm_kind kind, nsp_dtype dtype, nsp_dtype w_dtype, int64_t n_tokens, int32_t n_heads,
+                        int32_t n, const nsp_rows *x, const void *w, const nsp_rows *dy, const float *mean,
+                        const float *rstd, const nsp_rows *dx, void *dw, void *db, void *workspace, size_t ws_bytes,
+                        hipStream_t stream);
+
+#define NSP_TOKEN_LOGP_MAX_TOP 64
+/* Bytes of device workspace nsp_token_logp_fwd needs (0 for invalid sizes,
+ * and for calls of many rows, which need none); at most 4 MiB. */
+size_t nsp_token_logp_workspace(int64_t n_tokens, int32_t vocab, int32_t top);
+
+/*
+ * Log probabilities of given tokens, with entropy and the top alternatives.
+ * For row t of logits (n_tokens rows of `vocab` elements, row_stride elements
+ * apart), z = scale * logits[t] in float32 and p = exp(z - lse):
+ *     lse[t]     = log sum_v exp(z_v)
+ *     logp[t]    = z[targets[t]] - lse[t]
+ *     entropy[t] = lse[t] - sum_v p_v z_v
+ *     top_index[t][j], top_logp[t][j]: the `top` largest logits, largest
+ *                  first, equal ones by the lower index; z - lse of each
+ * A target outside 0 .. vocab - 1 is ignored: logp = 0.  Logits of -2^126
+ * (-8.5e37) and below, -inf and the types' lowest values among them, are a
+ * masked vocabulary: they have p = 0 and are no alternatives (places past the
+ * last logit above hold index -1 and -inf).  A row of nothing else has lse =
+ * -inf, entropy 0, and logp = -inf unless its target is ignored.  A row with a
+ * NaN or +inf has lse and entropy NaN, and logp and the alternatives' values
+ * too (NaN itself is never an alternative).
+ *   dtype       of the logits (NSP_BF16 or NSP_F32)
+ *   row_stride  >= 0 (rows may coincide)
+ *   targets     DEVICE, n_tokens int64; NULL with logp NULL
+ *   scale       2^-64 .. 2^64 (an inverse temperature)
+ *   logp, entropy   float32 [n_tokens]; either may be NULL.  lse: float32
+ *               [n_tokens], needed by the backward
+ *   top         0 .. NSP_TOKEN_LOGP_MAX_TOP; top_logp float32 and top_index
+ *               int64 [n_tokens][top], NULL with top = 0
+ *   workspace   nsp_token_logp_workspace bytes, 256-byte aligned; contents on
+ *               entry are ignored
+ *   vocab       1 .. 2^30
+ * Errors: NSP_EINVAL, NSP_EUNSUPPORTED (vocab, top), NSP_EWORKSPACE, NSP_EHIP.
+ */
+nsp_status nsp_token_logp_fwd(nsp_dtype dtype, int64_t n_tokens, int32_t vocab, const void *logits,
+                              int64_t row_stride, const int64_t *targets, float scale, float *logp, float *lse,
+                              float *entropy, int32_t top, float *top_logp, int64_t *top_index, void *workspace,
+                              size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Gradient of the above with respect to the logits, from the gradients of
+ * logp, lse and entropy (float32 [n_tokens]; NULL: zeros):
+ *     dlogits_v = scale (g_logp (1[v = target] - p_v) + g_lse p_v
+ *                        - g_entropy p_v (z_v - lse + entropy))
+ * in float32, rounded once.  An ignored target takes g_logp as 0.  A row of
+ * masked logits alone (lse = -inf) has gradient 0, and so has a row whose three gradients are
+ * 0, whatever its logits.  The alternatives' values have no gradient.
+ *   targets     may be NULL with g_logp NULL
+ *   lse         the forward's; entropy too, needed with g_entropy (else may
+ *               be NULL)
+ *   dlogits     rows of `vocab` elements of dtype, d_row_stride (>= vocab,
+ *               unless one row) apart; in place allowed; what lies between the
+ *               rows is left as it is
+ * Errors: NSP_EINVAL, NSP_EUNSUPPORTED (vocab), NSP_EHIP.
+ */
+nsp_status nsp_token_logp_bwd(nsp_dtype dtype, int64_t n_tokens, int32_t vocab, const void *logits,
+                              int64_t row_stride, const int64_t *targets, float scale, const float *lse,
+                              const float *entropy, const float *g_logp, const float *g_lse, const float *g_entropy,
+                              void *dlogits, int64_t d_row_stride, hipStream_t stream);
+
+/*
  * Kernel timing (instrumentation, off by default).  While enabled, every
  * kernel this library launches is bracketed by a pair of hipEvents recorded
  * on the launch's stream, so the measured time is the device time of that
  * kernel alone.  nsp_timing_query waits for the recorded events, folds them
  * into per-kernel totals and returns the launch count and total milliseconds
  * since the last nsp_timing_reset for one kernel name: "attn_fwd",
- * "bwd_preprocess", "bwd_dkdv", "bwd_dq" or "relayout".  (A backward runs
+ * "bwd_preprocess", "bwd_dkdv", "bwd_dq" or "relayout", or a row operator:
+ * "rotary", "norm_fwd", "norm_bwd", "token_logp_fwd" or "token_logp_bwd" (its
+ * launches together).  (An attention backward runs
  * "bwd_preprocess", "bwd_dkdv" with the sums of a split pass, "bwd_dq"; lists of
  * shorter items "bwd_dq", which takes in the preprocess, then "bwd_dkdv"; small
  * lists "bwd_preprocess", then both passes in one launch, counted as "bwd_dkdv".)

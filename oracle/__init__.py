@@ -29,10 +29,12 @@ What the oracle computes, and from which passage of the paper:
 * recompute.py -- the tree-level recomputation plan (Design, NSP Executor,
   Tree-Level Recomputation): SAVE / RECOMPUTE marks from an activation
   budget, walking the SP tree root first, in plain Python.
+* rows.py -- the row operators around the attention (rotary positions, norms
+  of rows, token log probabilities) and their gradients, by their definitions.
 
 Every function is pinned by tests/test_oracle_*.py against brute force,
 torch's fp64 SDPA + autograd, finite differences, closed forms and
 invariants; see those files for which pin catches which mistake.
 """
 
-from . import attention, planner, recompute, ulysses  # noqa: F401
+from . import attention, planner, recompute, rows, ulysses  # noqa: F401

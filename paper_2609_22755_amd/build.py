@@ -25,12 +25,14 @@ CXXFLAGS = [
     "-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
     # packed fp32 VALU forms are kept out of the generated code
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    # no NaN semantics needed (inputs are finite; masked scores are -inf):
-    # lets max/min skip operand canonicalisation.  Infinities are kept.
-    "-fno-honor-nans",
     "-Wall", "-Wno-unused-function",
     "-I", INCLUDE, "-I", CSRC,
 ]
+# No NaN semantics needed in the attention and re-layout (inputs are finite;
+# masked scores are -inf): lets max/min skip operand canonicalisation.
+# Infinities are kept.  The row operators hand a NaN on.
+NO_NANS = "-fno-honor-nans"
+KEEP_NANS = ("rotary.hip", "norm.hip", "token_logp.hip", "row_ops.cpp")
 
 
 def hipcc() -> str:
@@ -46,7 +48,8 @@ def sources():
 
 def _compile(src: str, verbose: bool) -> str:
     obj = os.path.join(BUILD, os.path.basename(src) + ".o")
-    cmd = [hipcc(), *CXXFLAGS, "-c", src, "-o", obj]
+    flags = CXXFLAGS if os.path.basename(src) in KEEP_NANS else [*CXXFLAGS, NO_NANS]
+    cmd = [hipcc(), *flags, "-c", src, "-o", obj]
     if src.endswith(".hip"):
         cmd[1:1] = ["-x", "hip"]
     r = subprocess.run(cmd, capture_output=True, text=True)

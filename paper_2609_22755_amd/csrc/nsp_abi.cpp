@@ -1200,9 +1200,17 @@ size_t bwd_workspace_bytes(const WlInfo &w) {
 
 namespace {
 
-const char *const kKernelNames[] = {"attn_fwd", "bwd_preprocess", "bwd_dkdv", "bwd_dq", "relayout"};
-constexpr int kNumKernels = 5;
-enum KernelId { K_FWD = 0, K_PRE = 1, K_DKDV = 2, K_DQ = 3, K_RELAYOUT = 4 };
+using nsp::kNumKernels;
+using nsp::timed_launch;
+using nsp::K_FWD;
+using nsp::K_PRE;
+using nsp::K_DKDV;
+using nsp::K_DQ;
+using nsp::K_RELAYOUT;
+const char *const kKernelNames[] = {"attn_fwd", "bwd_preprocess", "bwd_dkdv",      "bwd_dq",
+                                    "relayout", "rotary",         "norm_fwd",      "norm_bwd",
+                                    "token_logp_fwd", "token_logp_bwd"};
+static_assert(sizeof(kKernelNames) / sizeof(kKernelNames[0]) == kNumKernels, "a name for every kernel");
 
 struct TimingState {
   std::mutex mu;
@@ -1213,21 +1221,21 @@ struct TimingState {
 };
 TimingState g_timing;
 
-// Run `launch` on `stream`, bracketed by timing events when timing is on.
-template <class F>
-hipError_t timed_launch(KernelId id, hipStream_t stream, F launch) {
+}  // namespace
+
+hipError_t nsp::timed_call(KernelId id, hipStream_t stream, hipError_t (*launch)(void *), void *ctx) {
   bool on;
   {
     std::lock_guard<std::mutex> lock(g_timing.mu);
     on = g_timing.on;
   }
-  if (!on) return launch();
+  if (!on) return launch(ctx);
   hipEvent_t a = nullptr, b = nullptr;
   hipError_t e = hipEventCreate(&a);
   if (e == hipSuccess) e = hipEventCreate(&b);
   if (e == hipSuccess) e = hipEventRecord(a, stream);
   if (e != hipSuccess) return e;
-  e = launch();
+  e = launch(ctx);
   if (e != hipSuccess) return e;
   e = hipEventRecord(b, stream);
   if (e != hipSuccess) return e;
@@ -1235,6 +1243,8 @@ hipError_t timed_launch(KernelId id, hipStream_t stream, F launch) {
   g_timing.pending[id].push_back({a, b});
   return hipSuccess;
 }
+
+namespace {
 
 // Arguments of a backward call (everything but the workspace).
 nsp_status validate_bwd(const nsp_worklist *wl, float softmax_scale, int32_t causal, const void *q, const void *k,

@@ -144,6 +144,18 @@ hipError_t noalloc_scratch(char **ptr);
 // return `status`; also clears it when called with NSP_OK and no format.
 int32_t set_error(int32_t status, const char *fmt, ...);
 
+// Kernels by the names of nsp_timing_query.
+enum KernelId {
+  K_FWD = 0, K_PRE, K_DKDV, K_DQ, K_RELAYOUT, K_ROTARY, K_NORM_FWD, K_NORM_BWD, K_LOGP_FWD, K_LOGP_BWD, kNumKernels
+};
+
+// launch(ctx) on `stream`, bracketed by timing events when timing is on.
+hipError_t timed_call(KernelId id, hipStream_t stream, hipError_t (*launch)(void *), void *ctx);
+template <class F>
+hipError_t timed_launch(KernelId id, hipStream_t stream, F launch) {
+  return timed_call(id, stream, [](void *f) { return (*static_cast<F *>(f))(); }, &launch);
+}
+
 // Compute units of the current device (looked up once per device).
 hipError_t compute_units(int *cus);
 
@@ -157,5 +169,91 @@ hipError_t launch_bwd_dq(int head_dim, bool g_f32, const AttnArgs &a, int n_unit
 hipError_t launch_bwd_dkdv(int head_dim, bool g_f32, const AttnArgs &a, int n_units, hipStream_t s);
 hipError_t launch_relayout(const void *src, void *dst, const CopyTask *tasks, int n_tasks,
                            int sum_mode, hipStream_t s);
+
+// ------------------------------------------------------------ row operators --
+
+// Quotients of numbers below 2^31 by a divisor known on the host: one high
+// product, one sum and one shift (Granlund and Montgomery's round-up method).
+struct FastDiv {
+  uint32_t d, mul, shift;
+  FastDiv(uint32_t div = 1) : d(div), mul(0), shift(0) {
+    while ((uint64_t(1) << shift) < div) ++shift;
+    mul = uint32_t(((uint64_t(1) << 32) * ((uint64_t(1) << shift) - div)) / div + 1);
+  }
+  __host__ __device__ uint32_t quot(uint32_t x) const {
+    return (uint32_t)((((uint64_t)x * mul) >> 32) + x) >> shift;
+  }
+};
+
+// Rows (token, head) of contiguous elements; strides in elements.
+struct RowView {
+  char *data;
+  int64_t ts, hs;
+};
+
+struct RotaryArgs {
+  RowView x[2], y[2];        // queries, keys
+  int64_t n_tokens;
+  const double *freqs;
+  const int64_t *positions;
+  float scale;
+  float sign;                // -1 in the backward
+  int32_t heads[2];
+  int32_t head_dim, half;    // half: pairs a head
+  bool copy[2];              // the part that is not rotated has to be moved
+};
+hipError_t launch_rotary(bool pairs, bool f32, const RotaryArgs &a, hipStream_t s);
+
+// Widest row of a norm.
+constexpr int kNormMaxN = 65536;
+// Most workgroups of a norm's backward, each with a partial sum of dw and db.
+constexpr int kNormMaxParts = 1024;
+struct NormArgs {
+  RowView x, y, dy;          // backward: y is dx
+  const void *w, *b;
+  bool w_f32, rms;
+  int32_t rows, n;
+  FastDiv heads;
+  float eps;
+  float *mean, *rstd;
+  const float *mean_in, *rstd_in;
+  void *dw, *db;
+  float *part;               // [parts][2][n]: dw, db
+};
+// Workgroups of the backward (rows > 0).
+int norm_bwd_parts(int64_t rows, int n, bool f32);
+hipError_t launch_norm_fwd(bool f32, const NormArgs &a, hipStream_t s);
+hipError_t launch_norm_bwd(bool f32, const NormArgs &a, hipStream_t s);
+
+// Most parts that a row of logits is split in.
+constexpr int kLogpMaxParts = 64;
+// Widest vocabulary.
+constexpr int kLogpMaxVocab = 1 << 30;
+struct LogpArgs {
+  const char *logits;
+  int64_t row_stride;
+  const int64_t *targets;
+  float scale;
+  int32_t n_tokens, vocab, top;
+  float *logp, *lse, *entropy, *top_logp;
+  int64_t *top_index;
+  int32_t parts, part_len;   // parts a row, elements a part
+  float4 *part_sums;         // [row][part]: reference, sum, weighted sum
+  uint64_t *part_top;        // [row][part][top]
+};
+// Parts a row is split in.
+int token_logp_parts(int64_t n_tokens, int vocab);
+hipError_t launch_token_logp_fwd(bool f32, const LogpArgs &a, hipStream_t s);
+
+struct LogpBwdArgs {
+  const char *logits;
+  char *dlogits;
+  int64_t row_stride, d_row_stride;
+  const int64_t *targets;
+  float scale;
+  int32_t n_tokens, vocab;
+  const float *lse, *entropy, *g_logp, *g_lse, *g_entropy;
+};
+hipError_t launch_token_logp_bwd(bool f32, const LogpBwdArgs &a, hipStream_t s);
 
 }  // namespace nsp
