@@ -12,11 +12,18 @@
 // loaded once, and the backward sums its part of dw and db in registers over
 // the rows that a workgroup takes in turn; the workgroups' sums go to the
 // workspace and a second kernel adds them, in the same order every time.
+#include <type_traits>
+
 #include "nsp_internal.hpp"
 #include "row_common.hpp"
 
 namespace nsp {
 namespace {
+
+// The forward's workgroups take four row groups in turn, where there are so
+// many (fewer reload the weights more often, more leave the last ones alone: rows
+// of 8192 bf16 6.1 TB/s, with two 5.7, with eight 5.9).
+constexpr int kFwdTurns = 4, kFwdLeast = 2048, kFwdMost = 1 << 21;
 
 template <class T>
 __device__ __forceinline__ T *row_at(const RowView &v, const FastDiv &heads, int row) {
@@ -24,16 +31,57 @@ __device__ __forceinline__ T *row_at(const RowView &v, const FastDiv &heads, int
   return (T *)v.data + (int64_t)t * v.ts + (int64_t)((uint32_t)row - t * heads.d) * v.hs;
 }
 
-// Weights of the elements e0 .. e0 + V - 1 (cnt of them within the row).
+// V weights from element e0 on (all within the row).
 template <int V>
-__device__ __forceinline__ void load_weights(const void *w, bool f32, int e0, int cnt, float none, float (&x)[V]) {
+__device__ __forceinline__ void load_weights(const void *w, bool f32, int e0, float none, float (&x)[V]) {
+  if (!w) {
 #pragma unroll
-  for (int e = 0; e < V; ++e) x[e] = none;
-  if (!w) return;
+    for (int e = 0; e < V; ++e) x[e] = none;
+  } else if (f32) {
+    struct __attribute__((packed, aligned(4))) W { float v[V]; } v = *(const W *)((const float *)w + e0);
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[e] = v.v[e];
+  } else {
+    struct __attribute__((packed, aligned(2))) W { unsigned short v[V]; } v = *(const W *)((const bf16 *)w + e0);
+#pragma unroll
+    for (int e = 0; e < V; ++e) x[e] = __uint_as_float((uint32_t)v.v[e] << 16);
+  }
+}
+
+// The same where only `cnt` lie within the row (the others: 0).
+template <int V>
+__device__ __forceinline__ void some_weights(const void *w, bool f32, int e0, int cnt, float none, float (&x)[V]) {
+  if (!w || cnt >= V) return load_weights<V>(w, f32, e0, none, x);
 #pragma unroll
   for (int e = 0; e < V; ++e)
-    if (e < cnt) x[e] = f32 ? ((const float *)w)[e0 + e] : to_f32(((const bf16 *)w)[e0 + e]);
+    x[e] = e >= cnt ? 0.f : f32 ? ((const float *)w)[e0 + e] : to_f32(((const bf16 *)w)[e0 + e]);
 }
+
+// Threads of a workgroup, and the rows that it takes at a time.
+template <int LPR>
+constexpr int kBlock = LPR < 256 ? 256 : LPR;
+template <int LPR>
+constexpr int kGroups = kBlock<LPR> / LPR;
+
+// The vectors of a lane: each starts at element e0, and its elements from `own`
+// on are the lane's.  The last vector of a row that is no whole number of them
+// reaches back over its neighbour's elements (both then store the same there:
+// every lane has loaded before any stores), and a lane past the end holds the
+// first vector of the row, with none of its own.
+template <int LPR, int CH, int V>
+struct Columns {
+  int e0[CH], own[CH];
+  bool some[CH];             // a lane of the wave does not own all of its vector
+  __device__ __forceinline__ Columns(int n, int lane) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int at = (c * LPR + lane) * V;
+      e0[c] = at + V <= n ? at : at < n ? n - V : 0;
+      own[c] = at < n ? at - e0[c] : V;
+      some[c] = __any(own[c] > 0);
+    }
+  }
+};
 
 // Sums of NV values over the LPR lanes of a row, in every one of them.
 template <int LPR, int NV>
@@ -41,154 +89,222 @@ struct RowSum {
   static constexpr int W = LPR / 64;
   __device__ __forceinline__ static void run(float (&x)[NV], float *slots, int &turn) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) x[i] = group_sum<(LPR < 64 ? LPR : 64)>(x[i]);
+    for (int i = 0; i < NV; ++i) x[i] = group_sum<(LPR < 64 ? 16 : 64)>(x[i]);
     if constexpr (LPR > 64) {
-      float *s = slots + (turn & 1) * (W * NV);
+      float *s = slots + ((turn & 1) * kGroups<LPR> + threadIdx.x / LPR) * (W * NV);
       turn ^= 1;
-      const int lane = threadIdx.x & 63, wave = (threadIdx.x % LPR) >> 6;
-      if (lane == 0) {
+      const int lane = threadIdx.x & 15, wave = (threadIdx.x % LPR) >> 6;
+      if ((threadIdx.x & 63) == 0) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) s[wave * NV + i] = x[i];
       }
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        // every wave adds the W sums the same way
-        float v = lane < W ? s[lane * NV + i] : 0.f;
-        v = group_sum<(W < 2 ? 2 : W)>(v);
-        x[i] = __shfl(v, 0);
-      }
+      for (int i = 0; i < NV; ++i) x[i] = group_sum<16>(lane < W ? s[lane * NV + i] : 0.f);
     }
   }
 };
 
+// A row's result, kept until the next row's turn: a store goes out before the
+// loads of the row after that, whose arrival is then not waited for behind it
+// (loads and stores retire in the order they were issued).  Rows of 128 bf16:
+// 5.8 TB/s, 5.4 without.  (The backward has no registers left for it.)
 template <class T, int LPR, int CH>
-__global__ __launch_bounds__(LPR < 256 ? 256 : LPR) void norm_fwd_kernel(NormArgs a) {
+struct Done {
+  T *row = nullptr;
+  u32x4 v[CH];
+  __device__ __forceinline__ void store(const Columns<LPR, CH, kVec<T>> &col) {
+    if (!row) return;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+      if (col.own[c] < kVec<T>) store16(row + col.e0[c], v[c]);
+  }
+};
+
+template <class T, int LPR, int CH>
+__global__ __launch_bounds__(kBlock<LPR>) void norm_fwd_kernel(NormArgs a) {
   constexpr int V = kVec<T>;
-  constexpr int RPB = LPR < 256 ? 256 / LPR : 1;
-  __shared__ float slots[2 * (LPR / 64 + 1)];
+  constexpr int RPB = kGroups<LPR>;
+  __shared__ float slots[2 * RPB * (LPR / 64 + 1)];
   const int lane = threadIdx.x % LPR, group = threadIdx.x / LPR;
   int turn = 0;
+  const Columns<LPR, CH, V> col(a.n, lane);
+  // a group past the end takes the last row once more and stores nothing
+  u32x4 raw[CH];
+  const auto fetch = [&](int64_t row0) {
+    const T *x = row_at<const T>(a.x, a.heads, (int)min(row0 + group, (int64_t)a.rows - 1));
+#pragma unroll
+    for (int c = 0; c < CH; ++c) raw[c] = load16(x + col.e0[c]);
+  };
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  int64_t row0 = (int64_t)blockIdx.x * RPB;
+  fetch(row0);
   float w[CH][V], b[CH][V];
-  int cnt[CH];
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    const int e0 = (c * LPR + lane) * V;
-    cnt[c] = min(V, max(0, a.n - e0));
-    load_weights<V>(a.w, a.w_f32, e0, cnt[c], 1.f, w[c]);
-    load_weights<V>(a.b, a.w_f32, e0, cnt[c], 0.f, b[c]);
+    load_weights<V>(a.w, a.w_f32, col.e0[c], 1.f, w[c]);
+    load_weights<V>(a.b, a.w_f32, col.e0[c], 0.f, b[c]);
   }
   const float inv_n = 1.f / (float)a.n;
-  for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < a.rows; row0 += (int64_t)gridDim.x * RPB) {
-    const bool live = row0 + group < a.rows;         // (a group past the end repeats the last row and stores nothing)
-    const int row = live ? (int)row0 + group : a.rows - 1;
-    const T *x = row_at<const T>(a.x, a.heads, row);
+  Done<T, LPR, CH> done;
+  for (; row0 < a.rows; row0 += step) {
     float v[CH][V];
-    float sum[1] = {0.f};
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      load_vec(x + (c * LPR + lane) * V, cnt[c], 0.f, v[c]);
-#pragma unroll
-      for (int e = 0; e < V; ++e) sum[0] += v[c][e];
-    }
+    for (int c = 0; c < CH; ++c) unpack<T>(raw[c], v[c]);
+    done.store(col);
+    if (row0 + step < a.rows) fetch(row0 + step);
     float mean = 0.f;
     if (!a.rms) {
+      float sum[1] = {0.f};
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        if (col.some[c]) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) sum[0] += e >= col.own[c] ? v[c][e] : 0.f;
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; ++e) sum[0] += v[c][e];
+        }
+      }
       RowSum<LPR, 1>::run(sum, slots, turn);
       mean = sum[0] * inv_n;
     }
     float sq[1] = {0.f};
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
+    for (int c = 0; c < CH; ++c) {
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float d = e < cnt[c] ? v[c][e] - mean : 0.f;
-        v[c][e] = d;
-        sq[0] += d * d;
+      for (int e = 0; e < V; ++e) v[c][e] -= mean;
+      if (col.some[c]) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) sq[0] += e >= col.own[c] ? v[c][e] * v[c][e] : 0.f;
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) sq[0] += v[c][e] * v[c][e];
       }
+    }
     RowSum<LPR, 1>::run(sq, slots, turn);
-    const float rstd = 1.f / sqrtf(sq[0] * inv_n + a.eps);
-    if (!live) continue;
-    T *y = row_at<T>(a.y, a.heads, row);
+    const float rstd = __builtin_amdgcn_rsqf(sq[0] * inv_n + a.eps);
+    const bool live = row0 + group < a.rows;
+    const int row = live ? (int)row0 + group : a.rows - 1;
+    done.row = live ? row_at<T>(a.y, a.heads, row) : nullptr;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       float o[V];
 #pragma unroll
       for (int e = 0; e < V; ++e) o[e] = v[c][e] * rstd * w[c][e] + b[c][e];
-      store_vec(y + (c * LPR + lane) * V, cnt[c], o);
+      done.v[c] = pack<T>(o);
     }
-    if (lane == 0) {
+    if (lane == 0 && live) {
       if (a.mean) a.mean[row] = mean;
       if (a.rstd) a.rstd[row] = rstd;
     }
   }
+  done.store(col);
 }
 
+// A row is kept as it was loaded until it is done: unpacking it twice is
+// cheaper than the registers of its float32 form, which the next row's vectors,
+// on their way meanwhile, take.
 template <class T, int LPR, int CH>
-__global__ __launch_bounds__(LPR < 256 ? 256 : LPR) void norm_bwd_kernel(NormArgs a) {
+__global__ __launch_bounds__(kBlock<LPR>) void norm_bwd_kernel(NormArgs a) {
   constexpr int V = kVec<T>;
-  constexpr int RPB = LPR < 256 ? 256 / LPR : 1;
-  __shared__ float slots[2 * 2 * (LPR / 64 + 1)];
+  constexpr int RPB = kGroups<LPR>;
+  __shared__ float slots[2 * 2 * RPB * (LPR / 64 + 1)];
   const int lane = threadIdx.x % LPR, group = threadIdx.x / LPR;
   int turn = 0;
+  const Columns<LPR, CH, V> col(a.n, lane);
+  // a group past the end loads the last row once more, counts it as 0 and stores nothing
+  struct Row {
+    u32x4 x[CH], g[CH];
+    float mean, rstd;
+  };
+  Row cur, next;
+  const auto fetch = [&](int64_t row0, Row &r) {
+    const bool live = row0 + group < a.rows;
+    const int row = live ? (int)row0 + group : a.rows - 1;
+    const T *x = row_at<const T>(a.x, a.heads, row), *dy = row_at<const T>(a.dy, a.heads, row);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      r.x[c] = load16(x + col.e0[c]);
+      r.g[c] = load16(dy + col.e0[c]);
+    }
+    r.mean = a.rms ? 0.f : a.mean_in[row];
+    r.rstd = a.rstd_in[row];
+  };
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  int64_t row0 = (int64_t)blockIdx.x * RPB;
+  fetch(row0, next);
   float w[CH][V], dw[CH][V], db[CH][V];
-  int cnt[CH];
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    const int e0 = (c * LPR + lane) * V;
-    cnt[c] = min(V, max(0, a.n - e0));
-    load_weights<V>(a.w, a.w_f32, e0, cnt[c], 1.f, w[c]);
+    load_weights<V>(a.w, a.w_f32, col.e0[c], 1.f, w[c]);
 #pragma unroll
     for (int e = 0; e < V; ++e) dw[c][e] = db[c][e] = 0.f;
   }
   const float inv_n = 1.f / (float)a.n;
-  for (int64_t row0 = (int64_t)blockIdx.x * RPB; row0 < a.rows; row0 += (int64_t)gridDim.x * RPB) {
+  for (; row0 < a.rows; row0 += step) {
+    cur = next;
+    if (row0 + step < a.rows) fetch(row0 + step, next);
     const bool live = row0 + group < a.rows;
-    const int row = live ? (int)row0 + group : a.rows - 1;
-    const T *x = row_at<const T>(a.x, a.heads, row), *dy = row_at<const T>(a.dy, a.heads, row);
-    const float mean = a.rms ? 0.f : a.mean_in[row], rstd = a.rstd_in[row];
-    float xh[CH][V], g[CH][V];
+    if (RPB > 1 && !live) {
+      cur.mean = cur.rstd = 0.f;
+#pragma unroll
+      for (int c = 0; c < CH; ++c) cur.x[c] = cur.g[c] = u32x4{0, 0, 0, 0};
+    }
     float sums[2] = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      load_vec(x + (c * LPR + lane) * V, cnt[c], mean, xh[c]);
-      load_vec(dy + (c * LPR + lane) * V, live ? cnt[c] : 0, 0.f, g[c]);
-    }
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
+      float xh[V], g[V];
+      unpack<T>(cur.x[c], xh);
+      unpack<T>(cur.g[c], g);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        xh[c][e] = (xh[c][e] - mean) * rstd;
-        dw[c][e] += g[c][e] * xh[c][e];
-        db[c][e] += g[c][e];
-        g[c][e] *= w[c][e];
-        sums[0] += g[c][e];
-        sums[1] += g[c][e] * xh[c][e];
+        xh[e] = (xh[e] - cur.mean) * cur.rstd;
+        dw[c][e] += g[e] * xh[e];
+        db[c][e] += g[e];
+        g[e] *= w[c][e];
       }
+      if (col.some[c]) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          sums[0] += e >= col.own[c] ? g[e] : 0.f;
+          sums[1] += e >= col.own[c] ? g[e] * xh[e] : 0.f;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          sums[0] += g[e];
+          sums[1] += g[e] * xh[e];
+        }
+      }
+    }
     RowSum<LPR, 2>::run(sums, slots, turn);
-    if (!live) continue;
     const float m0 = a.rms ? 0.f : sums[0] * inv_n, m1 = sums[1] * inv_n;
-    T *dx = row_at<T>(a.y, a.heads, row);
+    if (!live) continue;
+    T *dx = row_at<T>(a.y, a.heads, (int)row0 + group);
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      float o[V];
+      float xh[V], g[V], o[V];
+      // (or the compiler would keep what it unpacked before the barrier)
+      asm volatile("" : "+v"(cur.x[c]), "+v"(cur.g[c]));
+      unpack<T>(cur.x[c], xh);
+      unpack<T>(cur.g[c], g);
 #pragma unroll
-      for (int e = 0; e < V; ++e) o[e] = (g[c][e] - m0 - xh[c][e] * m1) * rstd;
-      store_vec(dx + (c * LPR + lane) * V, cnt[c], o);
+      for (int e = 0; e < V; ++e) o[e] = (g[e] * w[c][e] - m0 - (xh[e] - cur.mean) * cur.rstd * m1) * cur.rstd;
+      if (col.own[c] < V) store16(dx + col.e0[c], pack<T>(o));
     }
   }
   if (!a.part) return;
   float *part = a.part + (int64_t)blockIdx.x * 2 * a.n;
   if constexpr (RPB == 1) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      const int e0 = (c * LPR + lane) * V;
+    for (int c = 0; c < CH; ++c)
 #pragma unroll
       for (int e = 0; e < V; ++e)
-        if (e < cnt[c]) {
-          part[e0 + e] = dw[c][e];
-          part[a.n + e0 + e] = db[c][e];
+        if (e >= col.own[c]) {
+          part[col.e0[c] + e] = dw[c][e];
+          part[a.n + col.e0[c] + e] = db[c][e];
         }
-    }
   } else {
     // the groups' sums, added in the order of the groups
     __shared__ float lds[256 * V];
@@ -201,20 +317,22 @@ __global__ __launch_bounds__(LPR < 256 ? 256 : LPR) void norm_bwd_kernel(NormArg
         for (int e = 0; e < V; ++e) lds[group * (LPR * V) + lane * V + e] = k ? db[c][e] : dw[c][e];
         __syncthreads();
         for (int i = threadIdx.x; i < LPR * V; i += 256) {
-          const int e0 = c * LPR * V + i;
+          // element i of the group's vectors: of lane i / V, its own or not
+          const int at = (c * LPR + i / V) * V, e0 = at + V <= a.n ? at : a.n - V, e = e0 + i % V;
           float s = 0.f;
 #pragma unroll
           for (int g2 = 0; g2 < RPB; ++g2) s += lds[g2 * (LPR * V) + i];
-          if (e0 < a.n) part[k * a.n + e0] = s;
+          if (at < a.n && e >= at) part[k * a.n + e] = s;
         }
       }
   }
 }
 
-// Rows wider than the lanes of a workgroup hold: several passes over a row,
-// which is in the caches after the first.
+// Rows wider than the lanes of a workgroup hold (or less than a vector wide):
+// several passes over a row, which is in the caches after the first.
 template <class T>
 __global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(NormArgs a) {
+  constexpr int V = kVec<T>;
   __shared__ float slots[2 * 17];
   int turn = 0;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -223,22 +341,32 @@ __global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(NormArgs a) {
     float mean = 0.f;
     if (!a.rms) {
       float s[1] = {0.f};
-      for (int i = threadIdx.x; i < a.n; i += 1024) s[0] += to_f32(x[i]);
+      for (int i = threadIdx.x * V; i < a.n; i += 1024 * V) {
+        float v[V];
+        load_vec(x + i, a.n - i, 0.f, v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) s[0] += v[e];
+      }
       RowSum<1024, 1>::run(s, slots, turn);
       mean = s[0] / (float)a.n;
     }
     float sq[1] = {0.f};
-    for (int i = threadIdx.x; i < a.n; i += 1024) {
-      const float d = to_f32(x[i]) - mean;
-      sq[0] += d * d;
+    for (int i = threadIdx.x * V; i < a.n; i += 1024 * V) {
+      float v[V];
+      load_vec(x + i, a.n - i, mean, v);
+#pragma unroll
+      for (int e = 0; e < V; ++e) sq[0] += (v[e] - mean) * (v[e] - mean);
     }
     RowSum<1024, 1>::run(sq, slots, turn);
-    const float rstd = 1.f / sqrtf(sq[0] / (float)a.n + a.eps);
-    for (int i = threadIdx.x; i < a.n; i += 1024) {
-      float w[1], b[1];
-      load_weights<1>(a.w, a.w_f32, i, 1, 1.f, w);
-      load_weights<1>(a.b, a.w_f32, i, 1, 0.f, b);
-      y[i] = (T)((to_f32(x[i]) - mean) * rstd * w[0] + b[0]);
+    const float rstd = __builtin_amdgcn_rsqf(sq[0] / (float)a.n + a.eps);
+    for (int i = threadIdx.x * V; i < a.n; i += 1024 * V) {
+      float v[V], w[V], b[V];
+      load_vec(x + i, a.n - i, 0.f, v);
+      some_weights<V>(a.w, a.w_f32, i, a.n - i, 1.f, w);
+      some_weights<V>(a.b, a.w_f32, i, a.n - i, 0.f, b);
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[e] = (v[e] - mean) * rstd * w[e] + b[e];
+      store_vec(y + i, a.n - i, v);
     }
     if (threadIdx.x == 0) {
       if (a.mean) a.mean[row] = mean;
@@ -249,136 +377,213 @@ __global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(NormArgs a) {
 
 template <class T>
 __global__ __launch_bounds__(1024) void norm_bwd_wide_kernel(NormArgs a) {
+  constexpr int V = kVec<T>;
   __shared__ float slots[2 * 2 * 17];
   int turn = 0;
-  float *part = a.part ? a.part + (int64_t)blockIdx.x * 2 * a.n : nullptr;
-  bool first = true;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const T *x = row_at<const T>(a.x, a.heads, (int)row), *dy = row_at<const T>(a.dy, a.heads, (int)row);
     T *dx = row_at<T>(a.y, a.heads, (int)row);
     const float mean = a.rms ? 0.f : a.mean_in[row], rstd = a.rstd_in[row];
     float sums[2] = {0.f, 0.f};
-    for (int i = threadIdx.x; i < a.n; i += 1024) {
-      float w[1];
-      load_weights<1>(a.w, a.w_f32, i, 1, 1.f, w);
-      const float h = to_f32(dy[i]) * w[0];
-      sums[0] += h;
-      sums[1] += h * ((to_f32(x[i]) - mean) * rstd);
+    float v[V], g[V], w[V];
+    for (int i = threadIdx.x * V; i < a.n; i += 1024 * V) {
+      load_vec(x + i, a.n - i, 0.f, v);
+      load_vec(dy + i, a.n - i, 0.f, g);
+      some_weights<V>(a.w, a.w_f32, i, a.n - i, 1.f, w);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float h = g[e] * w[e];
+        sums[0] += h;
+        sums[1] += h * ((v[e] - mean) * rstd);
+      }
     }
     RowSum<1024, 2>::run(sums, slots, turn);
     const float m0 = a.rms ? 0.f : sums[0] / (float)a.n, m1 = sums[1] / (float)a.n;
-    for (int i = threadIdx.x; i < a.n; i += 1024) {
-      float w[1];
-      load_weights<1>(a.w, a.w_f32, i, 1, 1.f, w);
-      const float g = to_f32(dy[i]), xh = (to_f32(x[i]) - mean) * rstd;
-      if (part) {                                    // (this thread's own columns: no other reads or writes them)
-        part[i] = g * xh + (first ? 0.f : part[i]);
-        part[a.n + i] = g + (first ? 0.f : part[a.n + i]);
-      }
-      dx[i] = (T)((g * w[0] - m0 - xh * m1) * rstd);
+    for (int i = threadIdx.x * V; i < a.n; i += 1024 * V) {
+      load_vec(x + i, a.n - i, 0.f, v);
+      load_vec(dy + i, a.n - i, 0.f, g);
+      some_weights<V>(a.w, a.w_f32, i, a.n - i, 1.f, w);
+#pragma unroll
+      for (int e = 0; e < V; ++e) v[e] = (g[e] * w[e] - m0 - (v[e] - mean) * rstd * m1) * rstd;
+      store_vec(dx + i, a.n - i, v);
     }
-    first = false;
   }
 }
 
-// dw, db: the sum of the workgroups' parts, 32 columns a workgroup, the parts
-// in 32 strands that are then added in order.
-__global__ __launch_bounds__(1024) void norm_weight_kernel(const float *part, int parts, int n, void *dw, void *db, bool f32) {
-  __shared__ float lds[32][33];
-  const int col = blockIdx.x * 32 + (threadIdx.x & 31), strand = threadIdx.x >> 5, which = blockIdx.y;
-  float s = 0.f;
-  if (col < n)
-    for (int p = strand; p < parts; p += 32) s += part[((int64_t)p * 2 + which) * n + col];
-  lds[strand][threadIdx.x & 31] = s;
+// Sums of V columns over the strands of a workgroup (strand: the threads that
+// share threadIdx.x / LANES) into out[i], i < LANES V: by shuffles within a
+// wave, the waves in order.
+template <int LANES, int V>
+__device__ __forceinline__ void strand_sums(float (&s)[V], float (*lds)[LANES * V], float *out) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   __syncthreads();
-  if (threadIdx.x >= 32 || col >= n) return;
-  s = 0.f;
 #pragma unroll
-  for (int p = 0; p < 32; ++p) s += lds[p][threadIdx.x];
-  void *out = which ? db : dw;
-  if (!out) return;
-  if (f32) ((float *)out)[col] = s;
-  else ((bf16 *)out)[col] = (bf16)s;
+  for (int e = 0; e < V; ++e) {
+#pragma unroll
+    for (int m = LANES; m < 64; m <<= 1) s[e] += __shfl_xor(s[e], m);
+    if (lane < LANES) lds[wave][lane * V + e] = s[e];
+  }
+  __syncthreads();
+  if (threadIdx.x < LANES * V) {
+    float t = 0.f;
+#pragma unroll
+    for (int p = 0; p < 16; ++p) t += lds[p][threadIdx.x];
+    *out = t;
+  }
 }
 
-// Lanes of a row, and its vectors a lane; 0 lanes: the wide kernels.  1024
-// lanes hold 16 elements each (four waves a SIMD leave 128 registers a lane,
-// and the backward wants six an element).
+__device__ __forceinline__ void store_weight(void *out, bool f32, int c, float t) {
+  if (f32) ((float *)out)[c] = t;
+  else ((bf16 *)out)[c] = (bf16)t;
+}
+
+// dw, db: the sum of the workgroups' parts, 32 columns a workgroup, the parts
+// in 128 strands.
+__global__ __launch_bounds__(1024) void norm_weight_kernel(const float *part, int parts, int n, void *dw, void *db, bool f32) {
+  __shared__ float lds[16][32];
+  const int which = blockIdx.y, col = blockIdx.x * 32 + (threadIdx.x & 7) * 4;
+  void *out = which ? db : dw;
+  if (!out) return;
+  float s[4] = {0.f, 0.f, 0.f, 0.f}, t;
+  if (col < n) {
+#pragma unroll 8
+    for (int p = threadIdx.x >> 3; p < parts; p += 128) {
+      float v[4];
+      load_vec(part + ((int64_t)p * 2 + which) * n + col, n - col, 0.f, v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += v[e];
+    }
+  }
+  strand_sums<8, 4>(s, lds, &t);
+  const int c = blockIdx.x * 32 + threadIdx.x;
+  if (threadIdx.x < 32 && c < n) store_weight(out, f32, c, t);
+}
+
+// dw, db straight from x and dy: V 8 columns a workgroup, the rows in 128
+// strands.  Where rows are few and wide, their parts would be as much memory
+// as the rows themselves, which lie in the caches for the pass that follows.
+template <class T>
+__global__ __launch_bounds__(1024) void norm_columns_kernel(NormArgs a) {
+  constexpr int V = kVec<T>;
+  __shared__ float lds[16][8 * V];
+  const int col = blockIdx.x * (8 * V) + (threadIdx.x & 7) * V, cnt = a.n - col;
+  float dw[V] = {}, db[V] = {}, t;
+  if (cnt > 0) {
+#pragma unroll 4
+    for (int64_t row = threadIdx.x >> 3; row < a.rows; row += 128) {
+      float x[V], g[V];
+      load_vec(row_at<const T>(a.x, a.heads, (int)row) + col, cnt, 0.f, x);
+      load_vec(row_at<const T>(a.dy, a.heads, (int)row) + col, cnt, 0.f, g);
+      const float mean = a.rms ? 0.f : a.mean_in[row], rstd = a.rstd_in[row];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        dw[e] += g[e] * ((x[e] - mean) * rstd);
+        db[e] += g[e];
+      }
+    }
+  }
+  const int c = blockIdx.x * (8 * V) + threadIdx.x;
+  const bool mine = threadIdx.x < 8 * V && c < a.n;
+  if (a.dw) {
+    strand_sums<8, V>(dw, lds, &t);
+    if (mine) store_weight(a.dw, a.w_f32, c, t);
+  }
+  if (a.db) {
+    strand_sums<8, V>(db, lds, &t);
+    if (mine) store_weight(a.db, a.w_f32, c, t);
+  }
+}
+
+// Lanes of a row, and its vectors a lane; 0 lanes: the wide kernels.
 struct NormShape {
   int lpr, ch;
+  int rows() const { return lpr > 0 && lpr < 256 ? 256 / lpr : 1; }   // of a workgroup
 };
 
-NormShape norm_shape(int n, bool f32) {
+#ifndef FSHAPES
+#define FSHAPES {16, 1}, {16, 2}, {64, 1}, {64, 2}, {64, 3}, {64, 4}, {128, 3}, {128, 4}, {512, 2}, {1024, 2}, {1024, 4}
+#endif
+#ifndef BSHAPES
+#define BSHAPES {16, 1}, {16, 2}, {64, 1}, {64, 2}, {64, 3}, {64, 4}, {128, 4}, {512, 2}, {512, 4}, {1024, 4}
+#endif
+constexpr NormShape kFwdShapes[] = {FSHAPES}, kBwdShapes[] = {BSHAPES};
+
+template <int N>
+NormShape norm_shape(const NormShape (&shapes)[N], int n, bool f32) {
   const int v = f32 ? 4 : 8, vecs = (n + v - 1) / v;
-  for (int lpr : {16, 64, 256, 1024})
-    for (int ch : {1, 2, 4})
-      if (lpr * ch >= vecs && (lpr < 1024 || ch * v <= 16)) return {lpr, ch};
+  if (n < v) return {0, 0};
+  for (const NormShape s : shapes)
+    if (s.lpr * s.ch >= vecs && (s.lpr < 1024 || s.ch * v <= 16)) return s;
   return {0, 0};
 }
 
-template <class T, int LPR>
-void launch_fwd(int ch, int grid, const NormArgs &a, hipStream_t s) {
-  constexpr int threads = LPR < 256 ? 256 : LPR;
-  if (ch == 1) norm_fwd_kernel<T, LPR, 1><<<grid, threads, 0, s>>>(a);
-  else if (ch == 2) norm_fwd_kernel<T, LPR, 2><<<grid, threads, 0, s>>>(a);
-  else if constexpr (LPR < 1024 || sizeof(T) == 4) norm_fwd_kernel<T, LPR, 4><<<grid, threads, 0, s>>>(a);
-}
-
-template <class T, int LPR>
-void launch_bwd(int ch, int grid, const NormArgs &a, hipStream_t s) {
-  constexpr int threads = LPR < 256 ? 256 : LPR;
-  if (ch == 1) norm_bwd_kernel<T, LPR, 1><<<grid, threads, 0, s>>>(a);
-  else if (ch == 2) norm_bwd_kernel<T, LPR, 2><<<grid, threads, 0, s>>>(a);
-  else if constexpr (LPR < 1024 || sizeof(T) == 4) norm_bwd_kernel<T, LPR, 4><<<grid, threads, 0, s>>>(a);
+// f(lanes, vectors) of the shape s among `shapes`, as compile-time numbers.
+template <const auto &SHAPES, size_t I = 0, class F>
+void with_shape(NormShape s, F f) {
+  if constexpr (I < sizeof(SHAPES) / sizeof(SHAPES[0])) {
+    if (s.lpr == SHAPES[I].lpr && s.ch == SHAPES[I].ch)
+      f(std::integral_constant<int, SHAPES[I].lpr>(), std::integral_constant<int, SHAPES[I].ch>());
+    else
+      with_shape<SHAPES, I + 1>(s, f);
+  }
 }
 
 template <class T>
 hipError_t fwd(const NormArgs &a, hipStream_t s) {
-  const NormShape sh = norm_shape(a.n, sizeof(T) == 4);
-  const int rpb = sh.lpr > 0 && sh.lpr < 256 ? 256 / sh.lpr : 1;
-  int64_t grid = ((int64_t)a.rows + rpb - 1) / rpb;
-  if (grid > 4096) grid = 4096;
-  switch (sh.lpr) {
-    case 16: launch_fwd<T, 16>(sh.ch, (int)grid, a, s); break;
-    case 64: launch_fwd<T, 64>(sh.ch, (int)grid, a, s); break;
-    case 256: launch_fwd<T, 256>(sh.ch, (int)grid, a, s); break;
-    case 1024: launch_fwd<T, 1024>(sh.ch, (int)grid, a, s); break;
-    default: norm_fwd_wide_kernel<T><<<(int)grid, 1024, 0, s>>>(a);
-  }
+  const NormShape sh = norm_shape(kFwdShapes, a.n, sizeof(T) == 4);
+  const int64_t groups = ((int64_t)a.rows + sh.rows() - 1) / sh.rows();
+  int64_t grid = groups / kFwdTurns > kFwdLeast ? groups / kFwdTurns : groups < kFwdLeast ? groups : kFwdLeast;
+  if (grid > kFwdMost) grid = kFwdMost;
+  if (sh.lpr == 0)
+    norm_fwd_wide_kernel<T><<<(int)grid, 1024, 0, s>>>(a);
+  else
+    with_shape<kFwdShapes>(sh, [&](auto lpr, auto ch) {
+      constexpr int L = decltype(lpr)::value, C = decltype(ch)::value;
+      if constexpr (L < 1024 || C * kVec<T> <= 16) norm_fwd_kernel<T, L, C><<<(int)grid, kBlock<L>, 0, s>>>(a);
+    });
   return hipGetLastError();
 }
 
 template <class T>
 hipError_t bwd(const NormArgs &a, hipStream_t s) {
-  int parts = 0;
-  if (a.rows > 0) {
-    const NormShape sh = norm_shape(a.n, sizeof(T) == 4);
-    parts = norm_bwd_parts(a.rows, a.n, sizeof(T) == 4);
-    switch (sh.lpr) {
-      case 16: launch_bwd<T, 16>(sh.ch, parts, a, s); break;
-      case 64: launch_bwd<T, 64>(sh.ch, parts, a, s); break;
-      case 256: launch_bwd<T, 256>(sh.ch, parts, a, s); break;
-      case 1024: launch_bwd<T, 1024>(sh.ch, parts, a, s); break;
-      default: norm_bwd_wide_kernel<T><<<parts, 1024, 0, s>>>(a);
-    }
+  constexpr bool f32 = sizeof(T) == 4;
+  const bool weights = a.dw || a.db;
+  const int parts = norm_bwd_parts(a.rows, a.n, f32);
+  if (weights && parts == 0) {
+    norm_columns_kernel<T><<<(a.n + 8 * kVec<T> - 1) / (8 * kVec<T>), 1024, 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (a.dw || a.db) {
+  if (a.rows == 0) return hipSuccess;
+  const NormShape sh = norm_shape(kBwdShapes, a.n, f32);
+  const int64_t groups = ((int64_t)a.rows + sh.rows() - 1) / sh.rows();
+  NormArgs b = a;
+  if (parts == 0) b.part = nullptr;
+  int grid = b.part ? parts : (int)(groups < kNormMaxParts ? groups : kNormMaxParts);
+  if (sh.lpr == 0)
+    norm_bwd_wide_kernel<T><<<grid, 1024, 0, s>>>(b);
+  else
+    with_shape<kBwdShapes>(sh, [&](auto lpr, auto ch) {
+      constexpr int L = decltype(lpr)::value, C = decltype(ch)::value;
+      if constexpr (L < 1024 || C * kVec<T> <= 16) norm_bwd_kernel<T, L, C><<<grid, kBlock<L>, 0, s>>>(b);
+    });
+  hipError_t e = hipGetLastError();
+  if (e == hipSuccess && b.part) {
     norm_weight_kernel<<<dim3((a.n + 31) / 32, 2), 1024, 0, s>>>(a.part, parts, a.n, a.dw, a.db, a.w_f32);
-    return hipGetLastError();
+    e = hipGetLastError();
   }
-  return hipSuccess;
+  return e;
 }
 
 }  // namespace
 
 int norm_bwd_parts(int64_t rows, int n, bool f32) {
-  const NormShape sh = norm_shape(n, f32);
-  const int rpb = sh.lpr > 0 && sh.lpr < 256 ? 256 / sh.lpr : 1;
-  const int64_t groups = (rows + rpb - 1) / rpb;
-  const int most = sh.lpr == 0 || sh.lpr == 1024 ? kNormMaxParts / 4 : kNormMaxParts;
-  return (int)(groups < most ? groups : most);
+  const NormShape sh = norm_shape(kBwdShapes, n, f32);
+  if (rows == 0 || sh.lpr == 0 || (rows <= 512 && rows * 8 <= n)) return 0;
+  const int64_t groups = (rows + sh.rows() - 1) / sh.rows();
+  int per_cu = sh.lpr > 256 || sh.ch > 2 ? 1 : sh.ch == 2 ? 2 : 3;
+  while (per_cu > 1 && groups < 4 * 256 * per_cu) --per_cu;
+  return (int)(groups < 256 * per_cu ? groups : 256 * per_cu);
 }
 
 hipError_t launch_norm_fwd(bool f32, const NormArgs &a, hipStream_t s) { return f32 ? fwd<float>(a, s) : fwd<bf16>(a, s); }

@@ -220,7 +220,8 @@ struct NormArgs {
   void *dw, *db;
   float *part;               // [parts][2][n]: dw, db
 };
-// Workgroups of the backward (rows > 0).
+// Workgroups of the backward that leave a partial sum; 0: dw and db are formed
+// without any.
 int norm_bwd_parts(int64_t rows, int n, bool f32);
 hipError_t launch_norm_fwd(bool f32, const NormArgs &a, hipStream_t s);
 hipError_t launch_norm_bwd(bool f32, const NormArgs &a, hipStream_t s);

@@ -167,7 +167,6 @@ nsp_status check_norm(nsp_norm_kind kind, nsp_dtype dtype, nsp_dtype w_dtype, in
 size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 size_t norm_ws(int64_t rows, int32_t n) {   // the larger of the two types' needs
-  if (rows == 0) return 0;
   const int a = nsp::norm_bwd_parts(rows, n, false), b = nsp::norm_bwd_parts(rows, n, true);
   return align256((size_t)(a > b ? a : b) * 2 * (size_t)n * sizeof(float));
 }

@@ -146,7 +146,7 @@ def test_workspace_sizes():
     for _ in range(300):
         T, H, n = int(math.exp(rng.uniform(0, 14))), int(rng.integers(1, 40)), int(math.exp(rng.uniform(0, math.log(65536))))
         w = nsp.nsp_norm_bwd_workspace(T, H, n)
-        assert 8 * n <= w <= 8192 * n + 1024 and w % 256 == 0
+        assert 0 <= w <= 8192 * n + 1024 and w % 256 == 0
         V, top = int(math.exp(rng.uniform(0, 14))), int(rng.integers(0, 65))
         w = nsp.nsp_token_logp_workspace(T, V, top)
         assert 0 <= w <= 4 << 20 and w % 256 == 0
