@@ -614,7 +614,7 @@ size_t nsp_token_logp_workspace(int64_t n_tokens, int32_t vocab, int32_t top);
  * masked vocabulary: they have p = 0 and are no alternatives (places past the
  * last logit above hold index -1 and -inf).  A row of nothing else has lse =
  * -inf, entropy 0, and logp = -inf unless its target is ignored.  A row with a
- * NaN or +inf has lse and entropy NaN, and logp and the alternatives' values
+ * NaN or +inf (or 2^126 / scale and more) has lse and entropy NaN, and logp and the alternatives' values
  * too (NaN itself is never an alternative).
  *   dtype       of the logits (NSP_BF16 or NSP_F32)
  *   row_stride  >= 0 (rows may coincide)
