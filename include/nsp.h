@@ -508,7 +508,7 @@ typedef enum { NSP_ROTARY_HALF = 0, NSP_ROTARY_PAIRS = 1 } nsp_rotary_layout;
  * nsp_rotary_bwd is the gradient: the transposed rotation (angle -a, the same
  * scale) of dq_out, dk_out into dq, dk.
  *   dtype       of every tensor (NSP_BF16 or NSP_F32)
- *   head_dim    1 .. 1024;  rot_dim even, 2 .. head_dim
+ *   head_dim    1 .. 256;  rot_dim even, 2 .. head_dim
  *   freqs       DEVICE, rot_dim / 2 doubles, as nsp_rotary_frequencies (or
  *               any other rule) gives them
  *   scale       amplitude of the rotated part, finite
@@ -517,7 +517,7 @@ typedef enum { NSP_ROTARY_HALF = 0, NSP_ROTARY_PAIRS = 1 } nsp_rotary_layout;
  *   k, k_out    k_heads (>= 0) heads; NULL with k_heads = 0; in place allowed
  * q and k (and their outputs) may be parts of one tensor; writing into a part
  * that another argument reads is the caller's race.
- * Errors: NSP_EINVAL, NSP_EUNSUPPORTED (head_dim > 1024), NSP_EHIP.
+ * Errors: NSP_EINVAL, NSP_EUNSUPPORTED (head_dim > 256), NSP_EHIP.
  */
 nsp_status nsp_rotary_fwd(nsp_rotary_layout layout, nsp_dtype dtype, int64_t n_tokens, int32_t head_dim,
                           int32_t rot_dim, const double *freqs, float scale, const int64_t *positions,

@@ -191,6 +191,8 @@ struct RowView {
   int64_t ts, hs;
 };
 
+// Widest head of a rotation: 64 lanes of 16 bytes in float32.
+constexpr int kRotaryMaxDim = 256;
 struct RotaryArgs {
   RowView x[2], y[2];        // queries, keys
   int64_t n_tokens;
@@ -239,6 +241,7 @@ struct LogpArgs {
   float *logp, *lse, *entropy, *top_logp;
   int64_t *top_index;
   int32_t parts, part_len;   // parts a row, elements a part
+  FastDiv by_parts;
   float4 *part_sums;         // [row][part]: reference, sum, weighted sum
   uint64_t *part_top;        // [row][part][top]
 };

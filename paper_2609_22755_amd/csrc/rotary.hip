@@ -5,12 +5,15 @@
 // cosine in float32, of an angle that is reduced to a turn in 64 bits, are
 // worth some 60 instructions, as much as memory gives time for in two vectors
 // of eight elements.  A token's angles are the same for all its heads, so a
-// workgroup takes a few whole tokens, forms their (cos, sin) once, in LDS, and
-// then turns all heads of these tokens with them.
+// wave takes a token (or, where there are few, a run of a token's heads): its
+// lanes form the pairs' (cos, sin) once, each some of them, pass them through
+// LDS, and keep those of their own columns in registers for all its heads.
 //
-// A task is one vector (16 bytes) of each half of a head, or one vector of
-// neighbouring pairs; the unrotated rest of a head is copied by tasks of one
-// vector (none in place).
+// A lane holds one vector (16 bytes) of a head, 64 / (vectors of a head) heads a
+// wave at a time, so every load and store of a wave is one run of memory
+// wherever the heads lie side by side; the other half of a pair comes from the
+// lane that holds it.  (A lane that loaded both its halves itself, in runs of
+// half a head, left half-used lines behind: heads of 96, 3.0 TB/s.)
 #include "nsp_internal.hpp"
 #include "row_common.hpp"
 
@@ -18,79 +21,121 @@ namespace nsp {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int64_t kMaxGrid = 1 << 22;   // workgroups of a launch (its threads stay below 2^32)
+constexpr int kWaves = kThreads / 64;
+constexpr int kMaxGrid = 1 << 20;
 
 struct RotaryShape {
-  int tokens;                // of a workgroup
-  int rot_tasks, row_tasks;  // of a head row: rotated, all
-  FastDiv half, row, token;  // pairs of a token, tasks of a row, rows of a token
+  int vecs, at_once;         // vectors of a head, heads of a wave at a time
+  int chunks, run;           // a token's heads in `chunks` runs of `run`
+  FastDiv by_vecs, by_chunks;
 };
 
-template <class T, bool PAIRS>
+// What one wave wrote to LDS is there for its other lanes (which run in step).
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// WHOLE: halves (or rotated parts) and heads are whole numbers of vectors.
+template <class T, bool PAIRS, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryShape sh) {
-  extern __shared__ float2 turn[];   // [token][pair]
   constexpr int V = kVec<T>;
-  for (int64_t t0 = (int64_t)blockIdx.x * sh.tokens; t0 < a.n_tokens; t0 += (int64_t)gridDim.x * sh.tokens) {
-    const int nt = (int)min((int64_t)sh.tokens, a.n_tokens - t0);
-    for (int i = threadIdx.x; i < nt * a.half; i += kThreads) {
-      const int tl = sh.half.quot(i), p = i - tl * a.half;
-      const double angle = (double)a.positions[t0 + tl] * a.freqs[p];
-      const double turns = angle * 0.15915494309189533576888376337251;   // 1 / (2 pi)
+  constexpr int U = 3;       // heads of a lane in flight
+  __shared__ float2 angles[kWaves][kRotaryMaxDim / 2];
+  __shared__ u32x4 stage[WHOLE ? 1 : kWaves][WHOLE ? 1 : 64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int slot = sh.by_vecs.quot(lane), vec = lane - slot * sh.vecs, e0 = vec * V;   // the lane's head of those at once, its vector
+  const int rot = 2 * a.half, heads = a.heads[0] + a.heads[1];
+  const bool turned = e0 < rot;
+  const int cnt = min(V, a.head_dim - e0);
+  const int64_t units = a.n_tokens * sh.chunks;
+  for (int64_t unit = (int64_t)blockIdx.x * kWaves + wave; unit < units; unit += (int64_t)gridDim.x * kWaves) {
+    const int token = (int)sh.by_chunks.quot((uint32_t)unit), chunk = (int)unit - token * sh.chunks;
+    const int end = min(heads, (chunk + 1) * sh.run);
+    int head = chunk * sh.run + slot;
+    const auto mine = [&](int h) { return slot < sh.at_once && h < end; };
+    const auto place = [&](const RowView (&v)[2], int h) {
+      const bool key = h >= a.heads[0];
+      const RowView &r = key ? v[1] : v[0];
+      return r.data + ((int64_t)token * r.ts + (int64_t)(key ? h - a.heads[0] : h) * r.hs + e0) * (int)sizeof(T);
+    };
+    u32x4 raw[U];
+    const auto load = [&](int h0) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int h = h0 + i * sh.at_once;
+        if (!mine(h)) continue;
+        const T *x = (const T *)place(a.x, h);
+        if (WHOLE || cnt == V) {
+          raw[i] = load16(x);
+        } else {
+          float v[V];
+          load_some(x, cnt, 0.f, v);
+          raw[i] = pack<T>(v);
+        }
+      }
+    };
+    load(head);                                  // (on its way while the angles are formed)
+    const double position = (double)a.positions[token];
+    for (int p = lane; p < a.half; p += 64) {
+      const double turns = position * a.freqs[p] * 0.15915494309189533576888376337251;   // 1 / (2 pi)
       float s, c;
       sincospif(2.f * (float)(turns - rint(turns)), &s, &c);
-      turn[i] = make_float2(c * a.scale, s * (a.scale * a.sign));
+      angles[wave][p] = make_float2(c * a.scale, s * (a.scale * a.sign));
     }
-    __syncthreads();
-
-    const int rows = a.heads[0] + a.heads[1];
-    const int total = nt * rows * sh.row_tasks;
-    for (int i = threadIdx.x; i < total; i += kThreads) {
-      const int r = sh.row.quot(i), c = i - r * sh.row_tasks;
-      const int tl = sh.token.quot(r);
-      int h = r - tl * rows;
-      const int kind = h >= a.heads[0];
-      h -= kind ? a.heads[0] : 0;
-      const RowView xv = kind ? a.x[1] : a.x[0], yv = kind ? a.y[1] : a.y[0];
-      const T *x = (const T *)xv.data + (t0 + tl) * xv.ts + h * xv.hs;
-      T *y = (T *)yv.data + (t0 + tl) * yv.ts + h * yv.hs;
-      if (c >= sh.rot_tasks) {
-        if (!(kind ? a.copy[1] : a.copy[0])) continue;
-        const int e0 = 2 * a.half + (c - sh.rot_tasks) * V, cnt = a.head_dim - e0;
-        if (cnt >= V) {
-          store16(y + e0, load16(x + e0));
+    wave_sync();
+    // y = x cos + other sin', sin' with the sign of the element's half
+    float cs[V], sn[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const int i = e0 + e;
+      const bool second = PAIRS ? e & 1 : WHOLE ? e0 >= a.half : i >= a.half;
+      const int p = PAIRS ? i >> 1 : second ? i - a.half : i;
+      const float2 w = i < rot ? angles[wave][p] : make_float2(1.f, 0.f);
+      cs[e] = w.x;
+      sn[e] = second ? w.y : -w.y;
+    }
+    wave_sync();                                 // before the next unit's angles
+    for (; __any(mine(head)); head += U * sh.at_once) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int h = head + i * sh.at_once;
+        float x[V], other[V], y[V];
+        unpack<T>(raw[i], x);
+        if constexpr (PAIRS && WHOLE) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) other[e] = x[e ^ 1];
+        } else if constexpr (WHOLE) {
+          const int from = e0 < a.half ? lane + a.half / V : lane - a.half / V;
+          u32x4 o;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[k] = (uint32_t)__shfl((int)raw[i][k], from);
+          unpack<T>(o, other);
         } else {
-          for (int e = 0; e < cnt; ++e) y[e0 + e] = x[e0 + e];
+          stage[wave][lane] = raw[i];
+          wave_sync();
+          const T *row = (const T *)&stage[wave][min(slot, sh.at_once - 1) * sh.vecs];
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const int at = e0 + e, o = PAIRS ? at ^ 1 : at < a.half ? at + a.half : at - a.half;
+            other[e] = at < rot ? to_f32(row[o]) : 0.f;
+          }
+          wave_sync();
         }
-        continue;
+#pragma unroll
+        for (int e = 0; e < V; ++e) y[e] = WHOLE || e0 + e < rot ? x[e] * cs[e] + other[e] * sn[e] : x[e];
+        if (!mine(h)) continue;
+        T *out = (T *)place(a.y, h);
+        if (turned) {
+          if (WHOLE || cnt == V) store16(out, pack<T>(y));
+          else store_some(out, cnt, y);
+        } else if (h < a.heads[0] ? a.copy[0] : a.copy[1]) {
+          if (WHOLE || cnt == V) store16(out, raw[i]);
+          else store_some(out, cnt, x);
+        }
       }
-      const float2 *cs = turn + tl * a.half;
-      if constexpr (PAIRS) {
-        const int e0 = c * V, cnt = 2 * a.half - e0;
-        float v[V], o[V];
-        load_vec(x + e0, cnt, 0.f, v);
-  #pragma unroll
-        for (int e = 0; e < V / 2; ++e) {
-          const float2 w = 2 * e < cnt ? cs[e0 / 2 + e] : make_float2(0.f, 0.f);
-          o[2 * e] = v[2 * e] * w.x - v[2 * e + 1] * w.y;
-          o[2 * e + 1] = v[2 * e + 1] * w.x + v[2 * e] * w.y;
-        }
-        store_vec(y + e0, cnt, o);
-      } else {
-        const int e0 = c * V, cnt = a.half - e0;
-        float v1[V], v2[V], o1[V], o2[V];
-        load_vec(x + e0, cnt, 0.f, v1);
-        load_vec(x + a.half + e0, cnt, 0.f, v2);
-  #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float2 w = e < cnt ? cs[e0 + e] : make_float2(0.f, 0.f);
-          o1[e] = v1[e] * w.x - v2[e] * w.y;
-          o2[e] = v2[e] * w.x + v1[e] * w.y;
-        }
-        store_vec(y + e0, cnt, o1);
-        store_vec(y + a.half + e0, cnt, o2);
-      }
+      load(head + U * sh.at_once);
     }
-    __syncthreads();   // before the next tokens' angles
   }
 }
 
@@ -98,18 +143,21 @@ template <class T, bool PAIRS>
 hipError_t launch(const RotaryArgs &a, hipStream_t s) {
   constexpr int V = kVec<T>;
   RotaryShape sh;
-  const int rows = a.heads[0] + a.heads[1];
-  sh.rot_tasks = ((PAIRS ? 2 : 1) * a.half + V - 1) / V;
-  const bool copies = a.copy[0] || a.copy[1];
-  sh.row_tasks = sh.rot_tasks + (copies ? (a.head_dim - 2 * a.half + V - 1) / V : 0);
-  sh.tokens = 1;
-  while (sh.tokens < 16 && 2 * sh.tokens * a.half <= kThreads && a.n_tokens / sh.tokens > 4096) sh.tokens *= 2;
-  sh.half = FastDiv(a.half);
-  sh.row = FastDiv(sh.row_tasks);
-  sh.token = FastDiv(rows);
-  int64_t grid = (a.n_tokens + sh.tokens - 1) / sh.tokens;
-  if (grid > kMaxGrid) grid = kMaxGrid;
-  rotary_kernel<T, PAIRS><<<dim3((uint32_t)grid), kThreads, sh.tokens * a.half * sizeof(float2), s>>>(a, sh);
+  sh.vecs = (a.head_dim + V - 1) / V;
+  sh.at_once = 64 / sh.vecs;
+  // a token's heads in runs, as long as there are not 16 waves a compute unit
+  const int heads = a.heads[0] + a.heads[1], rounds = (heads + sh.at_once - 1) / sh.at_once;
+  int chunks = (int)(4096 / a.n_tokens);
+  chunks = chunks < 1 ? 1 : chunks > rounds ? rounds : chunks;
+  sh.run = (rounds + chunks - 1) / chunks * sh.at_once;
+  sh.chunks = (heads + sh.run - 1) / sh.run;
+  sh.by_vecs = FastDiv(sh.vecs);
+  sh.by_chunks = FastDiv(sh.chunks);
+  const int64_t blocks = (a.n_tokens * sh.chunks + kWaves - 1) / kWaves;
+  const int grid = (int)(blocks < kMaxGrid ? blocks : kMaxGrid);
+  const bool whole = a.head_dim % V == 0 && (PAIRS ? 2 * a.half : a.half) % V == 0;
+  if (whole) rotary_kernel<T, PAIRS, true><<<grid, kThreads, 0, s>>>(a, sh);
+  else rotary_kernel<T, PAIRS, false><<<grid, kThreads, 0, s>>>(a, sh);
   return hipGetLastError();
 }
 

@@ -107,7 +107,8 @@ nsp_status rotary(bool bwd, nsp_rotary_layout layout, nsp_dtype dtype, int64_t n
     return set_error(NSP_EINVAL, "unknown rotary layout %d", (int)layout);
   NSP_TRY(check_dtype(dtype, "dtype"));
   if (head_dim < 1) return set_error(NSP_EINVAL, "head_dim = %d < 1", head_dim);
-  if (head_dim > 1024) return set_error(NSP_EUNSUPPORTED, "head_dim = %d > 1024", head_dim);
+  if (head_dim > nsp::kRotaryMaxDim)
+    return set_error(NSP_EUNSUPPORTED, "head_dim = %d > %d", head_dim, nsp::kRotaryMaxDim);
   if (rot_dim < 2 || rot_dim > head_dim || rot_dim % 2 != 0)
     return set_error(NSP_EINVAL, "rot_dim = %d is not even and in 2 .. head_dim = %d", rot_dim, head_dim);
   if (!std::isfinite(scale)) return set_error(NSP_EINVAL, "scale is not finite");

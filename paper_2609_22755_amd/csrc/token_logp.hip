@@ -13,17 +13,19 @@
 // hardly ever happens.
 //
 // Top alternatives, in two steps.  In the pass each lane keeps the largest
-// logit of its own elements, one comparison a vector.  The k-th largest of the
-// lanes' maxima is a bar that k logits at least reach, and that hardly more
-// do; so only the lanes whose maximum reaches it, about k of them, can hold
-// alternatives, and only their elements (a 256th of the row each) are read
-// once more.  A wave keeps the best keys (the logit in an order-keeping whole
-// number, then the complement of the index, 64 bits) one a lane, sorted; a key
-// that passes the k-th is inserted by the rank that a ballot gives, the keys
-// below moving one lane up.
+// logit of its own vectors, where it was, and the largest of its other
+// vectors.  The k-th largest of the lanes' maxima is a bar that k logits at
+// least reach, and that hardly more do: about k lanes have alternatives, nearly
+// all of them in their best vector alone, which is read once more (a lane whose
+// second vector reaches the bar too reads all of its own).  Whatever reaches the
+// bar is gathered in LDS as a key (the logit in an order-keeping whole number,
+// then the complement of the index, 64 bits), in any order: a key's rank is the
+// number of larger ones.  Only where more gather than there is room for (rows
+// of equal logits) a wave keeps its best keys one a lane, sorted, and inserts
+// what passes the k-th by the rank that a ballot gives.
 //
 // A workgroup takes a row, or a part of one where there are few rows; the
-// parts' sums and keys are then joined by one wave a row.
+// parts' sums and keys are then joined by one workgroup a row.
 #include "nsp_internal.hpp"
 #include "row_common.hpp"
 
@@ -136,104 +138,121 @@ __device__ __forceinline__ uint32_t kth_of(const uint32_t (&x)[N], int k) {
 
 // ----------------------------------------------------------------- forward --
 
-// The target of a row and its logit.
-struct Target {
-  bool given = false;
-  float z = 0.f;
-  template <class T>
-  __device__ __forceinline__ void load(const LogpArgs &a, int row, const T *z_row) {
-    if (!a.logp) return;
-    const int64_t y = a.targets[row];
-    given = y >= 0 && y < a.vocab;
-    if (given) z = to_f32(z_row[y]);
+constexpr int kRoom = kThreads;   // keys that a workgroup gathers
+
+struct Shared {
+  float4 sums[kWaves];
+  float firsts[kThreads];
+  uint64_t keys[kRoom];
+  int gathered;
+};
+
+// A lane's largest logit, the element its vector starts at, and the largest of
+// its other vectors.
+struct Largest {
+  float first = kNegInf, second = kNegInf;
+  int at = 0;
+  __device__ __forceinline__ void take(float most, int e0) {
+    second = fmaxf(second, fminf(first, most));
+    at = most > first ? e0 : at;
+    first = fmaxf(first, most);
   }
 };
 
-// What a row comes to, by one wave that holds its sums and keys.
-__device__ __forceinline__ void finish_row(const LogpArgs &a, int row, float c, const Sums &x, const TopKeys &top,
-                                           const Target &y) {
-  const int lane = threadIdx.x & 63;
-  const float log_s = log2f(x.s);
-  const bool none = x.s == 0.f;                 // nothing but masked logits
-  const auto logp = [&](float z) { return none ? kNegInf : (fmaf(z, c, -x.r) - log_s) * kLn2; };
-  if (lane == 0) {
-    a.lse[row] = none ? kNegInf : (x.r + log_s) * kLn2;
+// What a row comes to, from its sums (in every thread) and its alternatives
+// (thread i: the i-th, 0 if there is none).
+struct Finish {
+  float r, log_s, c;
+  bool none;                 // nothing but masked logits
+  __device__ __forceinline__ Finish(const Sums &x, float scale_log2) : r(x.r), log_s(log2f(x.s)), c(scale_log2), none(x.s == 0.f) {}
+  __device__ __forceinline__ float logp(float z) const { return none ? kNegInf : (fmaf(z, c, -r) - log_s) * kLn2; }
+  template <class T>
+  __device__ __forceinline__ void row(const LogpArgs &a, int row, const Sums &x, int64_t y, float z) const {
+    a.lse[row] = none ? kNegInf : (r + log_s) * kLn2;
     if (a.entropy) a.entropy[row] = none ? 0.f : (log_s - x.u / x.s) * kLn2;
-    if (a.logp) a.logp[row] = y.given ? logp(y.z) : 0.f;
+    if (a.logp) a.logp[row] = y >= 0 && y < a.vocab ? logp(z) : 0.f;
   }
-  if (lane < a.top) {
-    const int64_t at = (int64_t)row * a.top + lane;
-    const bool some = top.key != 0;
-    a.top_logp[at] = some ? logp(value_of((uint32_t)(top.key >> 32))) : kNegInf;
-    a.top_index[at] = some ? (int64_t)(int32_t)~(uint32_t)top.key : -1;
+  __device__ __forceinline__ void top(const LogpArgs &a, int row, int i, uint64_t key) const {
+    const int64_t at = (int64_t)row * a.top + i;
+    a.top_logp[at] = key ? logp(value_of((uint32_t)(key >> 32))) : kNegInf;
+    a.top_index[at] = key ? (int64_t)(int32_t)~(uint32_t)key : -1;
   }
-}
+};
 
-// The wave's alternatives among elements lo .. hi of a row, whose lanes'
-// largest are in `largest` (of all threads; mine: this thread's).
-template <class T>
-__device__ __forceinline__ TopKeys find_top(const T *z, int lo, int hi, int k, const float *largest, float mine) {
-  constexpr int V = kVec<T>;
+// put(i, key) of the i-th best key, i < k (0: there is none), by any thread.
+// each(bar, f) hands f the keys of the thread that reach the bar, whole waves
+// together (0: none).  first: the thread's largest logit.  Every thread of the
+// workgroup calls this; nothing else of `sh` is read any more.
+template <class Each, class Put>
+__device__ __forceinline__ void block_top(Shared &sh, int k, float first, Each each, Put put) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  sh.firsts[threadIdx.x] = first;
+  if (threadIdx.x == 0) sh.gathered = 0;
+  __syncthreads();
   uint32_t x[kWaves];
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) {
-    const float m = largest[i * 64 + lane];
+    const float m = sh.firsts[i * 64 + lane];
     x[i] = m > kMasked ? order_of(m) : 0;
   }
   const uint32_t bar = kth_of(x, k);
-  TopKeys top;
-  uint64_t lanes = __ballot(mine > kMasked && order_of(mine) >= bar);
-  // a lane's vectors, `each` lanes of the wave on one lane's
-  const int vecs = (hi - lo + kThreads * V - 1) / (kThreads * V);
-  int shift = 0;
-  while (shift < 6 && (1 << shift) < vecs) ++shift;
-  const int each = 1 << shift;
-  while (lanes) {
-    int of = -1;
-    for (int g = 0; g < 64 && lanes; g += each) {
-      if ((lane & -each) == g) of = __builtin_ctzll(lanes);
-      lanes &= lanes - 1;
+  each(bar, [&](uint64_t key) {
+    if (key) {
+      const int at = atomicAdd(&sh.gathered, 1);
+      if (at < kRoom) sh.keys[at] = key;
     }
-    for (int j0 = 0; j0 < vecs; j0 += each) {
-      const int e0 = lo + ((j0 + (lane & (each - 1))) * kThreads + wave * 64 + of) * V;
-      float v[V];
-      load_vec(z + e0, of < 0 ? 0 : hi - e0, kNegInf, v);
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const uint32_t o = order_of(v[e]);
-        top.offer(v[e] > kMasked && o >= bar ? ((uint64_t)o << 32) | (uint32_t)~(e0 + e) : 0, k);
-      }
+  });
+  __syncthreads();
+  const int n = sh.gathered;
+  if (n <= kRoom) {
+    const uint64_t mine = (int)threadIdx.x < n ? sh.keys[threadIdx.x] : 0;
+    int rank = (int)threadIdx.x < n ? 0 : (int)threadIdx.x;
+    if ((wave << 6) < n) {
+      int larger = 0;
+      for (int i = 0; i < n; ++i) larger += sh.keys[i] > mine;
+      if (mine) rank = larger;
+    }
+    if (rank < k) put(rank, mine);
+  } else {                                      // too many alike: each wave's best, then of the waves'
+    TopKeys top;
+    each(bar, [&](uint64_t key) { top.offer(key, k); });
+    __syncthreads();
+    sh.keys[threadIdx.x] = lane < k ? top.key : 0;
+    __syncthreads();
+    if (wave == 0) {
+      for (int w = 1; w < kWaves; ++w) top.offer(sh.keys[w * 64 + lane], k);
+      if (lane < k) put(lane, top.key);
     }
   }
-  return top;
 }
 
 template <class T, bool TOP>
 __global__ __launch_bounds__(kThreads) void token_logp_fwd_kernel(LogpArgs a) {
   constexpr int V = kVec<T>;
   constexpr int U = 4;                          // vectors of a lane in flight
-  __shared__ float4 sums[kWaves];
-  __shared__ uint64_t keys[kWaves][64];
-  __shared__ float largest[kThreads];
+  __shared__ Shared sh;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const float c = a.scale * kLog2e;
   const int64_t units = (int64_t)a.n_tokens * a.parts;
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int row = (int)(unit / a.parts), part = (int)(unit - (int64_t)row * a.parts);
+    const int row = (int)a.by_parts.quot((uint32_t)unit), part = (int)unit - row * a.parts;
     const T *z = (const T *)a.logits + (int64_t)row * a.row_stride;
     const int lo = part * a.part_len, hi = min(a.vocab, lo + a.part_len);
+    int64_t y = -1;
+    float zy = 0.f;
+    if (threadIdx.x == 0 && a.parts == 1 && a.logp) {
+      y = a.targets[row];
+      if (y >= 0 && y < a.vocab) zy = to_f32(z[y]);
+    }
     Sums x(c);
-    Target y;
-    if (threadIdx.x == 0 && a.parts == 1) y.load(a, row, z);
-    float mine = kNegInf;
-    const auto take = [&](const float (&v)[V]) {
+    Largest mine;
+    const auto take = [&](const float (&v)[V], int e0) {
       float most = max3(v[0], v[1], v[2]);
 #pragma unroll
       for (int e = 3; e < V; e += 2) most = max3(most, v[e], v[e + 1 < V ? e + 1 : e]);
       const bool up = fmaf(most, c, -x.r) > 16.f;
       if (__ballot(up)) x.move(up ? most * c : x.r);
-      if constexpr (TOP) mine = fmaxf(mine, most);
+      if constexpr (TOP) mine.take(most, e0);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const float d = fmaf(v[e], c, -x.r);
@@ -242,82 +261,122 @@ __global__ __launch_bounds__(kThreads) void token_logp_fwd_kernel(LogpArgs a) {
         x.u = fmaf(p, fmaxf(d, -200.f), x.u);   // (a masked one: 0, not 0 times infinity; a NaN stays one in p)
       }
     };
+    const auto place = [&](int b0, int i) { return b0 + (i * kThreads + (int)threadIdx.x) * V; };
     int b0 = lo;
-    for (; b0 + kThreads * V * U <= hi; b0 += kThreads * V * U) {
-      u32x4 raw[U];
+    const auto stream = [&](auto load) {
+      for (; b0 + kThreads * V * U <= hi; b0 += kThreads * V * U) {
+        u32x4 raw[U];
 #pragma unroll
-      for (int i = 0; i < U; ++i) raw[i] = load16(z + b0 + (i * kThreads + (int)threadIdx.x) * V);
+        for (int i = 0; i < U; ++i) raw[i] = load(z + place(b0, i));
 #pragma unroll
-      for (int i = 0; i < U; ++i) {
-        float v[V];
-        unpack<T>(raw[i], v);
-        take(v);
+        for (int i = 0; i < U; ++i) {
+          float v[V];
+          unpack<T>(raw[i], v);
+          take(v, place(b0, i));
+        }
       }
-    }
-    for (; b0 < hi; b0 += kThreads * V) {
-      const int e0 = b0 + (int)threadIdx.x * V;
-      float v[V];
-      load_vec(z + e0, hi - e0, kNegInf, v);
-      take(v);
+    };
+    if (sizeof(T) == 2 && ((uintptr_t)z & 2)) stream([](const T *p) { return load16_odd(p); });
+    else stream([](const T *p) { return load16(p); });
+    if (b0 < hi) {                              // what is left, in flight together too
+      float v[U][V];
+#pragma unroll
+      for (int i = 0; i < U; ++i) load_vec(z + place(b0, i), hi - place(b0, i), kNegInf, v[i]);
+#pragma unroll
+      for (int i = 0; i < U; ++i)
+        if (place(b0, i) - lane * V < hi) take(v[i], place(b0, i));   // (whole waves)
     }
     wave_join(x);
-    if (lane == 0) sums[wave] = make_float4(x.r, x.s, x.u, 0.f);
-    TopKeys top;
-    if constexpr (TOP) {
-      largest[threadIdx.x] = mine;
-      __syncthreads();
-      top = find_top(z, lo, hi, a.top, largest, mine);
-      keys[wave][lane] = lane < a.top ? top.key : 0;
-    }
+    if (lane == 0) sh.sums[wave] = make_float4(x.r, x.s, x.u, 0.f);
     __syncthreads();
-    if (wave == 0) {
-      const float4 f = sums[lane & (kWaves - 1)];
-      x.r = f.x;
-      x.s = lane < kWaves ? f.y : 0.f;
-      x.u = lane < kWaves ? f.z : 0.f;
-      wave_join(x);
-      if constexpr (TOP)
-        for (int w = 1; w < kWaves; ++w) top.offer(keys[w][lane], a.top);
-      if (a.parts == 1) {
-        finish_row(a, row, c, x, top, y);
-      } else {
-        if (lane == 0) a.part_sums[unit] = make_float4(x.r, x.s, x.u, 0.f);
-        if constexpr (TOP)
-          if (lane < a.top) a.part_top[((int64_t)row * a.top + lane) * a.parts + part] = top.key;
-      }
+    const float4 f = sh.sums[lane & (kWaves - 1)];
+    x.r = f.x;
+    x.s = lane < kWaves ? f.y : 0.f;
+    x.u = lane < kWaves ? f.z : 0.f;
+    wave_join(x);
+    if (a.parts == 1) {
+      const Finish end(x, c);
+      if (threadIdx.x == 0) end.row<T>(a, row, x, y, zy);
+    } else if (threadIdx.x == 0) {
+      a.part_sums[unit] = make_float4(x.r, x.s, x.u, 0.f);
+    }
+    if constexpr (TOP) {
+      const auto each = [&](uint32_t bar, auto f) {
+        const auto vec = [&](int e0, int cnt) {
+          float v[V];
+          load_vec(z + e0, cnt, kNegInf, v);
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const uint32_t o = order_of(v[e]);
+            f(v[e] > kMasked && o >= bar ? ((uint64_t)o << 32) | (uint32_t)~(e0 + e) : 0);
+          }
+        };
+        const auto reaches = [&](float m) { return m > kMasked && order_of(m) >= bar; };
+        const bool all = reaches(mine.second);
+        vec(mine.at, reaches(mine.first) && !all ? hi - mine.at : 0);
+        // all vectors of a lane, one a lane
+        for (uint64_t lanes = __ballot(all); lanes; lanes &= lanes - 1) {
+          const int from = lo + (wave * 64 + __builtin_ctzll(lanes)) * V;
+          for (int j0 = 0; from + j0 * kThreads * V < hi; j0 += 64) {
+            const int e0 = from + (j0 + lane) * kThreads * V;
+            vec(e0, hi - e0);
+          }
+        }
+      };
+      const Finish end(x, c);
+      block_top(sh, a.top, mine.first, each, [&](int i, uint64_t key) {
+        if (a.parts == 1) end.top(a, row, i, key);
+        else a.part_top[((int64_t)row * a.parts + part) * a.top + i] = key;
+      });
     }
     __syncthreads();                            // before the next unit's sums and keys
   }
 }
 
-// One wave a row: its parts' sums, a part a lane, and the parts' keys, the best
-// of all parts first.
+// One workgroup a row: its parts' sums, a part a lane, and the parts' keys.
 template <class T>
-__global__ __launch_bounds__(64) void token_logp_join_kernel(LogpArgs a) {
-  const int lane = threadIdx.x, row = blockIdx.x;
+__global__ __launch_bounds__(kThreads) void token_logp_join_kernel(LogpArgs a) {
+  __shared__ Shared sh;
+  const int lane = threadIdx.x & 63, row = blockIdx.x;
   const float c = a.scale * kLog2e;
-  Target y;
-  if (lane == 0) y.load(a, row, (const T *)a.logits + (int64_t)row * a.row_stride);
+  int64_t y = -1;
+  float zy = 0.f;
+  if (threadIdx.x == 0 && a.logp) {
+    y = a.targets[row];
+    if (y >= 0 && y < a.vocab) zy = to_f32(((const T *)a.logits + (int64_t)row * a.row_stride)[y]);
+  }
   const float4 f = a.part_sums[(int64_t)row * a.parts + min(lane, a.parts - 1)];
-  TopKeys top;
+  constexpr int U = kLogpMaxParts * 64 / kThreads;   // most keys of a thread
   const int keys = a.parts * a.top;
-  const uint64_t *from = a.part_top + (int64_t)row * keys;
-  uint64_t key = lane < keys ? from[lane] : 0;
-  for (int i = 0; i < keys; i += 64) {
-    const uint64_t next = i + 64 + lane < keys ? from[i + 64 + lane] : 0;
-    if (i == 0) {
-      const uint32_t x[1] = {(uint32_t)(key >> 32)};
-      if (x[0] < kth_of(x, a.top)) key = 0;     // (as many as are wanted reach it)
+  uint64_t key[U];
+  float first = kNegInf;
+  if (a.top > 0) {
+    const uint64_t *from = a.part_top + (int64_t)row * keys;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int at = i * kThreads + (int)threadIdx.x;
+      key[i] = at < keys ? from[at] : 0;
     }
-    top.offer(key, a.top);
-    key = next;
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < U; ++i) most = max(most, (uint32_t)(key[i] >> 32));
+    if (most) first = value_of(most);
   }
   Sums x(c);
   x.r = f.x;
   x.s = lane < a.parts ? f.y : 0.f;
   x.u = lane < a.parts ? f.z : 0.f;
   wave_join(x);
-  finish_row(a, row, c, x, top, y);
+  const Finish end(x, c);
+  if (threadIdx.x == 0) end.row<T>(a, row, x, y, zy);
+  if (a.top > 0)
+    block_top(
+        sh, a.top, first,
+        [&](uint32_t bar, auto f) {
+#pragma unroll
+          for (int i = 0; i < U; ++i) f((uint32_t)(key[i] >> 32) >= bar ? key[i] : 0);
+        },
+        [&](int i, uint64_t k) { end.top(a, row, i, k); });
 }
 
 // ---------------------------------------------------------------- backward --
@@ -341,37 +400,31 @@ __global__ __launch_bounds__(kThreads) void token_logp_bwd_kernel(LogpBwdArgs a,
     const bool zero = lse == kNegInf || (gl == 0.f && gs == 0.f && ge == 0.f);
     // dz = p (k0 + k1 d), d = (z - lse) log2(e)
     const float k0 = a.scale * (gs - gl - (ge != 0.f ? ge * a.entropy[row] : 0.f));
-    const float k1 = -a.scale * ge * kLn2, at_y = a.scale * gl;
-    const int first = chunk * (kThreads * V * kBwdVecs);
-    float v[kBwdVecs][V];
-    if (zero) {
-#pragma unroll
-      for (int r = 0; r < kBwdVecs; ++r) {
-        const int e0 = first + (r * kThreads + (int)threadIdx.x) * V;
-        const float o[V] = {};
-        store_vec(dz + e0, a.vocab - e0, o);
-      }
-      continue;
-    }
-#pragma unroll
-    for (int r = 0; r < kBwdVecs; ++r) {
-      const int e0 = first + (r * kThreads + (int)threadIdx.x) * V;
-      load_vec(z + e0, a.vocab - e0, kNegInf, v[r]);
-    }
-#pragma unroll
-    for (int r = 0; r < kBwdVecs; ++r) {
-      const int e0 = first + (r * kThreads + (int)threadIdx.x) * V;
-      float o[V];
+    const float k1 = -a.scale * ge * kLn2, at_y = zero ? 0.f : a.scale * gl;
+    const auto gradient = [&](const float (&v)[V], int e0, float (&o)[V]) {
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        const float d = (v[r][e] * a.scale - lse) * kLog2e;
+        const float d = (v[e] * a.scale - lse) * kLog2e;
         const float p = exp2_fast(d);
-        o[e] = p * (k0 + k1 * fmaxf(d, -200.f));
+        o[e] = zero ? 0.f : p * (k0 + k1 * fmaxf(d, -200.f));
       }
       if ((uint32_t)(y - e0) < (uint32_t)V) {
 #pragma unroll
         for (int e = 0; e < V; ++e) o[e] += y - e0 == e ? at_y : 0.f;
       }
+    };
+    const int first = chunk * (kThreads * V * kBwdVecs) + (int)threadIdx.x * V;
+    float v[kBwdVecs][V];
+#pragma unroll
+    for (int r = 0; r < kBwdVecs; ++r) {
+      const int e0 = first + r * kThreads * V;
+      load_vec(z + e0, zero ? 0 : a.vocab - e0, kNegInf, v[r]);   // (a row without a gradient is not read)
+    }
+#pragma unroll
+    for (int r = 0; r < kBwdVecs; ++r) {
+      const int e0 = first + r * kThreads * V;
+      float o[V];
+      gradient(v[r], e0, o);
       store_vec(dz + e0, a.vocab - e0, o);
     }
   }
@@ -382,12 +435,13 @@ hipError_t fwd(LogpArgs a, hipStream_t s) {
   constexpr int V = kVec<T>;
   const int64_t units = (int64_t)a.n_tokens * a.parts;
   a.part_len = (((a.vocab + a.parts - 1) / a.parts) + V - 1) / V * V;
+  a.by_parts = FastDiv(a.parts);
   const int grid = (int)(units < kMaxGrid ? units : kMaxGrid);
   if (a.top > 0) token_logp_fwd_kernel<T, true><<<grid, kThreads, 0, s>>>(a);
   else token_logp_fwd_kernel<T, false><<<grid, kThreads, 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.parts == 1) return e;
-  token_logp_join_kernel<T><<<a.n_tokens, 64, 0, s>>>(a);
+  token_logp_join_kernel<T><<<a.n_tokens, kThreads, 0, s>>>(a);
   return hipGetLastError();
 }
 
@@ -404,7 +458,10 @@ hipError_t bwd(const LogpBwdArgs &a, hipStream_t s) {
 
 int token_logp_parts(int64_t n_tokens, int vocab) {
   if (n_tokens <= 0) return 1;
-  int64_t p = (2048 + n_tokens - 1) / n_tokens;
+    // Two workgroups a compute unit, each with 2048 elements at least.  (32 rows of
+  // 131072 with one alternative: 11.4 us, with four a compute unit 13.8, with eight
+  // 17.9; 1000 rows of 32000 with five, one part a row, 19.4, two 28.6.)
+  int64_t p = (512 + n_tokens - 1) / n_tokens;
   const int64_t most = (vocab + 2047) / 2048;
   if (p > most) p = most;
   if (p > kLogpMaxParts) p = kLogpMaxParts;

@@ -190,7 +190,7 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.nsp_mfma_ceiling.argtypes = [i32, i32, i32, ctypes.c_int64, ctypes.POINTER(ctypes.c_double),
                                      ctypes.POINTER(ctypes.c_double)]
     lib.nsp_mfma_ceiling.restype = i32
-    i64, f64, rows = ctypes.c_int64, ctypes.c_double, ctypes.POINTER(CRows)
+    i64, f64, rows = ctypes.c_int64, ctypes.c_double, p
     for name in ("nsp_rotary_fwd", "nsp_rotary_bwd"):
         getattr(lib, name).argtypes = [i32, i32, i64, i32, i32, p, f32, p, i32, rows, rows, i32, rows, rows, p]
         getattr(lib, name).restype = i32
@@ -481,87 +481,6 @@ NSP_NORM_LAYER, NSP_NORM_RMS = 0, 1
 NSP_TOKEN_LOGP_MAX_TOP = 64
 
 
-def _place(first, *others) -> int:
-    """The GPU that holds every tensor of a call (None: an argument left out)."""
-    dev = first.device
-    if dev.type != "cuda":
-        raise TypeError(f"tensors must be on the GPU (got one on {dev})")
-    for t in others:
-        if t is not None and t.device != dev:
-            raise TypeError(f"tensors on {dev} and {t.device}")
-    return dev.index
-
-
-def _enqueue(call: str, dev: int, stream, *args):
-    """Call `call`(*args, stream) with `dev` current; stream: by default that GPU's current one."""
-    import torch
-    f = getattr(load_library(), call)
-    if dev == torch.cuda.current_device():
-        st = f(*args, _stream(stream))
-    else:
-        with torch.cuda.device(dev):
-            st = f(*args, _stream(stream))
-    if st != NSP_OK:
-        _check(st, call)
-
-
-def _rows(t, shape, dtype, name: str) -> CRows:
-    """A [tokens, n] or [tokens, heads, n] tensor as nsp_rows."""
-    if t.dtype is not dtype or t.shape != shape:
-        raise TypeError(f"{name}: {dtype} {tuple(shape)} is needed (got {t.dtype} {tuple(t.shape)})")
-    st = t.stride()
-    if st[-1] != 1 and shape[-1] > 1:
-        raise ValueError(f"{name}: a row's elements must be contiguous (strides {st})")
-    return CRows(t.data_ptr(), st[0], st[1] if len(st) == 3 else 0)
-
-
-def _array(t, n: int, dtype, name: str) -> Optional[int]:
-    """The address of n contiguous elements; None for an argument left out."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
-        raise TypeError(f"{name}: {n} contiguous elements of {dtype} are needed (got {t.dtype} {tuple(t.shape)}, strides {t.stride()})")
-    return t.data_ptr()
-
-
-def _ws(t):
-    return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
-
-
-def _rotary(call, positions, freqs, q, q_out, k, k_out, names, scale, layout, stream):
-    import torch
-    if q.dim() != 3:
-        raise TypeError(f"{names[0]}: [tokens, heads, head_dim] is needed (got {tuple(q.shape)})")
-    T, hq, D = q.shape
-    dt = q.dtype
-    dev = _place(q, q_out, k, k_out, positions, freqs)
-    a = [_rows(q, q.shape, dt, names[0]), _rows(q_out, q.shape, dt, names[1]), None, None]
-    hk = 0
-    if k is not None or k_out is not None:
-        if k is None or k_out is None or k.dim() != 3:
-            raise TypeError(f"{names[2]} and {names[3]}: [tokens, heads, head_dim] is needed of both")
-        hk = k.shape[1]
-        shape = torch.Size((T, hk, D))
-        a[2:] = _rows(k, shape, dt, names[2]), _rows(k_out, shape, dt, names[3])
-        if hk == 0:
-            a[2:] = None, None
-    half = freqs.numel()
-    _enqueue(call, dev, stream, layout, _dtype_code(q), T, D, 2 * half, _array(freqs, half, torch.float64, "freqs"), scale,
-             _array(positions, T, torch.int64, "positions"), hq, a[0], a[1], hk, a[2], a[3])
-
-
-def nsp_rotary_fwd(positions, freqs, q, q_out, k=None, k_out=None, scale: float = 1.0, layout: int = NSP_ROTARY_HALF, stream=None):
-    """Rotate the query (and key) heads [tokens, heads, head_dim] by their
-    positions (int64 [tokens]); freqs: float64 [rot_dim / 2] on the GPU, as
-    nsp_rotary_frequencies gives them.  q_out may be q itself (in place)."""
-    _rotary("nsp_rotary_fwd", positions, freqs, q, q_out, k, k_out, ("q", "q_out", "k", "k_out"), scale, layout, stream)
-
-
-def nsp_rotary_bwd(positions, freqs, dq_out, dq, dk_out=None, dk=None, scale: float = 1.0, layout: int = NSP_ROTARY_HALF, stream=None):
-    """Gradient of nsp_rotary_fwd: dq_out, dk_out into dq, dk (in place allowed)."""
-    _rotary("nsp_rotary_bwd", positions, freqs, dq_out, dq, dk_out, dk, ("dq_out", "dq", "dk_out", "dk"), scale, layout, stream)
-
-
 def nsp_rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: int = NSP_ROTARY_PLAIN, factor: float = 1.0,
                            context: float = 0.0, low: float = 1.0, high: float = 32.0):
     """(freqs, scale): the angle per position of every pair (float64
@@ -574,86 +493,26 @@ def nsp_rotary_frequencies(rot_dim: int, base: float = 10000.0, scaling: int = N
     return out, float(scale.value)
 
 
-def _norm_shape(x):
-    if x.dim() not in (2, 3):
-        raise TypeError(f"x: [tokens, n] or [tokens, heads, n] is needed (got {tuple(x.shape)})")
-    return x.shape[0], (x.shape[1] if x.dim() == 3 else 1), x.shape[-1]
-
-
-def nsp_norm_fwd(x, weight, bias, y, mean=None, rstd=None, eps: float = 1e-6, kind: int = NSP_NORM_LAYER, stream=None):
-    """Norm of the rows of x ([tokens, n] or [tokens, heads, n]) into y (x
-    itself: in place); weight, bias: [n] of one type, or None; mean, rstd:
-    float32 [rows], for the backward, or None."""
-    import torch
-    T, H, n = _norm_shape(x)
-    wt = weight if weight is not None else bias
-    wd = x.dtype if wt is None else wt.dtype
-    dev = _place(x, y, weight, bias, mean, rstd)
-    _enqueue("nsp_norm_fwd", dev, stream, kind, _dtype_code(x), _dtype_code(x if wt is None else wt), T, H, n, _rows(x, x.shape, x.dtype, "x"),
-             _array(weight, n, wd, "weight"), _array(bias, n, wd, "bias"), eps, _rows(y, x.shape, x.dtype, "y"),
-             _array(mean, T * H, torch.float32, "mean"), _array(rstd, T * H, torch.float32, "rstd"))
-
-
 def nsp_norm_bwd_workspace(n_tokens: int, n_heads: int, n: int) -> int:
     return int(load_library().nsp_norm_bwd_workspace(int(n_tokens), int(n_heads), int(n)))
-
-
-def nsp_norm_bwd(x, weight, dy, mean, rstd, dx, dweight, dbias, workspace, kind: int = NSP_NORM_LAYER, stream=None):
-    """Gradient of nsp_norm_fwd into dx, and dweight and dbias (of the
-    weight's type; None: not computed)."""
-    import torch
-    T, H, n = _norm_shape(x)
-    wt = next((t for t in (weight, dweight, dbias) if t is not None), None)
-    wd = x.dtype if wt is None else wt.dtype
-    dev = _place(x, weight, dy, mean, rstd, dx, dweight, dbias, workspace)
-    _enqueue("nsp_norm_bwd", dev, stream, kind, _dtype_code(x), _dtype_code(x if wt is None else wt), T, H, n, _rows(x, x.shape, x.dtype, "x"),
-             _array(weight, n, wd, "weight"), _rows(dy, x.shape, x.dtype, "dy"), _array(mean, T * H, torch.float32, "mean"),
-             _array(rstd, T * H, torch.float32, "rstd"), _rows(dx, x.shape, x.dtype, "dx"), _array(dweight, n, wd, "dweight"),
-             _array(dbias, n, wd, "dbias"), *_ws(workspace))
 
 
 def nsp_token_logp_workspace(n_tokens: int, vocab: int, top: int = 0) -> int:
     return int(load_library().nsp_token_logp_workspace(int(n_tokens), int(vocab), int(top)))
 
 
-def nsp_token_logp_fwd(logits, targets, logp, lse, entropy=None, top_logp=None, top_index=None, workspace=None, scale: float = 1.0,
-                       stream=None):
-    """Log probabilities of the targets (int64 [tokens]; outside the vocabulary:
-    ignored) under logits [tokens, vocab], with their log-sum-exp, entropy
-    (float32 [tokens]) and the top alternatives ([tokens, top], float32 and
-    int64).  Everything but logits and lse may be None."""
-    import torch
-    if logits.dim() != 2:
-        raise TypeError(f"logits: [tokens, vocab] is needed (got {tuple(logits.shape)})")
-    T, V = logits.shape
-    k = 0
-    if top_logp is not None or top_index is not None:
-        if top_logp is None or top_index is None or top_logp.dim() != 2:
-            raise TypeError("top_logp and top_index: [tokens, top] is needed of both")
-        k = top_logp.shape[1]
-    dev = _place(logits, targets, logp, lse, entropy, top_logp, top_index, workspace)
-    f32 = torch.float32
-    z = _rows(logits, logits.shape, logits.dtype, "logits")
-    _enqueue("nsp_token_logp_fwd", dev, stream, _dtype_code(logits), T, V, z.data, z.token_stride, _array(targets, T, torch.int64, "targets"),
-             scale, _array(logp, T, f32, "logp"), _array(lse, T, f32, "lse"), _array(entropy, T, f32, "entropy"), k,
-             _array(top_logp, T * k, f32, "top_logp"), _array(top_index, T * k, torch.int64, "top_index"), *_ws(workspace))
+_ROW_CALLS = ("nsp_rotary_fwd", "nsp_rotary_bwd", "nsp_norm_fwd", "nsp_norm_bwd", "nsp_token_logp_fwd", "nsp_token_logp_bwd")
 
 
-def nsp_token_logp_bwd(logits, targets, lse, dlogits, g_logp=None, g_entropy=None, entropy=None, g_lse=None, scale: float = 1.0,
-                       stream=None):
-    """Gradient of nsp_token_logp_fwd's logp, entropy and lse (float32
-    [tokens] each, or None) with respect to the logits, into dlogits (the
-    logits themselves: in place)."""
-    import torch
-    if logits.dim() != 2:
-        raise TypeError(f"logits: [tokens, vocab] is needed (got {tuple(logits.shape)})")
-    T, V = logits.shape
-    dev = _place(logits, targets, lse, dlogits, g_logp, g_entropy, entropy, g_lse)
-    f32 = torch.float32
-    z, d = _rows(logits, logits.shape, logits.dtype, "logits"), _rows(dlogits, logits.shape, logits.dtype, "dlogits")
-    _enqueue("nsp_token_logp_bwd", dev, stream, _dtype_code(logits), T, V, z.data, z.token_stride, _array(targets, T, torch.int64, "targets"),
-             scale, _array(lse, T, f32, "lse"), _array(entropy, T, f32, "entropy"), _array(g_logp, T, f32, "g_logp"),
-             _array(g_lse, T, f32, "g_lse"), _array(g_entropy, T, f32, "g_entropy"), d.data, d.token_stride)
+def __getattr__(name):
+    """The row operators' calls, which need torch, on their first use (the
+    planner and the schedule queries do without it)."""
+    if name in _ROW_CALLS:
+        from . import rows
+        for n in _ROW_CALLS:
+            globals()[n] = getattr(rows, n)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 
 ROW_KERNELS = ("rotary", "norm_fwd", "norm_bwd", "token_logp_fwd", "token_logp_bwd")

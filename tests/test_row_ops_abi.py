@@ -1,21 +1,20 @@
 """Refusals of the row operators, their workspace sizes and the rotary
 frequencies: host code, checked without a GPU (nothing is launched on any of
 the error paths, and the addresses are never used)."""
-import ctypes
 import math
 
 import numpy as np
 import pytest
 import torch
 
-from paper_2609_22755_amd import nsp
+from paper_2609_22755_amd import nsp, rows
 
 FAKE = 0x10000
 EINVAL, EUNSUPPORTED, EWORKSPACE = nsp.NSP_EINVAL, nsp.NSP_EUNSUPPORTED, nsp.NSP_EWORKSPACE
 
 
 def _rows(data=FAKE, ts=0, hs=0):
-    return ctypes.byref(nsp.CRows(data, ts, hs))
+    return bytes(nsp.CRows(data, ts, hs))
 
 
 def _call(name, args):
@@ -65,7 +64,7 @@ INF, NAN = float("inf"), float("nan")
 @pytest.mark.parametrize("call", ["nsp_rotary_fwd", "nsp_rotary_bwd"])
 @pytest.mark.parametrize("kw,status,word", [
     (dict(layout=2), EINVAL, "layout"), (dict(dtype=2), EINVAL, "dtype"), (dict(T=-1), EINVAL, "n_tokens"), (dict(T=1 << 31), EINVAL, "n_tokens"),
-    (dict(T=(1 << 31) - 1), EINVAL, "rows"), (dict(D=0, rot=2), EINVAL, "head_dim"), (dict(D=1026, rot=2), EUNSUPPORTED, "head_dim"),
+    (dict(T=(1 << 31) - 1), EINVAL, "rows"), (dict(D=0, rot=2), EINVAL, "head_dim"), (dict(D=257, rot=2), EUNSUPPORTED, "head_dim"),
     (dict(rot=0), EINVAL, "rot_dim"), (dict(rot=63), EINVAL, "rot_dim"), (dict(rot=66), EINVAL, "rot_dim"), (dict(scale=INF), EINVAL, "scale"),
     (dict(scale=NAN), EINVAL, "scale"), (dict(freqs=None), EINVAL, "freqs"), (dict(freqs=FAKE + 4), EINVAL, "freqs"),
     (dict(pos=None), EINVAL, "positions"), (dict(pos=FAKE + 4), EINVAL, "positions"), (dict(hq=0), EINVAL, "q_heads"),
@@ -100,7 +99,8 @@ def test_norm_refusals(kw, status, word):
     (dict(dx=None), EINVAL, "dx"), (dict(dx=_rows(3 * FAKE, 0, 64)), EINVAL, "overlap"), (dict(dx=_rows(2 * FAKE, 128, 65)), EINVAL, "overlap"),
     (dict(dx=_rows(2 * FAKE + 4, 128, 64)), EINVAL, "same view"), (dict(dx=_rows(FAKE + 4, 128, 64)), EINVAL, "same view"),
     (dict(mean=None), EINVAL, "mean"), (dict(rstd=None), EINVAL, "rstd"), (dict(dw=FAKE + 1), EINVAL, "dw"), (dict(db=FAKE + 1), EINVAL, "db"),
-    (dict(ws=None), EWORKSPACE, "workspace"), (dict(ws=FAKE + 128), EINVAL, "workspace"), (dict(ws_bytes=10), EWORKSPACE, "workspace"),
+    (dict(T=64, ws=None), EWORKSPACE, "workspace"), (dict(T=64, ws=FAKE + 128), EINVAL, "workspace"),
+    (dict(T=64, ws_bytes=10), EWORKSPACE, "workspace"),
 ])
 def test_norm_backward_refusals(kw, status, word):
     st, msg = _call("nsp_norm_bwd", _norm_bwd(**kw))
@@ -200,12 +200,22 @@ def test_the_binding_refuses_what_it_cannot_describe():
     with pytest.raises(TypeError, match="on the GPU"):
         nsp.nsp_token_logp_bwd(m, None, None, m)
     with pytest.raises(TypeError, match="float32"):
-        nsp._rows(x.float(), x.shape, torch.bfloat16, "y")
+        rows._rows(x.float(), x.shape, torch.bfloat16, -1, "y")
     with pytest.raises(TypeError, match="y:"):
-        nsp._rows(x[:3], x.shape, torch.bfloat16, "y")
+        rows._rows(x[:3], x.shape, torch.bfloat16, -1, "y")
+    with pytest.raises(TypeError, match="y: a tensor on cpu"):
+        rows._rows(x, x.shape, torch.bfloat16, 0, "y")
     with pytest.raises(ValueError, match="contiguous"):
-        nsp._rows(x.transpose(1, 2), torch.Size((4, 64, 2)), torch.bfloat16, "y")
+        rows._rows(x.transpose(1, 2), torch.Size((4, 64, 2)), torch.bfloat16, -1, "y")
+    with pytest.raises(ValueError, match="contiguous"):
+        rows._logits(x[0].t(), torch.Size((64, 2)), torch.bfloat16, -1, "dlogits")
+    with pytest.raises(TypeError, match="dlogits"):
+        rows._logits(x[0], torch.Size((2, 63)), torch.bfloat16, -1, "dlogits")
     with pytest.raises(TypeError, match="positions"):
-        nsp._array(torch.zeros(4, dtype=torch.int32), 4, torch.int64, "positions")
+        rows._array(torch.zeros(4, dtype=torch.int32), 4, torch.int64, -1, "positions")
     with pytest.raises(TypeError, match="w:"):
-        nsp._array(torch.zeros(8)[::2], 4, torch.float32, "w")
+        rows._array(torch.zeros(8)[::2], 4, torch.float32, -1, "w")
+    with pytest.raises(TypeError, match="w: a tensor on cpu"):
+        rows._array(torch.zeros(4), 4, torch.float32, 0, "w")
+    with pytest.raises(TypeError, match="unsupported dtype"):
+        rows._code(torch.float16, "x")
