@@ -24,6 +24,7 @@ namespace {
 // many (fewer reload the weights more often, more leave the last ones alone: rows
 // of 8192 bf16 6.1 TB/s, with two 5.7, with eight 5.9).
 constexpr int kFwdTurns = 4, kFwdLeast = 2048, kFwdMost = 1 << 21;
+constexpr int kBwdMost = 1024;   // workgroups of a backward that leaves no parts
 
 template <class T>
 __device__ __forceinline__ T *row_at(const RowView &v, const FastDiv &heads, int row) {
@@ -500,20 +501,24 @@ struct NormShape {
   int rows() const { return lpr > 0 && lpr < 256 ? 256 / lpr : 1; }   // of a workgroup
 };
 
-#ifndef FSHAPES
-#define FSHAPES {16, 1}, {16, 2}, {64, 1}, {64, 2}, {64, 3}, {64, 4}, {128, 3}, {128, 4}, {512, 2}, {1024, 2}, {1024, 4}
-#endif
-#ifndef BSHAPES
-#define BSHAPES {16, 1}, {16, 2}, {64, 1}, {64, 2}, {64, 3}, {64, 4}, {128, 4}, {512, 2}, {512, 4}, {1024, 4}
-#endif
-constexpr NormShape kFwdShapes[] = {FSHAPES}, kBwdShapes[] = {BSHAPES};
+// The first of a list that holds the row is taken.  A wave holds a row as long
+// as its lanes do (up to 32 elements each: sums without a barrier; float32 rows
+// of 1111 in 5 vectors a lane 5.6 TB/s backward, in 4 of 128 lanes 5.0), then few
+// wide groups; three vectors a lane where four would leave many empty.
+constexpr NormShape kFwdShapes[] = {{16, 1}, {16, 2}, {64, 1}, {64, 2}, {64, 3}, {64, 4}, {128, 3}, {128, 4}, {512, 2}, {1024, 2}, {1024, 4}};
+constexpr NormShape kBwdShapes[] = {{16, 1}, {16, 2}, {64, 1},  {64, 2},  {64, 3},  {64, 4},  {64, 5},
+                                    {64, 6}, {64, 8}, {128, 4}, {512, 1}, {512, 2}, {512, 4}, {1024, 4}};
+
+// Whether a type's vectors of v elements go in this shape: 32 elements a lane,
+// 16 where 1024 lanes leave 128 registers each.
+constexpr bool fits(int lpr, int ch, int v) { return ch * v <= (lpr < 1024 ? 32 : 16); }
 
 template <int N>
 NormShape norm_shape(const NormShape (&shapes)[N], int n, bool f32) {
   const int v = f32 ? 4 : 8, vecs = (n + v - 1) / v;
   if (n < v) return {0, 0};
   for (const NormShape s : shapes)
-    if (s.lpr * s.ch >= vecs && (s.lpr < 1024 || s.ch * v <= 16)) return s;
+    if (s.lpr * s.ch >= vecs && fits(s.lpr, s.ch, v)) return s;
   return {0, 0};
 }
 
@@ -539,7 +544,7 @@ hipError_t fwd(const NormArgs &a, hipStream_t s) {
   else
     with_shape<kFwdShapes>(sh, [&](auto lpr, auto ch) {
       constexpr int L = decltype(lpr)::value, C = decltype(ch)::value;
-      if constexpr (L < 1024 || C * kVec<T> <= 16) norm_fwd_kernel<T, L, C><<<(int)grid, kBlock<L>, 0, s>>>(a);
+      if constexpr (fits(L, C, kVec<T>)) norm_fwd_kernel<T, L, C><<<(int)grid, kBlock<L>, 0, s>>>(a);
     });
   return hipGetLastError();
 }
@@ -559,13 +564,13 @@ hipError_t bwd(const NormArgs &a, hipStream_t s) {
   const int64_t groups = ((int64_t)a.rows + sh.rows() - 1) / sh.rows();
   NormArgs b = a;
   if (parts == 0) b.part = nullptr;
-  int grid = b.part ? parts : (int)(groups < kNormMaxParts ? groups : kNormMaxParts);
+  int grid = b.part ? parts : (int)(groups < kBwdMost ? groups : kBwdMost);
   if (sh.lpr == 0)
     norm_bwd_wide_kernel<T><<<grid, 1024, 0, s>>>(b);
   else
     with_shape<kBwdShapes>(sh, [&](auto lpr, auto ch) {
       constexpr int L = decltype(lpr)::value, C = decltype(ch)::value;
-      if constexpr (L < 1024 || C * kVec<T> <= 16) norm_bwd_kernel<T, L, C><<<grid, kBlock<L>, 0, s>>>(b);
+      if constexpr (fits(L, C, kVec<T>)) norm_bwd_kernel<T, L, C><<<grid, kBlock<L>, 0, s>>>(b);
     });
   hipError_t e = hipGetLastError();
   if (e == hipSuccess && b.part) {
@@ -577,8 +582,13 @@ hipError_t bwd(const NormArgs &a, hipStream_t s) {
 
 }  // namespace
 
+// As many workgroups as keep some 32 KB a compute unit on the way (a lane has
+// its next row's vectors of x and dy in flight): more of them get in each
+// other's way in memory (2 M rows of 128 bf16: three a compute unit 264 us, two
+// 277, four 306), and each leaves a part.
 int norm_bwd_parts(int64_t rows, int n, bool f32) {
   const NormShape sh = norm_shape(kBwdShapes, n, f32);
+  // few wide rows: 512 x 8192 bf16 18.9 us without parts, 26.9 with; 1024 x 4096 27.0 and 19.0
   if (rows == 0 || sh.lpr == 0 || (rows <= 512 && rows * 8 <= n)) return 0;
   const int64_t groups = (rows + sh.rows() - 1) / sh.rows();
   int per_cu = sh.lpr > 256 || sh.ch > 2 ? 1 : sh.ch == 2 ? 2 : 3;

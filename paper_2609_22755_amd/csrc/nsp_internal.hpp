@@ -208,8 +208,6 @@ hipError_t launch_rotary(bool pairs, bool f32, const RotaryArgs &a, hipStream_t 
 
 // Widest row of a norm.
 constexpr int kNormMaxN = 65536;
-// Most workgroups of a norm's backward, each with a partial sum of dw and db.
-constexpr int kNormMaxParts = 1024;
 struct NormArgs {
   RowView x, y, dy;          // backward: y is dx
   const void *w, *b;

@@ -119,6 +119,14 @@ class WorkList:
     def hkv(self) -> np.ndarray:
         return (self.kv_heads[:, 1] - self.kv_heads[:, 0]).astype(np.int64)
 
+    def positions(self, rank: int = 0) -> np.ndarray:
+        """The position, within its own sequence, of every token of the
+        sequence-sharded layout (int64; item j's shard on `rank` of its SP
+        group, taken modulo sp_j, starts at rank * L_j / sp_j)."""
+        n = (self.lengths // self.sp).astype(np.int64)
+        start = (rank % self.sp.astype(np.int64)) * n
+        return np.concatenate([np.zeros(0, np.int64)] + [s + np.arange(m) for s, m in zip(start.tolist(), n.tolist())])
+
     def q_elems(self) -> int:
         return int(np.sum(self.lengths.astype(np.int64) * self.hq)) * self.head_dim
 
