@@ -1,8 +1,9 @@
-"""Build libnsp.so (HIP kernels for gfx950 + the C ABI) in-tree with hipcc.
+"""Build libnsp.so (HIP kernels for gfx950 + the C ABI) in-tree with hipcc, and
+_rows.so, the Python module of the row operators' calls, beside it.
 
     python -m paper_2609_22755_amd.build [-v]
 
-Objects go to <repo>/_build/, the library to paper_2609_22755_amd/libnsp.so.
+Objects go to <repo>/_build/, the libraries to paper_2609_22755_amd/.
 Every source is compiled on each call (the build check must really build).
 """
 from __future__ import annotations
@@ -12,6 +13,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -19,6 +21,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libnsp.so")
+ROWS = os.path.join(PKG, "_rows.so")
 
 ARCH = "gfx950"
 CXXFLAGS = [
@@ -72,8 +75,16 @@ def build(verbose: bool = False) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}{r.stderr}")
     os.replace(tmp, LIB)
+    # host code only; it finds libnsp.so beside itself
+    cmd = [hipcc(), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__", "-I", INCLUDE,
+           "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "python", "rows_module.cpp"), "-o", ROWS + ".tmp",
+           "-L", PKG, "-l:libnsp.so", "-Wl,-rpath,$ORIGIN"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"building {os.path.basename(ROWS)} failed:\n{r.stdout}{r.stderr}")
+    os.replace(ROWS + ".tmp", ROWS)
     if verbose:
-        print(f"built {LIB}")
+        print(f"built {LIB} and {os.path.basename(ROWS)}")
     return LIB
 
 

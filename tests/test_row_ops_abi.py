@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2609_22755_amd import nsp, rows
+from paper_2609_22755_amd import nsp
 
 FAKE = 0x10000
 EINVAL, EUNSUPPORTED, EWORKSPACE = nsp.NSP_EINVAL, nsp.NSP_EUNSUPPORTED, nsp.NSP_EWORKSPACE
@@ -185,37 +185,82 @@ def test_frequency_refusals(a):
     assert e.value.status == EINVAL
 
 
+BF, F = torch.bfloat16, torch.float32
+
+
+def _t(*shape, dtype=F):
+    return torch.zeros(shape, dtype=dtype)
+
+
+def _refuse(error, match, call, *a, **kw):
+    with pytest.raises(error, match=match):
+        call(*a, **kw)
+
+
 def test_the_binding_refuses_what_it_cannot_describe():
-    """Types, shapes and places are checked before an address is taken."""
-    x = torch.zeros(4, 2, 64, dtype=torch.bfloat16)
-    with pytest.raises(TypeError, match="on the GPU"):
-        nsp.nsp_norm_fwd(x, None, None, x)
-    with pytest.raises(TypeError, match="on the GPU"):
-        nsp.nsp_rotary_fwd(torch.zeros(4, dtype=torch.int64), torch.zeros(32, dtype=torch.float64), x, x)
-    with pytest.raises(TypeError, match="head_dim"):
-        nsp.nsp_rotary_fwd(None, None, x[0], x[0])
-    with pytest.raises(TypeError, match="tokens, vocab"):
-        nsp.nsp_token_logp_fwd(x, None, None, None)
-    m = torch.zeros(4, 64, dtype=torch.bfloat16, device="meta")
-    with pytest.raises(TypeError, match="on the GPU"):
-        nsp.nsp_token_logp_bwd(m, None, None, m)
-    with pytest.raises(TypeError, match="float32"):
-        rows._rows(x.float(), x.shape, torch.bfloat16, -1, "y")
-    with pytest.raises(TypeError, match="y:"):
-        rows._rows(x[:3], x.shape, torch.bfloat16, -1, "y")
-    with pytest.raises(TypeError, match="y: a tensor on cpu"):
-        rows._rows(x, x.shape, torch.bfloat16, 0, "y")
-    with pytest.raises(ValueError, match="contiguous"):
-        rows._rows(x.transpose(1, 2), torch.Size((4, 64, 2)), torch.bfloat16, -1, "y")
-    with pytest.raises(ValueError, match="contiguous"):
-        rows._logits(x[0].t(), torch.Size((64, 2)), torch.bfloat16, -1, "dlogits")
-    with pytest.raises(TypeError, match="dlogits"):
-        rows._logits(x[0], torch.Size((2, 63)), torch.bfloat16, -1, "dlogits")
-    with pytest.raises(TypeError, match="positions"):
-        rows._array(torch.zeros(4, dtype=torch.int32), 4, torch.int64, -1, "positions")
-    with pytest.raises(TypeError, match="w:"):
-        rows._array(torch.zeros(8)[::2], 4, torch.float32, -1, "w")
-    with pytest.raises(TypeError, match="w: a tensor on cpu"):
-        rows._array(torch.zeros(4), 4, torch.float32, 0, "w")
-    with pytest.raises(TypeError, match="unsupported dtype"):
-        rows._code(torch.float16, "x")
+    """Types, shapes, strides and places are checked before an address is
+    taken; tensors on the host pass all of it but the last."""
+    x, w, r = _t(4, 2, 64, dtype=BF), _t(64), _t(8)
+    nf, nb, rf, lf, lb = nsp.nsp_norm_fwd, nsp.nsp_norm_bwd, nsp.nsp_rotary_fwd, nsp.nsp_token_logp_fwd, nsp.nsp_token_logp_bwd
+    _refuse(TypeError, "on the GPU", nf, x, w, None, x, r, r)
+    _refuse(TypeError, "x: a tensor", nf, None, w, None, x)
+    _refuse(TypeError, "x: a tensor", nf, 3, w, None, x)
+    _refuse(TypeError, r"x: \[tokens, n\]", nf, w, w, None, w)
+    _refuse(TypeError, r"x: \[tokens, n\]", nf, _t(2, 2, 2, 2), w, None, x)
+    _refuse(TypeError, "y: torch.bfloat16", nf, x, w, None, x.float())
+    _refuse(TypeError, "y: .*is needed", nf, x, w, None, x[:3])
+    _refuse(TypeError, "y: .*is needed", nf, x, w, None, x.view(8, 64))
+    _refuse(ValueError, "y: .*contiguous", nf, x, w, None, _t(4, 64, 2, dtype=BF).transpose(1, 2))
+    _refuse(TypeError, "weight: 64 contiguous", nf, x, _t(63), None, x)
+    _refuse(TypeError, "weight: 64 contiguous", nf, x, _t(128)[::2], None, x)
+    _refuse(TypeError, "bias: 64 contiguous elements of torch.float32", nf, x, w, w.to(BF), x)
+    _refuse(TypeError, "weight: unsupported dtype", nf, x, w.half(), None, x)
+    _refuse(TypeError, "x: unsupported dtype", nf, x.half(), None, None, x.half())
+    _refuse(TypeError, "mean: 8 contiguous", nf, x, w, None, x, _t(7))
+    _refuse(TypeError, "rstd: 8 contiguous", nf, x, w, None, x, None, _t(8, dtype=torch.float64))
+    _refuse(TypeError, "misses 'y'", nf, x, w, None)
+    _refuse(TypeError, "unexpected argument 'epsilon'", nf, x, w, None, x, epsilon=1.0)
+    _refuse(TypeError, "'x' twice", nf, x, w, None, x, x=x)
+    _refuse(TypeError, "at most", nf, *([x] * 10))
+    _refuse(TypeError, None, nf, x, w, None, x, eps="a")
+    _refuse(TypeError, "on the GPU", nb, x, w, x, r, r, x, w, None, _t(16, dtype=torch.uint8))
+    _refuse(TypeError, "dy: .*is needed", nb, x, w, x[:, :1], r, r, x, w, None, None)
+    _refuse(TypeError, "dbias: 64 contiguous", nb, x, w, x, r, r, x, w, _t(65), None)
+    _refuse(TypeError, "workspace: contiguous", nb, x, w, x, r, r, x, w, None, _t(16)[::2])
+    pos, fr = torch.zeros(4, dtype=torch.int64), _t(32, dtype=torch.float64)
+    _refuse(TypeError, "on the GPU", rf, pos, fr, x, x, x, x)
+    _refuse(TypeError, "q: .*head_dim", rf, pos, fr, x[0], x[0])
+    _refuse(TypeError, "positions: 4 contiguous elements of torch.int64", rf, pos.int(), fr, x, x)
+    _refuse(TypeError, "positions: 4", rf, pos[:3], fr, x, x)
+    _refuse(TypeError, "freqs: .*float64", rf, pos, fr.float(), x, x)
+    _refuse(TypeError, "k and k_out: both", rf, pos, fr, x, x, x)
+    _refuse(TypeError, "k: .*is needed", rf, pos, fr, x, x, x[:3], x[:3])
+    _refuse(TypeError, "k_out: .*is needed", rf, pos, fr, x, x, x, x[:, :1])
+    _refuse(TypeError, "dk: .*is needed", nsp.nsp_rotary_bwd, pos, fr, x, x, x, x.float())
+    z, y, v = _t(4, 90), torch.zeros(4, dtype=torch.int64), _t(4)
+    _refuse(TypeError, "on the GPU", lf, z, y, v, v, v, _t(4, 3), torch.zeros(4, 3, dtype=torch.int64), None, scale=2)
+    _refuse(TypeError, "tokens, vocab", lf, x, y, v, v)
+    _refuse(TypeError, "lse: a tensor", lf, z, y, v, None)
+    _refuse(TypeError, "targets: 4", lf, z, y.int(), v, v)
+    _refuse(ValueError, "logits: .*contiguous", lf, _t(90, 4).t(), y, v, v)
+    _refuse(TypeError, "top_logp and top_index", lf, z, y, v, v, v, _t(4, 3))
+    _refuse(TypeError, "top_index: 12", lf, z, y, v, v, v, _t(4, 3), torch.zeros(4, 2, dtype=torch.int64))
+    _refuse(TypeError, r"top_logp: \[tokens, top\]", lf, z, y, v, v, v, _t(3, 4), torch.zeros(4, 3, dtype=torch.int64))
+    _refuse(TypeError, "dlogits: .*is needed", lb, z, y, v, z[:, :80])
+    _refuse(TypeError, "g_logp: 4", lb, z, y, v, z, g_logp=_t(5))
+    _refuse(TypeError, "on the GPU", lb, z, y, v, z, g_logp=v, g_entropy=v, entropy=v, g_lse=v, stream=0)
+    m = torch.zeros(4, 90, device="meta")
+    _refuse(TypeError, "on the GPU", lb, m, None, torch.zeros(4, device="meta"), m)
+
+
+def test_calls_leave_no_references():
+    """Refused calls neither keep nor lose references to what they were given."""
+    import sys
+    x, w = _t(4, 2, 64, dtype=BF), _t(64)
+    before = [sys.getrefcount(t) for t in (x, w, BF, F)]
+    for _ in range(1000):
+        for a in ((x, w, None, x), (x, w, None, w), (x, x, None, x), (x, None, w, x, w)):
+            with pytest.raises((TypeError, ValueError)):
+                nsp.nsp_norm_fwd(*a)
+    after = [sys.getrefcount(t) for t in (x, w, BF, F)]
+    assert all(abs(a - b) < 100 for a, b in zip(after, before)), (before, after)
