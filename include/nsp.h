@@ -572,8 +572,9 @@ nsp_status nsp_norm_fwd(nsp_norm_kind kind, nsp_dtype dtype, nsp_dtype w_dtype, 
                         int32_t n, const nsp_rows *x, const void *w, const void *b, float eps, const nsp_rows *y,
                         float *mean, float *rstd, hipStream_t stream);
 
-/* Bytes of device workspace nsp_norm_bwd needs (0 for invalid sizes): the
- * partial sums of dw and db; at most 8192 n + 1024 for any number of rows. */
+/* Bytes of device workspace nsp_norm_bwd needs (0 for invalid sizes, and for
+ * few rows, which need none): the partial sums of dw and db; at most
+ * 8192 n + 1024 for any number of rows. */
 size_t nsp_norm_bwd_workspace(int64_t n_tokens, int32_t n_heads, int32_t n);
 
 /*
@@ -585,8 +586,8 @@ size_t nsp_norm_bwd_workspace(int64_t n_tokens, int32_t n_heads, int32_t n);
  *               NSP_NORM_RMS and may be NULL)
  *   dx          may be dy's or x's very view
  *   dw, db      n elements of w_dtype; either may be NULL (not computed)
- *   workspace   nsp_norm_bwd_workspace bytes, 256-byte aligned (NULL if neither
- *               dw nor db is wanted); contents on entry are ignored
+ *   workspace   nsp_norm_bwd_workspace bytes, 256-byte aligned (NULL where that
+ *               is 0 or neither dw nor db is wanted); contents on entry are ignored
  * With no rows dw and db are zeros.
  * Errors: NSP_EINVAL, NSP_EUNSUPPORTED, NSP_EWORKSPACE, NSP_EHIP.
  */

@@ -77,7 +77,7 @@ def build(verbose: bool = False) -> str:
     os.replace(tmp, LIB)
     # host code only; it finds libnsp.so beside itself
     cmd = [hipcc(), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__", "-I", INCLUDE,
-           "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "python", "rows_module.cpp"), "-o", ROWS + ".tmp",
+           "-I", sysconfig.get_paths()["include"], os.path.join(PKG, "binding", "rows_module.cpp"), "-o", ROWS + ".tmp",
            "-L", PKG, "-l:libnsp.so", "-Wl,-rpath,$ORIGIN"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

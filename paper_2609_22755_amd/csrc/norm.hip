@@ -203,6 +203,80 @@ __global__ __launch_bounds__(kBlock<LPR>) void norm_fwd_kernel(NormArgs a) {
   done.store(col);
 }
 
+// Sums of V columns over the strands of a workgroup (strand: the threads that
+// share threadIdx.x / LANES) into out[i], i < LANES V: by shuffles within a
+// wave, the waves in order.
+template <int WAVES, int LANES, int V>
+__device__ __forceinline__ void strand_sums(float (&s)[V], float (*lds)[LANES * V], float *out) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+#pragma unroll
+    for (int m = LANES; m < 64; m <<= 1) s[e] += __shfl_xor(s[e], m);
+    if (lane < LANES) lds[wave][lane * V + e] = s[e];
+  }
+  __syncthreads();
+  if (threadIdx.x < LANES * V) {
+    float t = 0.f;
+#pragma unroll
+    for (int p = 0; p < WAVES; ++p) t += lds[p][threadIdx.x];
+    *out = t;
+  }
+}
+
+__device__ __forceinline__ void store_weight(void *out, bool f32, int c, float t) {
+  if (f32) ((float *)out)[c] = t;
+  else ((bf16 *)out)[c] = (bf16)t;
+}
+
+// dw, db straight from x and dy, by the workgroup `block` of those that do: 4 or
+// 8 lanes' vectors of columns, the rows in strands of so many lanes.  Where rows
+// are few, the parts of a workgroup for each would be as much memory as the rows
+// themselves, and a kernel more; where dx leaves x and dy alone, it is formed
+// beside this.
+template <class T, int THREADS>
+__device__ __forceinline__ void norm_columns(const NormArgs &a, int block) {
+  constexpr int V = kVec<T>, LANES = THREADS > 256 ? 8 : 4, STRANDS = THREADS / LANES;
+  __shared__ float lds[THREADS / 64][LANES * V];
+  const int col = block * (LANES * V) + (threadIdx.x % LANES) * V, cnt = a.n - col;
+  float dw[V] = {}, db[V] = {}, t;
+  if (cnt > 0) {
+#pragma unroll 8
+    for (int64_t row = threadIdx.x / LANES; row < a.rows; row += STRANDS) {
+      float x[V], g[V];
+      load_vec_kept(row_at<const T>(a.x, a.heads, (int)row) + col, cnt, 0.f, x);
+      load_vec_kept(row_at<const T>(a.dy, a.heads, (int)row) + col, cnt, 0.f, g);
+      const float mean = a.rms ? 0.f : a.mean_in[row], rstd = a.rstd_in[row];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        dw[e] += g[e] * ((x[e] - mean) * rstd);
+        db[e] += g[e];
+      }
+    }
+  }
+  const int c = block * (LANES * V) + threadIdx.x;
+  const bool mine = threadIdx.x < LANES * V && c < a.n;
+  if (a.dw) {
+    strand_sums<THREADS / 64, LANES, V>(dw, lds, &t);
+    if (mine) store_weight(a.dw, a.w_f32, c, t);
+  }
+  if (a.db) {
+    strand_sums<THREADS / 64, LANES, V>(db, lds, &t);
+    if (mine) store_weight(a.db, a.w_f32, c, t);
+  }
+}
+template <class T, int THREADS>
+int column_blocks(int n) {
+  const int per = (THREADS > 256 ? 8 : 4) * kVec<T>;
+  return (n + per - 1) / per;
+}
+
+template <class T>
+__global__ __launch_bounds__(1024) void norm_columns_kernel(NormArgs a) {
+  norm_columns<T, 1024>(a, blockIdx.x);
+}
+
 // A row is kept as it was loaded until it is done: unpacking it twice is
 // cheaper than the registers of its float32 form, which the next row's vectors,
 // on their way meanwhile, take.
@@ -210,6 +284,8 @@ template <class T, int LPR, int CH>
 __global__ __launch_bounds__(kBlock<LPR>) void norm_bwd_kernel(NormArgs a) {
   constexpr int V = kVec<T>;
   constexpr int RPB = kGroups<LPR>;
+  if ((int)blockIdx.x < a.column_blocks) return norm_columns<T, kBlock<LPR>>(a, blockIdx.x);
+  const int block = (int)blockIdx.x - a.column_blocks, blocks = (int)gridDim.x - a.column_blocks;
   __shared__ float slots[2 * 2 * RPB * (LPR / 64 + 1)];
   const int lane = threadIdx.x % LPR, group = threadIdx.x / LPR;
   int turn = 0;
@@ -232,8 +308,8 @@ __global__ __launch_bounds__(kBlock<LPR>) void norm_bwd_kernel(NormArgs a) {
     r.mean = a.rms ? 0.f : a.mean_in[row];
     r.rstd = a.rstd_in[row];
   };
-  const int64_t step = (int64_t)gridDim.x * RPB;
-  int64_t row0 = (int64_t)blockIdx.x * RPB;
+  const int64_t step = (int64_t)blocks * RPB;
+  int64_t row0 = (int64_t)block * RPB;
   fetch(row0, next);
   float w[CH][V], dw[CH][V], db[CH][V];
 #pragma unroll
@@ -296,7 +372,7 @@ __global__ __launch_bounds__(kBlock<LPR>) void norm_bwd_kernel(NormArgs a) {
     }
   }
   if (!a.part) return;
-  float *part = a.part + (int64_t)blockIdx.x * 2 * a.n;
+  float *part = a.part + (int64_t)block * 2 * a.n;
   if constexpr (RPB == 1) {
 #pragma unroll
     for (int c = 0; c < CH; ++c)
@@ -411,33 +487,6 @@ __global__ __launch_bounds__(1024) void norm_bwd_wide_kernel(NormArgs a) {
   }
 }
 
-// Sums of V columns over the strands of a workgroup (strand: the threads that
-// share threadIdx.x / LANES) into out[i], i < LANES V: by shuffles within a
-// wave, the waves in order.
-template <int LANES, int V>
-__device__ __forceinline__ void strand_sums(float (&s)[V], float (*lds)[LANES * V], float *out) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  __syncthreads();
-#pragma unroll
-  for (int e = 0; e < V; ++e) {
-#pragma unroll
-    for (int m = LANES; m < 64; m <<= 1) s[e] += __shfl_xor(s[e], m);
-    if (lane < LANES) lds[wave][lane * V + e] = s[e];
-  }
-  __syncthreads();
-  if (threadIdx.x < LANES * V) {
-    float t = 0.f;
-#pragma unroll
-    for (int p = 0; p < 16; ++p) t += lds[p][threadIdx.x];
-    *out = t;
-  }
-}
-
-__device__ __forceinline__ void store_weight(void *out, bool f32, int c, float t) {
-  if (f32) ((float *)out)[c] = t;
-  else ((bf16 *)out)[c] = (bf16)t;
-}
-
 // dw, db: the sum of the workgroups' parts, 32 columns a workgroup, the parts
 // in 128 strands.
 __global__ __launch_bounds__(1024) void norm_weight_kernel(const float *part, int parts, int n, void *dw, void *db, bool f32) {
@@ -455,44 +504,9 @@ __global__ __launch_bounds__(1024) void norm_weight_kernel(const float *part, in
       for (int e = 0; e < 4; ++e) s[e] += v[e];
     }
   }
-  strand_sums<8, 4>(s, lds, &t);
+  strand_sums<16, 8, 4>(s, lds, &t);
   const int c = blockIdx.x * 32 + threadIdx.x;
   if (threadIdx.x < 32 && c < n) store_weight(out, f32, c, t);
-}
-
-// dw, db straight from x and dy: V 8 columns a workgroup, the rows in 128
-// strands.  Where rows are few and wide, their parts would be as much memory
-// as the rows themselves, which lie in the caches for the pass that follows.
-template <class T>
-__global__ __launch_bounds__(1024) void norm_columns_kernel(NormArgs a) {
-  constexpr int V = kVec<T>;
-  __shared__ float lds[16][8 * V];
-  const int col = blockIdx.x * (8 * V) + (threadIdx.x & 7) * V, cnt = a.n - col;
-  float dw[V] = {}, db[V] = {}, t;
-  if (cnt > 0) {
-#pragma unroll 4
-    for (int64_t row = threadIdx.x >> 3; row < a.rows; row += 128) {
-      float x[V], g[V];
-      load_vec(row_at<const T>(a.x, a.heads, (int)row) + col, cnt, 0.f, x);
-      load_vec(row_at<const T>(a.dy, a.heads, (int)row) + col, cnt, 0.f, g);
-      const float mean = a.rms ? 0.f : a.mean_in[row], rstd = a.rstd_in[row];
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        dw[e] += g[e] * ((x[e] - mean) * rstd);
-        db[e] += g[e];
-      }
-    }
-  }
-  const int c = blockIdx.x * (8 * V) + threadIdx.x;
-  const bool mine = threadIdx.x < 8 * V && c < a.n;
-  if (a.dw) {
-    strand_sums<8, V>(dw, lds, &t);
-    if (mine) store_weight(a.dw, a.w_f32, c, t);
-  }
-  if (a.db) {
-    strand_sums<8, V>(db, lds, &t);
-    if (mine) store_weight(a.db, a.w_f32, c, t);
-  }
 }
 
 // Lanes of a row, and its vectors a lane; 0 lanes: the wide kernels.
@@ -552,27 +566,35 @@ hipError_t fwd(const NormArgs &a, hipStream_t s) {
 template <class T>
 hipError_t bwd(const NormArgs &a, hipStream_t s) {
   constexpr bool f32 = sizeof(T) == 4;
-  const bool weights = a.dw || a.db;
-  const int parts = norm_bwd_parts(a.rows, a.n, f32);
-  if (weights && parts == 0) {
-    norm_columns_kernel<T><<<(a.n + 8 * kVec<T> - 1) / (8 * kVec<T>), 1024, 0, s>>>(a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  if (a.rows == 0) return hipSuccess;
   const NormShape sh = norm_shape(kBwdShapes, a.n, f32);
-  const int64_t groups = ((int64_t)a.rows + sh.rows() - 1) / sh.rows();
+  const int parts = norm_bwd_parts(a.rows, a.n, f32);
+  const bool columns = (a.dw || a.db) && parts == 0;
+  hipError_t e = hipSuccess;
+  if (columns && (a.rows == 0 || sh.lpr == 0)) {
+    norm_columns_kernel<T><<<column_blocks<T, 1024>(a.n), 1024, 0, s>>>(a);
+    e = hipGetLastError();
+  }
+  if (e != hipSuccess || a.rows == 0) return e;
   NormArgs b = a;
   if (parts == 0) b.part = nullptr;
-  int grid = b.part ? parts : (int)(groups < kBwdMost ? groups : kBwdMost);
+  const int64_t groups = ((int64_t)a.rows + sh.rows() - 1) / sh.rows();
+  const int grid = b.part ? parts : (int)(groups < kBwdMost ? groups : kBwdMost);
   if (sh.lpr == 0)
     norm_bwd_wide_kernel<T><<<grid, 1024, 0, s>>>(b);
   else
     with_shape<kBwdShapes>(sh, [&](auto lpr, auto ch) {
       constexpr int L = decltype(lpr)::value, C = decltype(ch)::value;
-      if constexpr (fits(L, C, kVec<T>)) norm_bwd_kernel<T, L, C><<<grid, kBlock<L>, 0, s>>>(b);
+      if constexpr (fits(L, C, kVec<T>)) {
+        b.column_blocks = columns ? column_blocks<T, kBlock<L>>(a.n) : 0;
+        // dw and db read what dx in place would overwrite: by a launch of their own, before
+        if (columns && (a.y.data == a.x.data || a.y.data == a.dy.data)) {
+          norm_bwd_kernel<T, L, C><<<b.column_blocks, kBlock<L>, 0, s>>>(b);
+          b.column_blocks = 0;
+        }
+        norm_bwd_kernel<T, L, C><<<grid + b.column_blocks, kBlock<L>, 0, s>>>(b);
+      }
     });
-  hipError_t e = hipGetLastError();
+  e = hipGetLastError();
   if (e == hipSuccess && b.part) {
     norm_weight_kernel<<<dim3((a.n + 31) / 32, 2), 1024, 0, s>>>(a.part, parts, a.n, a.dw, a.db, a.w_f32);
     e = hipGetLastError();
@@ -588,8 +610,10 @@ hipError_t bwd(const NormArgs &a, hipStream_t s) {
 // 277, four 306), and each leaves a part.
 int norm_bwd_parts(int64_t rows, int n, bool f32) {
   const NormShape sh = norm_shape(kBwdShapes, n, f32);
-  // few wide rows: 512 x 8192 bf16 18.9 us without parts, 26.9 with; 1024 x 4096 27.0 and 19.0
-  if (rows == 0 || sh.lpr == 0 || (rows <= 512 && rows * 8 <= n)) return 0;
+  // Few rows: without parts 24 x 4096 bf16 5.4 us, with them 11.3; 200 x 1000 6.8
+  // and 9.1; 500 x 128 float32 8.3 and 7.1.  Wide ones longer: 600 x 8192 19.0 and
+  // 24.9; 500 x 4096 24.8 and 18.3.
+  if (rows <= 200 || sh.lpr == 0 || (rows <= 640 && rows * 12 <= n)) return 0;
   const int64_t groups = (rows + sh.rows() - 1) / sh.rows();
   int per_cu = sh.lpr > 256 || sh.ch > 2 ? 1 : sh.ch == 2 ? 2 : 3;
   while (per_cu > 1 && groups < 4 * 256 * per_cu) --per_cu;

@@ -219,6 +219,7 @@ struct NormArgs {
   const float *mean_in, *rstd_in;
   void *dw, *db;
   float *part;               // [parts][2][n]: dw, db
+  int32_t column_blocks;     // the first workgroups form dw and db from the rows
 };
 // Workgroups of the backward that leave a partial sum; 0: dw and db are formed
 // without any.

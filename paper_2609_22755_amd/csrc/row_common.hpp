@@ -95,6 +95,13 @@ __device__ __forceinline__ void load_vec(const T *p, int cnt, float fill, float 
   else load_some(p, cnt, fill, x);
 }
 
+// The same of what other workgroups read too.
+template <class T>
+__device__ __forceinline__ void load_vec_kept(const T *p, int cnt, float fill, float (&x)[kVec<T>]) {
+  if (cnt >= kVec<T>) unpack<T>(*(const u32x4_any *)p, x);
+  else load_some(p, cnt, fill, x);
+}
+
 template <class T>
 __device__ __forceinline__ void store_vec(T *p, int cnt, const float (&x)[kVec<T>]) {
   if (cnt >= kVec<T>) store16(p, pack<T>(x));

@@ -1,7 +1,7 @@
 """The row operators' calls (rotary positions, norms of rows, token log
 probabilities) on torch tensors: the part of the binding that
 ``paper_2609_22755_amd.nsp`` offers under the same names, compiled
-(csrc/python/rows_module.cpp) because a small call's time is its binding's.
+(binding/rows_module.cpp) because a small call's time is its binding's.
 
 Sizes, strides and types come from the tensors: a wrong one raises TypeError or
 ValueError; what the C ABI refuses raises NspError.  A call goes to the GPU that

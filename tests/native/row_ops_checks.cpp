@@ -41,7 +41,7 @@ hipError_t launch_norm_fwd(bool, const NormArgs &a, hipStream_t) { ++g_launches;
 hipError_t launch_norm_bwd(bool, const NormArgs &a, hipStream_t) { ++g_launches; g_norm = a; return hipSuccess; }
 hipError_t launch_token_logp_fwd(bool, const LogpArgs &a, hipStream_t) { ++g_launches; g_logp = a; return hipSuccess; }
 hipError_t launch_token_logp_bwd(bool, const LogpBwdArgs &a, hipStream_t) { ++g_launches; g_logp_bwd = a; return hipSuccess; }
-int norm_bwd_parts(int64_t rows, int n, bool) { return rows * 8 <= n ? 0 : (int)(rows < 768 ? rows : 768); }
+int norm_bwd_parts(int64_t rows, int n, bool) { return rows <= 200 || rows * 8 <= n ? 0 : (int)(rows < 768 ? rows : 768); }
 int token_logp_parts(int64_t n, int vocab) { return n > 0 && n < 64 && vocab > 4096 ? 8 : 1; }
 }  // namespace nsp
 
