@@ -99,8 +99,8 @@ def test_norm_refusals(kw, status, word):
     (dict(dx=None), EINVAL, "dx"), (dict(dx=_rows(3 * FAKE, 0, 64)), EINVAL, "overlap"), (dict(dx=_rows(2 * FAKE, 128, 65)), EINVAL, "overlap"),
     (dict(dx=_rows(2 * FAKE + 4, 128, 64)), EINVAL, "same view"), (dict(dx=_rows(FAKE + 4, 128, 64)), EINVAL, "same view"),
     (dict(mean=None), EINVAL, "mean"), (dict(rstd=None), EINVAL, "rstd"), (dict(dw=FAKE + 1), EINVAL, "dw"), (dict(db=FAKE + 1), EINVAL, "db"),
-    (dict(T=640, ws=None), EWORKSPACE, "workspace"), (dict(T=640, ws=FAKE + 128), EINVAL, "workspace"),
-    (dict(T=640, ws_bytes=10), EWORKSPACE, "workspace"),
+    (dict(T=200, ws=None), EWORKSPACE, "workspace"), (dict(T=200, ws=FAKE + 128), EINVAL, "workspace"),
+    (dict(T=200, ws_bytes=10), EWORKSPACE, "workspace"),
 ])
 def test_norm_backward_refusals(kw, status, word):
     st, msg = _call("nsp_norm_bwd", _norm_bwd(**kw))
