@@ -640,7 +640,8 @@ nsp_status nsp_token_logp_fwd(nsp_dtype dtype, int64_t n_tokens, int32_t vocab, 
  * logp, lse and entropy (float32 [n_tokens]; NULL: zeros):
  *     dlogits_v = scale (g_logp (1[v = target] - p_v) + g_lse p_v
  *                        - g_entropy p_v (z_v - lse + entropy))
- * in float32, rounded once.  An ignored target takes g_logp as 0.  A row of
+ * in float32, rounded once, with p = exp(z - lse) of the lse given (at most 1;
+ * where |lse| is 2^24 and more, its own rounding shows).  An ignored target takes g_logp as 0.  A row of
  * masked logits alone (lse = -inf) has gradient 0, and so has a row whose three gradients are
  * 0, whatever its logits.  The alternatives' values have no gradient.
  *   targets     may be NULL with g_logp NULL

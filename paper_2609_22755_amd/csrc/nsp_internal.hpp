@@ -241,8 +241,8 @@ struct LogpArgs {
   int64_t *top_index;
   int32_t parts, part_len;   // parts a row, elements a part
   FastDiv by_parts;
-  float4 *part_sums;         // [row][part]: reference, sum, weighted sum
-  uint64_t *part_top;        // [row][part][top]
+  float4 *part_sums;         // [row][part]: reference, sum, weighted sum, the reference's logit
+  uint64_t *part_top;        // [row][part][top], largest first
 };
 // Parts a row is split in.
 int token_logp_parts(int64_t n_tokens, int vocab);

@@ -56,24 +56,34 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
 
 // ------------------------------------------------------------ running sums --
 
+// From |r| = 2^28 on, r is a rounded number of whole exponents: logits next to
+// each other lie further apart than a softmax sees, but their products with
+// log2(e) round past each other.  There d is taken from the differences of the
+// logits themselves (an operation more an element).
+__device__ __forceinline__ bool is_far(float r) { return fabsf(r) >= 0x1p28f; }
+
 struct Sums {
-  float r, s = 0.f, u = 0.f;
+  float r, m = kNoRef, s = 0.f, u = 0.f;        // m: the logit that r = m scale log2(e) comes from
 
   // c: scale log2(e), 2^-64 .. 2^65.
   __device__ __forceinline__ explicit Sums(float c) : r(fmaxf(kNoRef * c, -0x1.fffffep126f)) {}
-  // The same sums with a reference to >= r.
-  __device__ __forceinline__ void move(float to) {
-    const float d = fmaxf(r - to, -1e4f);        // (an exponential of 0 long before; keeps d s finite)
+  __device__ __forceinline__ Sums(const float4 &f) : r(f.x), m(f.w), s(f.y), u(f.z) {}
+  __device__ __forceinline__ float4 packed() const { return make_float4(r, s, u, m); }
+  // The same sums with the reference of a logit to >= m (to_r: its r).
+  __device__ __forceinline__ void move(float to, float to_r, float c) {
+    const float d = fmaxf(is_far(to_r) ? (m - to) * c : r - to_r, -1e4f);   // (an exponential of 0 long before; keeps d s finite)
     const float f = exp2_fast(d);
     u = f * (u + d * s);
     s *= f;
-    r = to;
+    m = to;
+    r = to_r;
   }
 };
 
 // Over the lanes of a wave, in every lane.
-__device__ __forceinline__ void wave_join(Sums &x) {
-  x.move(wave_max(x.r));
+__device__ __forceinline__ void wave_join(Sums &x, float c) {
+  const float to = wave_max(x.m), to_r = wave_max(x.r);   // (r grows with m)
+  x.move(to, to_r, c);
   x.s = group_sum<64>(x.s);
   x.u = group_sum<64>(x.u);
 }
@@ -162,10 +172,13 @@ struct Largest {
 // What a row comes to, from its sums (in every thread) and its alternatives
 // (thread i: the i-th, 0 if there is none).
 struct Finish {
-  float r, log_s, c;
+  float r, m, log_s, c;
   bool none;                 // nothing but masked logits
-  __device__ __forceinline__ Finish(const Sums &x, float scale_log2) : r(x.r), log_s(log2f(x.s)), c(scale_log2), none(x.s == 0.f) {}
-  __device__ __forceinline__ float logp(float z) const { return none ? kNegInf : (fmaf(z, c, -r) - log_s) * kLn2; }
+  __device__ __forceinline__ Finish(const Sums &x, float scale_log2)
+      : r(x.r), m(x.m), log_s(log2f(x.s)), c(scale_log2), none(x.s == 0.f) {}
+  __device__ __forceinline__ float logp(float z) const {
+    return none ? kNegInf : ((is_far(r) ? (z - m) * c : fmaf(z, c, -r)) - log_s) * kLn2;
+  }
   template <class T>
   __device__ __forceinline__ void row(const LogpArgs &a, int row, const Sums &x, int64_t y, float z) const {
     a.lse[row] = none ? kNegInf : (r + log_s) * kLn2;
@@ -245,20 +258,29 @@ __global__ __launch_bounds__(kThreads) void token_logp_fwd_kernel(LogpArgs a) {
       if (y >= 0 && y < a.vocab) zy = to_f32(z[y]);
     }
     Sums x(c);
+    bool far = true;                            // of a lane of the wave (as long as one has no logit yet, too)
     Largest mine;
     const auto take = [&](const float (&v)[V], int e0) {
       float most = max3(v[0], v[1], v[2]);
 #pragma unroll
       for (int e = 3; e < V; e += 2) most = max3(most, v[e], v[e + 1 < V ? e + 1 : e]);
-      const bool up = fmaf(most, c, -x.r) > 16.f;
-      if (__ballot(up)) x.move(up ? most * c : x.r);
+      const bool up = (far ? (most - x.m) * c : fmaf(most, c, -x.r)) > 16.f;
+      if (__ballot(up)) {
+        x.move(up ? most : x.m, up ? most * c : x.r, c);
+        far = __any(is_far(x.r));
+      }
       if constexpr (TOP) mine.take(most, e0);
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float d = fmaf(v[e], c, -x.r);
+      const auto add = [&](float d) {
         const float p = exp2_fast(d);
         x.s += p;
         x.u = fmaf(p, fmaxf(d, -200.f), x.u);   // (a masked one: 0, not 0 times infinity; a NaN stays one in p)
+      };
+      if (far) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) add((v[e] - x.m) * c);
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) add(fmaf(v[e], c, -x.r));
       }
     };
     const auto place = [&](int b0, int i) { return b0 + (i * kThreads + (int)threadIdx.x) * V; };
@@ -286,19 +308,17 @@ __global__ __launch_bounds__(kThreads) void token_logp_fwd_kernel(LogpArgs a) {
       for (int i = 0; i < U; ++i)
         if (place(b0, i) - lane * V < hi) take(v[i], place(b0, i));   // (whole waves)
     }
-    wave_join(x);
-    if (lane == 0) sh.sums[wave] = make_float4(x.r, x.s, x.u, 0.f);
+    wave_join(x, c);
+    if (lane == 0) sh.sums[wave] = x.packed();
     __syncthreads();
-    const float4 f = sh.sums[lane & (kWaves - 1)];
-    x.r = f.x;
-    x.s = lane < kWaves ? f.y : 0.f;
-    x.u = lane < kWaves ? f.z : 0.f;
-    wave_join(x);
+    x = Sums(sh.sums[lane & (kWaves - 1)]);
+    if (lane >= kWaves) x.s = x.u = 0.f;
+    wave_join(x, c);
     if (a.parts == 1) {
       const Finish end(x, c);
       if (threadIdx.x == 0) end.row<T>(a, row, x, y, zy);
     } else if (threadIdx.x == 0) {
-      a.part_sums[unit] = make_float4(x.r, x.s, x.u, 0.f);
+      a.part_sums[unit] = x.packed();
     }
     if constexpr (TOP) {
       const auto each = [&](uint32_t bar, auto f) {
@@ -362,11 +382,9 @@ __global__ __launch_bounds__(kThreads) void token_logp_join_kernel(LogpArgs a) {
     for (int i = 0; i < U; ++i) most = max(most, (uint32_t)(key[i] >> 32));
     if (most) first = value_of(most);
   }
-  Sums x(c);
-  x.r = f.x;
-  x.s = lane < a.parts ? f.y : 0.f;
-  x.u = lane < a.parts ? f.z : 0.f;
-  wave_join(x);
+  Sums x(f);
+  if (lane >= a.parts) x.s = x.u = 0.f;
+  wave_join(x, c);
   const Finish end(x, c);
   if (threadIdx.x == 0) end.row<T>(a, row, x, y, zy);
   if (a.top > 0)
@@ -399,13 +417,14 @@ __global__ __launch_bounds__(kThreads) void token_logp_bwd_kernel(LogpBwdArgs a,
     const float lse = a.lse[row];
     const bool zero = lse == kNegInf || (gl == 0.f && gs == 0.f && ge == 0.f);
     // dz = p (k0 + k1 d), d = (z - lse) log2(e)
-    const float k0 = a.scale * (gs - gl - (ge != 0.f ? ge * a.entropy[row] : 0.f));
+    const float nan = lse != lse ? lse : 0.f;          // (p is none, whatever lse is)
+    const float k0 = a.scale * (gs - gl - (ge != 0.f ? ge * a.entropy[row] : 0.f)) + nan;
     const float k1 = -a.scale * ge * kLn2, at_y = zero ? 0.f : a.scale * gl;
     const auto gradient = [&](const float (&v)[V], int e0, float (&o)[V]) {
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         const float d = (v[e] * a.scale - lse) * kLog2e;
-        const float p = exp2_fast(d);
+        const float p = exp2_fast(fminf(d, 0.f));   // (of 2^24 and more, lse is rounded by whole numbers)
         o[e] = zero ? 0.f : p * (k0 + k1 * fmaxf(d, -200.f));
       }
       if ((uint32_t)(y - e0) < (uint32_t)V) {
