@@ -14,6 +14,10 @@
 // wherever the heads lie side by side; the other half of a pair comes from the
 // lane that holds it.  (A lane that loaded both its halves itself, in runs of
 // half a head, left half-used lines behind: heads of 96, 3.0 TB/s.)
+//
+// 65536 tokens x 36 heads of 128 bf16: 200 us, 6.0 TB/s (a copy: 5.7); half of
+// each head rotated 198, float32 5.6 TB/s, heads of 80 with 20 rotated (no whole
+// vectors) 84 us, 3.8; 24 tokens 4 us.
 #include "nsp_internal.hpp"
 #include "row_common.hpp"
 
@@ -40,7 +44,7 @@ __device__ __forceinline__ void wave_sync() {
 template <class T, bool PAIRS, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryArgs a, RotaryShape sh) {
   constexpr int V = kVec<T>;
-  constexpr int U = 3;       // heads of a lane in flight
+  constexpr int U = 3;       // heads of a lane in flight (36 of 128 in 9 turns; 1000 tokens 5.9 us, with two 6.8, six 6.4)
   __shared__ float2 angles[kWaves][kRotaryMaxDim / 2];
   __shared__ u32x4 stage[WHOLE ? 1 : kWaves][WHOLE ? 1 : 64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -146,6 +150,7 @@ hipError_t launch(const RotaryArgs &a, hipStream_t s) {
   sh.vecs = (a.head_dim + V - 1) / V;
   sh.at_once = 64 / sh.vecs;
   // a token's heads in runs, as long as there are not 16 waves a compute unit
+  // (1000 tokens 5.9 us; with 8 waves 6.8, 32 6.9)
   const int heads = a.heads[0] + a.heads[1], rounds = (heads + sh.at_once - 1) / sh.at_once;
   int chunks = (int)(4096 / a.n_tokens);
   chunks = chunks < 1 ? 1 : chunks > rounds ? rounds : chunks;

@@ -26,6 +26,12 @@
 //
 // A workgroup takes a row, or a part of one where there are few rows; the
 // parts' sums and keys are then joined by one workgroup a row.
+//
+// 4096 x 151643 bf16 200 us, 6.2 TB/s (a read: 7.1; some ten vector operations
+// an element, an exponential counting four, keep the vector units busy most of
+// that time); 777 x 50021 float32 with 20 alternatives 36 us, 4.3 TB/s; 8 x 131072
+// with eight 11 us, two launches.  The gradient of 8192 x 131072 bf16 698 us, 6.1
+// TB/s read and written.
 #include "nsp_internal.hpp"
 #include "row_common.hpp"
 
