@@ -483,8 +483,8 @@ nsp_status nsp_sp_tree_worklist(const nsp_plan_params *prm, const int64_t *lengt
  *     captured into a HIP graph at once.  A workspace is used from a call's
  *     first kernel to its last: two calls that may run at the same time (also
  *     two graphs) need two.
- *   - Results are deterministic: no atomics, sums in a fixed order that
- *     depends on the shapes and types only.
+ *   - Results are deterministic: sums are taken in a fixed order that depends
+ *     on the shapes and types only.
  *   - n_tokens, and n_tokens * n_heads, up to 2^31 - 1; 0 tokens are a valid
  *     call.
  */
