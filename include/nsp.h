@@ -478,7 +478,8 @@ nsp_status nsp_sp_tree_worklist(const nsp_plan_params *prm, const int64_t *lengt
  *     the rows is faster, not required.
  *   - An output may be the very view of the input of the same shape (same
  *     address and strides: in place, where the call says so); any other
- *     overlap of an output's extent with that input's is NSP_EINVAL.
+ *     overlap of an output's extent with that input's is NSP_EINVAL.  An
+ *     output may not lie over any other argument of its call.
  *   - Nothing is allocated and no work list is kept: every call can be
  *     captured into a HIP graph at once.  A workspace is used from a call's
  *     first kernel to its last: two calls that may run at the same time (also

@@ -318,7 +318,10 @@ __global__ __launch_bounds__(kBlock<LPR>) void norm_bwd_kernel(NormArgs a) {
   };
   const int64_t step = (int64_t)blocks * RPB;
   int64_t row0 = (int64_t)block * RPB;
-  fetch(row0, next);
+  // (1024 lanes have 128 registers each: no room for a row ahead, which spilled and
+  // ran at 3.0 TB/s for float32 rows of 16384)
+  constexpr bool AHEAD = LPR < 1024;
+  if constexpr (AHEAD) fetch(row0, next);
   float w[CH][V], dw[CH][V], db[CH][V];
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
@@ -328,8 +331,12 @@ __global__ __launch_bounds__(kBlock<LPR>) void norm_bwd_kernel(NormArgs a) {
   }
   const float inv_n = 1.f / (float)a.n;
   for (; row0 < a.rows; row0 += step) {
-    cur = next;
-    if (row0 + step < a.rows) fetch(row0 + step, next);
+    if constexpr (AHEAD) {
+      cur = next;
+      if (row0 + step < a.rows) fetch(row0 + step, next);
+    } else {
+      fetch(row0, cur);
+    }
     const bool live = row0 + group < a.rows;
     if (RPB > 1 && !live) {
       cur.mean = cur.rstd = 0.f;
