@@ -573,8 +573,8 @@ struct NormShape {
 // forward 5.3 TB/s in 3 of 512 lanes, 4.1 in 2 of 1024).
 constexpr NormShape kFwdShapes[] = {{16, 1},  {16, 2},  {64, 1},  {64, 2},  {64, 3},   {64, 4},  {128, 3},
                                     {128, 4}, {256, 3}, {512, 2}, {512, 3}, {1024, 2}, {1024, 4}};
-constexpr NormShape kBwdShapes[] = {{16, 1}, {16, 2}, {64, 1},  {64, 2},  {64, 3},  {64, 4},  {64, 5}, {64, 6},
-                                    {64, 8}, {128, 4}, {512, 1}, {512, 2}, {512, 3}, {512, 4}, {1024, 4}};
+constexpr NormShape kBwdShapes[] = {{16, 1}, {16, 2}, {64, 1},  {64, 2},  {64, 3},  {64, 4},  {64, 5},  {64, 6},
+                                    {64, 8}, {128, 3}, {128, 4}, {512, 1}, {512, 2}, {512, 3}, {512, 4}, {1024, 4}};
 
 // Whether a type's vectors of v elements go in this shape: 32 elements a lane,
 // 16 where 1024 lanes leave 128 registers each.
@@ -661,7 +661,8 @@ hipError_t bwd(const NormArgs &a, hipStream_t s) {
 // As many workgroups as keep some 32 KB a compute unit on the way (a lane has
 // its next row's vectors of x and dy in flight): more of them get in each
 // other's way in memory (2 M rows of 128 bf16: three a compute unit 264 us, two
-// 277, four 306), and each leaves a part.
+// 277, four 306), and each leaves a part; fewer leave it idle (120 K rows of 1111
+// bf16, three vectors a lane: two 182 us, one 207).
 int norm_bwd_parts(int64_t rows, int n, bool f32) {
   const NormShape sh = norm_shape(kBwdShapes, n, f32);
   // Few rows: without parts 24 x 4096 bf16 5.4 us, with them 11.3; 200 x 1000 6.8
@@ -669,7 +670,7 @@ int norm_bwd_parts(int64_t rows, int n, bool f32) {
   // 24.9; 500 x 4096 24.8 and 18.3.
   if (rows <= 200 || sh.lpr == 0 || (rows <= 640 && rows * 12 <= n)) return 0;
   const int64_t groups = (rows + sh.rows() - 1) / sh.rows();
-  int per_cu = sh.lpr > 256 || sh.ch > 2 ? 1 : sh.ch == 2 ? 2 : 3;
+  int per_cu = sh.lpr > 256 || sh.ch > 3 ? 1 : sh.ch > 1 ? 2 : 3;
   while (per_cu > 1 && groups < 4 * 256 * per_cu) --per_cu;
   return (int)(groups < 256 * per_cu ? groups : 256 * per_cu);
 }
