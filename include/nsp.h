@@ -563,7 +563,10 @@ typedef enum { NSP_NORM_LAYER = 0, NSP_NORM_RMS = 1 } nsp_norm_kind;
  *   dtype       of x and y; w_dtype of w and b (each NSP_BF16 or NSP_F32)
  *   n           1 .. 65536
  *   w, b        n contiguous elements; NULL: ones, zeros
- *   eps         finite, >= 0
+ *   eps         finite, >= 0.  The squares are float32's: below 2^-126 they keep
+ *               fewer bits (v is off by up to 2^-149, and 0 where all differences are
+ *               below 2^-75), and where their sum passes 2^128 (differences of some 1e19)
+ *               v is infinite and rstd 0
  *   y           in place allowed
  *   mean, rstd  float32 [n_tokens * n_heads] in row order (t, then h), for the
  *               backward; either may be NULL (mean is not written by NSP_NORM_RMS)

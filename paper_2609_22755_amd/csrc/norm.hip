@@ -188,7 +188,7 @@ __global__ __launch_bounds__(kBlock<LPR>) void norm_fwd_kernel(NormArgs a) {
       }
     }
     RowSum<LPR, 1>::run(sq, slots, turn);
-    const float rstd = __builtin_amdgcn_rsqf(sq[0] * inv_n + a.eps);
+    const float rstd = rsqrtf(sq[0] * inv_n + a.eps);   // (the instruction alone takes subnormal variances for 0)
     const bool live = row0 + group < a.rows;
     const int row = live ? (int)row0 + group : a.rows - 1;
     done.row = live ? row_at<T>(a.y, a.heads, row) : nullptr;
@@ -486,7 +486,7 @@ __global__ __launch_bounds__(1024) void norm_fwd_wide_kernel(NormArgs a) {
       for (int e = 0; e < V; ++e) sq[0] += (v[e] - mean) * (v[e] - mean);
     }
     RowSum<1024, 1>::run(sq, slots, turn);
-    const float rstd = __builtin_amdgcn_rsqf(sq[0] / (float)a.n + a.eps);
+    const float rstd = rsqrtf(sq[0] / (float)a.n + a.eps);
     for (int i = threadIdx.x * V; i < a.n; i += 1024 * V) {
       float v[V], w[V], b[V];
       load_vec(x + i, a.n - i, 0.f, v);
