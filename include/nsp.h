@@ -619,8 +619,10 @@ size_t nsp_token_logp_workspace(int64_t n_tokens, int32_t vocab, int32_t top);
  * masked vocabulary: they have p = 0 and are no alternatives (places past the
  * last logit above hold index -1 and -inf).  A row of nothing else has lse =
  * -inf, entropy 0, and logp = -inf unless its target is ignored.  A row with a
- * NaN or +inf (or 2^126 / scale and more) has lse and entropy NaN, and logp and the alternatives' values
- * too (NaN itself is never an alternative).
+ * NaN or +inf, or whose largest logit m has |scale m log2(e)| of 2^128 and more
+ * (|scale m| from 2.36e38 on: float32 holds no lse of it), has lse and entropy NaN,
+ * and logp (unless its target is ignored) and the alternatives' values too (NaN
+ * itself is never an alternative).
  *   dtype       of the logits (NSP_BF16 or NSP_F32)
  *   row_stride  >= 0 (rows may coincide)
  *   targets     DEVICE, n_tokens int64; NULL with logp NULL
@@ -646,8 +648,9 @@ nsp_status nsp_token_logp_fwd(nsp_dtype dtype, int64_t n_tokens, int32_t vocab, 
  *                        - g_entropy p_v (z_v - lse + entropy))
  * in float32, rounded once, with p = exp(z - lse) of the lse given (at most 1;
  * where |lse| is 2^24 and more, its own rounding shows).  An ignored target takes g_logp as 0.  A row of
- * masked logits alone (lse = -inf) has gradient 0, and so has a row whose three gradients are
- * 0, whatever its logits.  The alternatives' values have no gradient.
+ * masked logits alone (lse = -inf) has gradient 0, and so has a row whose three
+ * gradients are 0, whatever its logits.  With an lse of NaN or +inf the row's
+ * gradient is NaN.  The alternatives' values have no gradient.
  *   targets     may be NULL with g_logp NULL
  *   lse         the forward's; entropy too, needed with g_entropy (else may
  *               be NULL)

@@ -49,6 +49,7 @@ constexpr float kMasked = -0x1p126f;
 // is 2^102 or more below it.
 constexpr float kNoRef = -0x1.fffffep125f;
 constexpr float kNegInf = -__builtin_inff();
+constexpr float kNan = __builtin_nanf("");
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -180,8 +181,14 @@ struct Largest {
 struct Finish {
   float r, m, log_s, c;
   bool none;                 // nothing but masked logits
+  // The reference is taken from its logit again: what the sums hold is cut off at
+  // -2^127.  Past float32 it leaves nothing of the row but NaN.
   __device__ __forceinline__ Finish(const Sums &x, float scale_log2)
-      : r(x.r), m(x.m), log_s(log2f(x.s)), c(scale_log2), none(x.s == 0.f) {}
+      : r(reference(x.m, scale_log2)), m(x.m), log_s(fabsf(r) < -kNegInf ? log2f(x.s) : kNan), c(scale_log2), none(x.s == 0.f) {}
+  __device__ __forceinline__ static float reference(float m, float c) {
+#pragma clang fp contract(off)
+    return m * c;            // (rounded, as it was subtracted)
+  }
   __device__ __forceinline__ float logp(float z) const {
     return none ? kNegInf : ((is_far(r) ? (z - m) * c : fmaf(z, c, -r)) - log_s) * kLn2;
   }
@@ -423,7 +430,7 @@ __global__ __launch_bounds__(kThreads) void token_logp_bwd_kernel(LogpBwdArgs a,
     const float lse = a.lse[row];
     const bool zero = lse == kNegInf || (gl == 0.f && gs == 0.f && ge == 0.f);
     // dz = p (k0 + k1 d), d = (z - lse) log2(e)
-    const float nan = lse != lse ? lse : 0.f;          // (p is none, whatever lse is)
+    const float nan = lse < -kNegInf ? 0.f : kNan;     // (without an lse there is no p)
     const float k0 = a.scale * (gs - gl - (ge != 0.f ? ge * a.entropy[row] : 0.f)) + nan;
     const float k1 = -a.scale * ge * kLn2, at_y = zero ? 0.f : a.scale * gl;
     const auto gradient = [&](const float (&v)[V], int e0, float (&o)[V]) {
