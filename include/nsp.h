@@ -616,8 +616,9 @@ size_t nsp_token_logp_workspace(int64_t n_tokens, int32_t vocab, int32_t top);
  *                  first, equal ones by the lower index; z - lse of each
  * A target outside 0 .. vocab - 1 is ignored: logp = 0.  Logits of -2^126
  * (-8.5e37) and below, -inf and the types' lowest values among them, are a
- * masked vocabulary: they have p = 0 and are no alternatives (places past the
- * last logit above hold index -1 and -inf).  A row of nothing else has lse =
+ * masked vocabulary: they have p = 0, as targets logp = -inf, and are no
+ * alternatives (places past the last logit above hold index -1 and -inf).  (A log
+ * probability below -2.3e38 may come out as -inf too.)  A row of nothing else has lse =
  * -inf, entropy 0, and logp = -inf unless its target is ignored.  A row with a
  * NaN or +inf, or whose largest logit m has |scale m log2(e)| of 2^128 and more
  * (|scale m| from 2.36e38 on: float32 holds no lse of it), has lse and entropy NaN,

@@ -71,7 +71,7 @@ def token_logp(logits, targets, scale=1.0, top=0):
             ent = lse - (p[p > 0] * z[p > 0]).sum()
         out["lse"][t], out["entropy"][t] = lse, ent
         if given:
-            out["logp"][t] = -np.inf if lse == -np.inf else raw[t, y] * scale - lse
+            out["logp"][t] = -np.inf if lse == -np.inf else z[y] - lse
         order = [v for v in np.lexsort((np.arange(V), -np.where(np.isnan(raw[t]), -np.inf, raw[t])))[:top]
                  if raw[t, v] > MASKED]
         out["top_index"][t, :len(order)] = order

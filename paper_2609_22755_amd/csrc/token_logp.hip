@@ -196,7 +196,7 @@ struct Finish {
   __device__ __forceinline__ void row(const LogpArgs &a, int row, const Sums &x, int64_t y, float z) const {
     a.lse[row] = none ? kNegInf : (r + log_s) * kLn2;
     if (a.entropy) a.entropy[row] = none ? 0.f : (log_s - x.u / x.s) * kLn2;
-    if (a.logp) a.logp[row] = y >= 0 && y < a.vocab ? logp(z) : 0.f;
+    if (a.logp) a.logp[row] = y >= 0 && y < a.vocab ? logp(z <= kMasked ? kNegInf : z) : 0.f;
   }
   __device__ __forceinline__ void top(const LogpArgs &a, int row, int i, uint64_t key) const {
     const int64_t at = (int64_t)row * a.top + i;
