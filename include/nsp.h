@@ -465,8 +465,10 @@ nsp_status nsp_sp_tree_worklist(const nsp_plan_params *prm, const int64_t *lengt
  * through a norm before the projections, the query and key heads through a
  * norm and the rotation by their positions before the prologue, and the last
  * rows' logits into the log probabilities that are trained on or answered
- * with.  All three are bound by memory: every call reads each input once and
- * writes each output once, however the rows lie.
+ * with.  All three are bound by memory: a call reads each input once and writes
+ * each output once, however the rows lie, but for the norms of rows of more than
+ * 16384 elements or less than 16 bytes, which pass over a row two or three times,
+ * and the weight gradients of those and of few rows, which read the rows once more.
  *
  * They share the conventions above, with these differences:
  *   - A tensor of rows is given as nsp_rows: row (t, h) of token t and head h
@@ -585,7 +587,8 @@ size_t nsp_norm_bwd_workspace(int64_t n_tokens, int32_t n_heads, int32_t n);
  * Gradient of the norm, with h = dy w, xh = (x - m) rstd and means over the row:
  *     dx = rstd (h - mean(h) - xh mean(h xh))    (NSP_NORM_RMS: without mean(h))
  *     dw = sum over rows of dy xh,  db = sum over rows of dy
- * the sums over rows in float32, in a fixed order, rounded once to w_dtype.
+ * the sums over rows in float32, in a fixed order, at most 128 + rows / 256 terms
+ * one after another, rounded once to w_dtype.
  *   x, w        as in the forward; mean, rstd its outputs (mean is not read by
  *               NSP_NORM_RMS and may be NULL)
  *   dx          may be dy's or x's very view

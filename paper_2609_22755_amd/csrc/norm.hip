@@ -235,19 +235,19 @@ __device__ __forceinline__ void store_weight(void *out, bool f32, int c, float t
 }
 
 // dw, db straight from x and dy, by the workgroup `block` of those that do: 4 or
-// 8 lanes' vectors of columns, the rows in strands of so many lanes.  Where rows
-// are few, the parts of a workgroup for each would be as much memory as the rows
-// themselves, and a kernel more; where dx leaves x and dy alone, it is formed
-// beside this.
-template <class T, int THREADS>
-__device__ __forceinline__ void norm_columns(const NormArgs &a, int block) {
+// 8 lanes' vectors of columns, the rows first .. last in strands of so many lanes.
+// Where rows are few, the parts of a workgroup for each would be as much memory as
+// the rows themselves, and a kernel more; where dx leaves x and dy alone, it is
+// formed beside this.  PART: a part of the rows, left at `part`.
+template <class T, int THREADS, bool PART = false>
+__device__ __forceinline__ void norm_columns(const NormArgs &a, int block, int64_t first, int64_t last, float *part = nullptr) {
   constexpr int V = kVec<T>, LANES = THREADS > 256 ? 8 : 4, STRANDS = THREADS / LANES;
   __shared__ float lds[THREADS / 64][LANES * V];
   const int col = block * (LANES * V) + (threadIdx.x % LANES) * V, cnt = a.n - col;
   float dw[V] = {}, db[V] = {}, t;
   if (cnt > 0) {
 #pragma unroll 8
-    for (int64_t row = threadIdx.x / LANES; row < a.rows; row += STRANDS) {
+    for (int64_t row = first + threadIdx.x / LANES; row < last; row += STRANDS) {
       float x[V], g[V];
       load_vec_kept(row_at<const T>(a.x, a.heads, (int)row) + col, cnt, 0.f, x);
       load_vec_kept(row_at<const T>(a.dy, a.heads, (int)row) + col, cnt, 0.f, g);
@@ -263,11 +263,11 @@ __device__ __forceinline__ void norm_columns(const NormArgs &a, int block) {
   const bool mine = threadIdx.x < LANES * V && c < a.n;
   if (a.dw) {
     strand_sums<THREADS / 64, LANES, V>(dw, lds, &t);
-    if (mine) store_weight(a.dw, a.w_f32, c, t);
+    if (mine) store_weight(PART ? part : a.dw, PART || a.w_f32, c, t);
   }
   if (a.db) {
     strand_sums<THREADS / 64, LANES, V>(db, lds, &t);
-    if (mine) store_weight(a.db, a.w_f32, c, t);
+    if (mine) store_weight(PART ? part + a.n : a.db, PART || a.w_f32, c, t);
   }
 }
 template <class T, int THREADS>
@@ -276,9 +276,11 @@ int column_blocks(int n) {
   return (n + per - 1) / per;
 }
 
-template <class T>
+// By all workgroups of a launch, in its y as many parts of the rows.
+template <class T, bool PART>
 __global__ __launch_bounds__(1024) void norm_columns_kernel(NormArgs a) {
-  norm_columns<T, 1024>(a, blockIdx.x);
+  const int64_t per = ((int64_t)a.rows + gridDim.y - 1) / gridDim.y, first = blockIdx.y * per;
+  norm_columns<T, 1024, PART>(a, blockIdx.x, first, min(first + per, (int64_t)a.rows), PART ? a.part + (int64_t)blockIdx.y * 2 * a.n : nullptr);
 }
 
 // A row is kept as it was loaded until it is done: unpacking it twice is
@@ -292,7 +294,7 @@ __global__ __launch_bounds__(kBlock<LPR>) void norm_bwd_kernel(NormArgs a) {
   constexpr int V = kVec<T>;
   constexpr int RPB = kGroups<LPR>;
   if constexpr (COLUMNS)
-    if ((int)blockIdx.x < a.column_blocks) return norm_columns<T, kBlock<LPR>>(a, blockIdx.x);
+    if ((int)blockIdx.x < a.column_blocks) return norm_columns<T, kBlock<LPR>>(a, blockIdx.x, 0, a.rows);
   const int before = COLUMNS ? a.column_blocks : 0, block = (int)blockIdx.x - before, blocks = (int)gridDim.x - before;
   __shared__ float slots[2 * 2 * RPB * (LPR / 64 + 1)];
   const int lane = threadIdx.x % LPR, group = threadIdx.x / LPR;
@@ -623,15 +625,17 @@ hipError_t bwd(const NormArgs &a, hipStream_t s) {
   const int parts = norm_bwd_parts(a.rows, a.n, f32);
   const bool columns = (a.dw || a.db) && parts == 0;
   hipError_t e = hipSuccess;
-  if (columns && (a.rows == 0 || sh.lpr == 0)) {
-    norm_columns_kernel<T><<<column_blocks<T, 1024>(a.n), 1024, 0, s>>>(a);
+  NormArgs b = a;
+  if (parts == 0) b.part = nullptr;
+  if ((a.dw || a.db) && (a.rows == 0 || sh.lpr == 0)) {   // (before dx, which may lie over x or dy)
+    const int strips = column_blocks<T, 1024>(a.n);
+    if (b.part) norm_columns_kernel<T, true><<<dim3(strips, parts), 1024, 0, s>>>(b);
+    else norm_columns_kernel<T, false><<<strips, 1024, 0, s>>>(b);
     e = hipGetLastError();
   }
   if (e != hipSuccess || a.rows == 0) return e;
-  NormArgs b = a;
-  if (parts == 0) b.part = nullptr;
   const int64_t groups = ((int64_t)a.rows + sh.rows() - 1) / sh.rows();
-  const int grid = b.part ? parts : (int)(groups < kBwdMost ? groups : kBwdMost);
+  const int grid = b.part && sh.lpr > 0 ? parts : (int)(groups < kBwdMost ? groups : kBwdMost);
   if (sh.lpr == 0)
     norm_bwd_wide_kernel<T><<<grid, 1024, 0, s>>>(b);
   else
@@ -668,7 +672,9 @@ int norm_bwd_parts(int64_t rows, int n, bool f32) {
   // Few rows: without parts 24 x 4096 bf16 5.4 us, with them 11.3; 200 x 1000 6.8
   // and 9.1; 500 x 128 float32 8.3 and 7.1.  Wide ones longer: 600 x 8192 19.0 and
   // 24.9; 500 x 4096 24.8 and 18.3.
-  if (rows <= 200 || sh.lpr == 0 || (rows <= 640 && rows * 12 <= n)) return 0;
+  if (rows <= 200 || (rows <= 640 && rows * 12 <= n)) return 0;
+  // The widths of the wide kernels: parts of 4096 rows, 32 a strand one after another.
+  if (sh.lpr == 0) return rows <= 4096 ? 0 : rows <= 1023 * 4096 ? (int)((rows + 4095) / 4096) : 1024;
   const int64_t groups = (rows + sh.rows() - 1) / sh.rows();
   int per_cu = sh.lpr > 256 || sh.ch > 3 ? 1 : sh.ch > 1 ? 2 : 3;
   while (per_cu > 1 && groups < 4 * 256 * per_cu) --per_cu;

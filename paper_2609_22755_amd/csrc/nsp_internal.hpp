@@ -221,8 +221,8 @@ struct NormArgs {
   float *part;               // [parts][2][n]: dw, db
   int32_t column_blocks;     // the first workgroups form dw and db from the rows
 };
-// Workgroups of the backward that leave a partial sum; 0: dw and db are formed
-// without any.
+// Workgroups (at the widths of the wide kernels: parts of the rows) of the backward
+// that leave a partial sum, 1024 at most; 0: dw and db are formed without any.
 int norm_bwd_parts(int64_t rows, int n, bool f32);
 hipError_t launch_norm_fwd(bool f32, const NormArgs &a, hipStream_t s);
 hipError_t launch_norm_bwd(bool f32, const NormArgs &a, hipStream_t s);
