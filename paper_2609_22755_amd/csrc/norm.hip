@@ -24,12 +24,6 @@
 namespace nsp {
 namespace {
 
-// The forward's workgroups take four row groups in turn, where there are so
-// many (fewer reload the weights more often, more leave the last ones alone: rows
-// of 8192 bf16 6.1 TB/s, with two 5.7, with eight 5.9).
-constexpr int kFwdTurns = 4, kFwdLeast = 2048, kFwdMost = 1 << 21;
-constexpr int kBwdMost = 1024;   // workgroups of a backward that leaves no parts
-
 template <class T>
 __device__ __forceinline__ T *row_at(const RowView &v, const FastDiv &heads, int row) {
   const uint32_t t = heads.quot((uint32_t)row);
@@ -562,67 +556,40 @@ __global__ __launch_bounds__(1024) void norm_weight_kernel(const float *part, in
   if (threadIdx.x < 32 && c < n) store_weight(out, f32, c, t);
 }
 
-// Lanes of a row, and its vectors a lane; 0 lanes: the wide kernels.
-struct NormShape {
-  int lpr, ch;
-  int rows() const { return lpr > 0 && lpr < 256 ? 256 / lpr : 1; }   // of a workgroup
-};
-
-// The first of a list that holds the row is taken.  A wave holds a row as long
-// as its lanes do (up to 32 elements each: sums without a barrier; float32 rows
-// of 1111 in 5 vectors a lane 5.6 TB/s backward, in 4 of 128 lanes 5.0), then few
-// wide groups; three vectors a lane where four would leave many empty (10000 bf16
-// forward 5.3 TB/s in 3 of 512 lanes, 4.1 in 2 of 1024).
-constexpr NormShape kFwdShapes[] = {{16, 1},  {16, 2},  {64, 1},  {64, 2},  {64, 3},   {64, 4},  {128, 3},
-                                    {128, 4}, {256, 3}, {512, 2}, {512, 3}, {1024, 2}, {1024, 4}};
-constexpr NormShape kBwdShapes[] = {{16, 1}, {16, 2}, {64, 1},  {64, 2},  {64, 3},  {64, 4},  {64, 5},  {64, 6},
-                                    {64, 8}, {128, 3}, {128, 4}, {512, 1}, {512, 2}, {512, 3}, {512, 4}, {1024, 4}};
-
-// Whether a type's vectors of v elements go in this shape: 32 elements a lane,
-// 16 where 1024 lanes leave 128 registers each.
-constexpr bool fits(int lpr, int ch, int v) { return ch * v <= (lpr < 1024 ? 32 : 16); }
-
-template <int N>
-NormShape norm_shape(const NormShape (&shapes)[N], int n, bool f32) {
-  const int v = f32 ? 4 : 8, vecs = (n + v - 1) / v;
-  if (n < v) return {0, 0};
-  for (const NormShape s : shapes)
-    if (s.lpr * s.ch >= vecs && fits(s.lpr, s.ch, v)) return s;
-  return {0, 0};
-}
-
-// f(lanes, vectors) of the shape s among `shapes`, as compile-time numbers.
+// f(lanes, vectors) of the shape s among `shapes`, as compile-time numbers; false
+// if it is none of them.
 template <const auto &SHAPES, size_t I = 0, class F>
-void with_shape(NormShape s, F f) {
+bool with_shape(plan::NormShape s, F f) {
   if constexpr (I < sizeof(SHAPES) / sizeof(SHAPES[0])) {
-    if (s.lpr == SHAPES[I].lpr && s.ch == SHAPES[I].ch)
-      f(std::integral_constant<int, SHAPES[I].lpr>(), std::integral_constant<int, SHAPES[I].ch>());
-    else
-      with_shape<SHAPES, I + 1>(s, f);
+    if (s.lpr != SHAPES[I].lpr || s.ch != SHAPES[I].ch) return with_shape<SHAPES, I + 1>(s, f);
+    f(std::integral_constant<int, SHAPES[I].lpr>(), std::integral_constant<int, SHAPES[I].ch>());
+    return true;
+  } else {
+    return false;
   }
 }
 
 template <class T>
 hipError_t fwd(const NormArgs &a, hipStream_t s) {
-  const NormShape sh = norm_shape(kFwdShapes, a.n, sizeof(T) == 4);
-  const int64_t groups = ((int64_t)a.rows + sh.rows() - 1) / sh.rows();
-  int64_t grid = groups / kFwdTurns > kFwdLeast ? groups / kFwdTurns : groups < kFwdLeast ? groups : kFwdLeast;
-  if (grid > kFwdMost) grid = kFwdMost;
-  if (sh.lpr == 0)
-    norm_fwd_wide_kernel<T><<<(int)grid, 1024, 0, s>>>(a);
-  else
-    with_shape<kFwdShapes>(sh, [&](auto lpr, auto ch) {
-      constexpr int L = decltype(lpr)::value, C = decltype(ch)::value;
-      if constexpr (fits(L, C, kVec<T>)) norm_fwd_kernel<T, L, C><<<(int)grid, kBlock<L>, 0, s>>>(a);
-    });
-  return hipGetLastError();
+  constexpr bool f32 = sizeof(T) == 4;
+  const plan::NormShape sh = plan::norm_fwd_shape(a.n, f32);
+  const int grid = plan::norm_fwd_grid(a.rows, sh);
+  const auto launch = [&](auto lpr, auto ch) {
+    constexpr int L = decltype(lpr)::value, C = decltype(ch)::value;
+    norm_fwd_kernel<T, L, C><<<grid, kBlock<L>, 0, s>>>(a);
+  };
+  bool known = true;
+  if (sh.lpr == 0) norm_fwd_wide_kernel<T><<<grid, 1024, 0, s>>>(a);
+  else if constexpr (f32) known = with_shape<plan::kNormFwdF32>(sh, launch);
+  else known = with_shape<plan::kNormFwdBf16>(sh, launch);
+  return known ? hipGetLastError() : hipErrorInvalidValue;
 }
 
 template <class T>
 hipError_t bwd(const NormArgs &a, hipStream_t s) {
   constexpr bool f32 = sizeof(T) == 4;
-  const NormShape sh = norm_shape(kBwdShapes, a.n, f32);
-  const int parts = norm_bwd_parts(a.rows, a.n, f32);
+  const plan::NormShape sh = plan::norm_bwd_shape(a.n, f32);
+  const int parts = plan::norm_parts(a.rows, a.n, f32);
   const bool columns = (a.dw || a.db) && parts == 0;
   hipError_t e = hipSuccess;
   NormArgs b = a;
@@ -634,25 +601,23 @@ hipError_t bwd(const NormArgs &a, hipStream_t s) {
     e = hipGetLastError();
   }
   if (e != hipSuccess || a.rows == 0) return e;
-  const int64_t groups = ((int64_t)a.rows + sh.rows() - 1) / sh.rows();
-  const int grid = b.part && sh.lpr > 0 ? parts : (int)(groups < kBwdMost ? groups : kBwdMost);
-  if (sh.lpr == 0)
-    norm_bwd_wide_kernel<T><<<grid, 1024, 0, s>>>(b);
-  else
-    with_shape<kBwdShapes>(sh, [&](auto lpr, auto ch) {
-      constexpr int L = decltype(lpr)::value, C = decltype(ch)::value;
-      if constexpr (fits(L, C, kVec<T>)) {
-        b.column_blocks = columns ? column_blocks<T, kBlock<L>>(a.n) : 0;
-        // dw and db read what dx in place would overwrite: by a launch of their own, before
-        if (columns && (a.y.data == a.x.data || a.y.data == a.dy.data)) {
-          norm_bwd_kernel<T, L, C, true><<<b.column_blocks, kBlock<L>, 0, s>>>(b);
-          b.column_blocks = 0;
-        }
-        if (b.column_blocks > 0) norm_bwd_kernel<T, L, C, true><<<grid + b.column_blocks, kBlock<L>, 0, s>>>(b);
-        else norm_bwd_kernel<T, L, C, false><<<grid, kBlock<L>, 0, s>>>(b);
-      }
-    });
-  e = hipGetLastError();
+  const int grid = plan::norm_bwd_grid(a.rows, sh, b.part ? parts : 0);
+  const auto launch = [&](auto lpr, auto ch) {
+    constexpr int L = decltype(lpr)::value, C = decltype(ch)::value;
+    b.column_blocks = columns ? column_blocks<T, kBlock<L>>(a.n) : 0;
+    // dw and db read what dx in place would overwrite: by a launch of their own, before
+    if (columns && (a.y.data == a.x.data || a.y.data == a.dy.data)) {
+      norm_bwd_kernel<T, L, C, true><<<b.column_blocks, kBlock<L>, 0, s>>>(b);
+      b.column_blocks = 0;
+    }
+    if (b.column_blocks > 0) norm_bwd_kernel<T, L, C, true><<<grid + b.column_blocks, kBlock<L>, 0, s>>>(b);
+    else norm_bwd_kernel<T, L, C, false><<<grid, kBlock<L>, 0, s>>>(b);
+  };
+  bool known = true;
+  if (sh.lpr == 0) norm_bwd_wide_kernel<T><<<grid, 1024, 0, s>>>(b);
+  else if constexpr (f32) known = with_shape<plan::kNormBwdF32>(sh, launch);
+  else known = with_shape<plan::kNormBwdBf16>(sh, launch);
+  e = known ? hipGetLastError() : hipErrorInvalidValue;
   if (e == hipSuccess && b.part) {
     norm_weight_kernel<<<dim3((a.n + 31) / 32, 2), 1024, 0, s>>>(a.part, parts, a.n, a.dw, a.db, a.w_f32);
     e = hipGetLastError();
@@ -662,24 +627,7 @@ hipError_t bwd(const NormArgs &a, hipStream_t s) {
 
 }  // namespace
 
-// As many workgroups as keep some 32 KB a compute unit on the way (a lane has
-// its next row's vectors of x and dy in flight): more of them get in each
-// other's way in memory (2 M rows of 128 bf16: three a compute unit 264 us, two
-// 277, four 306), and each leaves a part; fewer leave it idle (120 K rows of 1111
-// bf16, three vectors a lane: two 182 us, one 207).
-int norm_bwd_parts(int64_t rows, int n, bool f32) {
-  const NormShape sh = norm_shape(kBwdShapes, n, f32);
-  // Few rows: without parts 24 x 4096 bf16 5.4 us, with them 11.3; 200 x 1000 6.8
-  // and 9.1; 500 x 128 float32 8.3 and 7.1.  Wide ones longer: 600 x 8192 19.0 and
-  // 24.9; 500 x 4096 24.8 and 18.3.
-  if (rows <= 200 || (rows <= 640 && rows * 12 <= n)) return 0;
-  // The widths of the wide kernels: parts of 4096 rows, 32 a strand one after another.
-  if (sh.lpr == 0) return rows <= 4096 ? 0 : rows <= 1023 * 4096 ? (int)((rows + 4095) / 4096) : 1024;
-  const int64_t groups = (rows + sh.rows() - 1) / sh.rows();
-  int per_cu = sh.lpr > 256 || sh.ch > 3 ? 1 : sh.ch > 1 ? 2 : 3;
-  while (per_cu > 1 && groups < 4 * 256 * per_cu) --per_cu;
-  return (int)(groups < 256 * per_cu ? groups : 256 * per_cu);
-}
+int norm_bwd_parts(int64_t rows, int n, bool f32) { return plan::norm_parts(rows, n, f32); }
 
 hipError_t launch_norm_fwd(bool f32, const NormArgs &a, hipStream_t s) { return f32 ? fwd<float>(a, s) : fwd<bf16>(a, s); }
 hipError_t launch_norm_bwd(bool f32, const NormArgs &a, hipStream_t s) { return f32 ? bwd<float>(a, s) : bwd<bf16>(a, s); }

@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "row_plans.hpp"
+
 namespace nsp {
 
 // One item of the work list in the attention layout.  Offsets are in
@@ -227,8 +229,7 @@ int norm_bwd_parts(int64_t rows, int n, bool f32);
 hipError_t launch_norm_fwd(bool f32, const NormArgs &a, hipStream_t s);
 hipError_t launch_norm_bwd(bool f32, const NormArgs &a, hipStream_t s);
 
-// Most parts that a row of logits is split in.
-constexpr int kLogpMaxParts = 64;
+using plan::kLogpMaxParts;
 // Widest vocabulary.
 constexpr int kLogpMaxVocab = 1 << 30;
 struct LogpArgs {

@@ -466,7 +466,7 @@ template <class T>
 hipError_t fwd(LogpArgs a, hipStream_t s) {
   constexpr int V = kVec<T>;
   const int64_t units = (int64_t)a.n_tokens * a.parts;
-  a.part_len = (((a.vocab + a.parts - 1) / a.parts) + V - 1) / V * V;
+  a.part_len = plan::logp_part_len(a.vocab, a.parts, V);
   a.by_parts = FastDiv(a.parts);
   const int grid = (int)(units < kMaxGrid ? units : kMaxGrid);
   if (a.top > 0) token_logp_fwd_kernel<T, true><<<grid, kThreads, 0, s>>>(a);
@@ -488,17 +488,7 @@ hipError_t bwd(const LogpBwdArgs &a, hipStream_t s) {
 
 }  // namespace
 
-int token_logp_parts(int64_t n_tokens, int vocab) {
-  if (n_tokens <= 0) return 1;
-    // Two workgroups a compute unit, each with 2048 elements at least.  (32 rows of
-  // 131072 with one alternative: 11.4 us, with four a compute unit 13.8, with eight
-  // 17.9; 1000 rows of 32000 with five, one part a row, 19.4, two 28.6.)
-  int64_t p = (512 + n_tokens - 1) / n_tokens;
-  const int64_t most = (vocab + 2047) / 2048;
-  if (p > most) p = most;
-  if (p > kLogpMaxParts) p = kLogpMaxParts;
-  return (int)p;
-}
+int token_logp_parts(int64_t n_tokens, int vocab) { return plan::logp_parts(n_tokens, vocab); }
 
 hipError_t launch_token_logp_fwd(bool f32, const LogpArgs &a, hipStream_t s) { return f32 ? fwd<float>(a, s) : fwd<bf16>(a, s); }
 hipError_t launch_token_logp_bwd(bool f32, const LogpBwdArgs &a, hipStream_t s) { return f32 ? bwd<float>(a, s) : bwd<bf16>(a, s); }
