@@ -23,7 +23,7 @@ namespace {
 
 // Python objects that every call needs; set up with the module, never freed.
 PyObject *g_bf16, *g_f32, *g_f64, *g_i64, *g_error, *g_raw_stream;
-PyObject *s_dtype, *s_shape, *s_stride, *s_data_ptr, *s_get_device, *s_numel, *s_is_contiguous, *s_element_size, *s_cuda_stream;
+PyObject *s_dtype, *s_shape, *s_stride, *s_data_ptr, *s_get_device, *s_numel, *s_is_contiguous, *s_element_size, *s_cuda_stream, *s_device_index;
 
 struct Failed {};   // a Python error is set
 
@@ -176,7 +176,8 @@ float real(PyObject *o, float none) {
 
 int whole(PyObject *o, int none) { return o ? (int)number(o) : none; }
 
-// call(stream) with the tensors' GPU current, on `stream` (None: that GPU's current one).
+// call(stream) with the tensors' GPU current, on `stream` (None: that GPU's current
+// one; a Stream of another GPU is refused, a handle is taken as it is).
 template <class F>
 PyObject *launch(const char *name, const Place &at, PyObject *stream, F call) {
   if (at.dev < 0) fail(PyExc_TypeError, std::string(name) + ": tensors must be on the GPU");
@@ -187,6 +188,14 @@ PyObject *launch(const char *name, const Place &at, PyObject *stream, F call) {
     } else {
       Ref h(PyObject_GetAttr(stream, s_cuda_stream));
       s = reinterpret_cast<hipStream_t>(number(h.o));
+      PyObject *d = PyObject_GetAttr(stream, s_device_index);
+      if (d) {
+        Ref r(d);
+        if (number(d) != at.dev)
+          fail(PyExc_ValueError, "stream: of GPU " + std::to_string(number(d)) + ", the tensors are on GPU " + std::to_string(at.dev));
+      } else {
+        PyErr_Clear();
+      }
     }
   } else {
     Ref dev(PyLong_FromLong(at.dev));
@@ -453,7 +462,7 @@ PyMODINIT_FUNC PyInit__rows() {
   return guarded([]() -> PyObject * {
     for (auto [p, s] : {std::pair{&s_dtype, "dtype"}, {&s_shape, "shape"}, {&s_stride, "stride"}, {&s_data_ptr, "data_ptr"},
                         {&s_get_device, "get_device"}, {&s_numel, "numel"}, {&s_is_contiguous, "is_contiguous"},
-                        {&s_element_size, "element_size"}, {&s_cuda_stream, "cuda_stream"}})
+                        {&s_element_size, "element_size"}, {&s_cuda_stream, "cuda_stream"}, {&s_device_index, "device_index"}})
       if (!(*p = PyUnicode_InternFromString(s))) throw Failed();
     for (Signature *f : {&k_rotary_fwd, &k_rotary_bwd, &k_norm_fwd, &k_norm_bwd, &k_logp_fwd, &k_logp_bwd})
       for (int i = 0; i < f->n; ++i)

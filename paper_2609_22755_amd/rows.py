@@ -5,7 +5,8 @@ probabilities) on torch tensors: the part of the binding that
 
 Sizes, strides and types come from the tensors: a wrong one raises TypeError or
 ValueError; what the C ABI refuses raises NspError.  A call goes to the GPU that
-holds the tensors, by default on its current stream.
+holds the tensors, by default on its current stream; a Stream of another GPU
+raises ValueError.
 """
 from __future__ import annotations
 
