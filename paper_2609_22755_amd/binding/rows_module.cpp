@@ -174,7 +174,12 @@ float real(PyObject *o, float none) {
   return (float)v;
 }
 
-int whole(PyObject *o, int none) { return o ? (int)number(o) : none; }
+int whole(PyObject *o, int none, const char *name) {
+  if (!o) return none;
+  const long long v = number(o);
+  if (v != (int)v) fail(PyExc_ValueError, std::string(name) + ": " + std::to_string(v) + " is past 32 bits");
+  return (int)v;
+}
 
 // call(stream) with the tensors' GPU current, on `stream` (None: that GPU's current
 // one; a Stream of another GPU is refused, a handle is taken as it is).
@@ -280,7 +285,7 @@ PyObject *rotary(const Signature &f, bool bwd, PyObject *const *args, Py_ssize_t
   const auto *freqs = static_cast<const double *>(array(a[1], half, g_f64, at, "freqs"));
   const nsp_dtype c = code(dtype, nm[0]);
   const float scale = real(a[6], 1.f);
-  const auto layout = (nsp_rotary_layout)whole(a[7], NSP_ROTARY_HALF);
+  const auto layout = (nsp_rotary_layout)whole(a[7], NSP_ROTARY_HALF, "layout");
   if (d.d[1] > INT32_MAX || dk.d[1] > INT32_MAX || d.d[2] > INT32_MAX || half > INT32_MAX / 2) fail(PyExc_ValueError, "sizes past 2^31 - 1");
   const bool keys = dk.d[1] > 0;
   return launch(f.function, at, a[8], [&](hipStream_t s) {
@@ -314,7 +319,7 @@ PyObject *norm_fwd(PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames) {
   auto *mean = static_cast<float *>(array(a[4], z.T * z.H, g_f32, at, "mean")), *rstd = static_cast<float *>(array(a[5], z.T * z.H, g_f32, at, "rstd"));
   const nsp_dtype c = code(z.dtype, "x"), cw = code(wd, "weight");
   const float eps = real(a[6], 1e-6f);
-  const auto kind = (nsp_norm_kind)whole(a[7], NSP_NORM_LAYER);
+  const auto kind = (nsp_norm_kind)whole(a[7], NSP_NORM_LAYER, "kind");
   return launch("nsp_norm_fwd", at, a[8], [&](hipStream_t s) {
     return nsp_norm_fwd(kind, c, cw, z.T, (int32_t)z.H, (int32_t)z.n, &x, w, b, eps, &y, mean, rstd, s);
   });
@@ -339,7 +344,7 @@ PyObject *norm_bwd(PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames) {
   void *dw = array(a[6], z.n, wd, at, "dweight"), *db = array(a[7], z.n, wd, at, "dbias");
   const Workspace ws(a[8], at);
   const nsp_dtype c = code(z.dtype, "x"), cw = code(wd, "weight");
-  const auto kind = (nsp_norm_kind)whole(a[9], NSP_NORM_LAYER);
+  const auto kind = (nsp_norm_kind)whole(a[9], NSP_NORM_LAYER, "kind");
   return launch("nsp_norm_bwd", at, a[10], [&](hipStream_t s) {
     return nsp_norm_bwd(kind, c, cw, z.T, (int32_t)z.H, (int32_t)z.n, &x, w, &dy, mean, rstd, &dx, dw, db, ws.data, ws.bytes, s);
   });

@@ -56,3 +56,15 @@ def test_a_stream_of_another_gpu_is_refused():
         for gpu in (0, 2):
             with pytest.raises(ValueError, match=f"stream: of GPU {gpu}, the tensors are on GPU 1"):
                 call(_stream(gpu))
+
+
+def test_numbers_past_32_bits_are_refused():
+    x, w = torch.zeros(4, 2, 64), torch.zeros(64)
+    pos, freqs = torch.zeros(4, dtype=torch.int64), torch.zeros(32, dtype=torch.float64)
+    for n in (1 << 32, (1 << 32) + 1, -(1 << 32), 1 << 31):
+        with pytest.raises(ValueError, match="kind"):
+            nsp.nsp_norm_fwd(x, w, None, x, kind=n)
+        with pytest.raises(ValueError, match="kind"):
+            nsp.nsp_norm_bwd(x, w, x, None, torch.zeros(8), x, None, None, None, kind=n)
+        with pytest.raises(ValueError, match="layout"):
+            nsp.nsp_rotary_fwd(pos, freqs, x, x, layout=n)
