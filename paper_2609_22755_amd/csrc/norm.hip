@@ -234,14 +234,14 @@ __device__ __forceinline__ void store_weight(void *out, bool f32, int c, float t
 // the rows themselves, and a kernel more; where dx leaves x and dy alone, it is
 // formed beside this.  PART: a part of the rows, left at `part`.
 template <class T, int THREADS, bool PART = false>
-__device__ __forceinline__ void norm_columns(const NormArgs &a, int block, int64_t first, int64_t last, float *part = nullptr) {
+__device__ __forceinline__ void norm_columns(const NormArgs &a, int block, uint32_t first, uint32_t last, float *part = nullptr) {
   constexpr int V = kVec<T>, LANES = THREADS > 256 ? 8 : 4, STRANDS = THREADS / LANES;
   __shared__ float lds[THREADS / 64][LANES * V];
   const int col = block * (LANES * V) + (threadIdx.x % LANES) * V, cnt = a.n - col;
   float dw[V] = {}, db[V] = {}, t;
   if (cnt > 0) {
 #pragma unroll 8
-    for (int64_t row = first + threadIdx.x / LANES; row < last; row += STRANDS) {
+    for (uint32_t row = first + threadIdx.x / LANES; row < last; row += STRANDS) {
       float x[V], g[V];
       load_vec_kept(row_at<const T>(a.x, a.heads, (int)row) + col, cnt, 0.f, x);
       load_vec_kept(row_at<const T>(a.dy, a.heads, (int)row) + col, cnt, 0.f, g);
@@ -270,11 +270,15 @@ int column_blocks(int n) {
   return (n + per - 1) / per;
 }
 
-// By all workgroups of a launch, in its y as many parts of the rows.
+// By all workgroups of a launch; PART: of `per` rows for each of its y.
 template <class T, bool PART>
-__global__ __launch_bounds__(1024) void norm_columns_kernel(NormArgs a) {
-  const int64_t per = ((int64_t)a.rows + gridDim.y - 1) / gridDim.y, first = blockIdx.y * per;
-  norm_columns<T, 1024, PART>(a, blockIdx.x, first, min(first + per, (int64_t)a.rows), PART ? a.part + (int64_t)blockIdx.y * 2 * a.n : nullptr);
+__global__ __launch_bounds__(1024) void norm_columns_kernel(NormArgs a, uint32_t per) {
+  if constexpr (PART) {
+    const uint32_t first = min(blockIdx.y * per, (uint32_t)a.rows);
+    norm_columns<T, 1024, true>(a, blockIdx.x, first, min(first + per, (uint32_t)a.rows), a.part + (int64_t)blockIdx.y * 2 * a.n);
+  } else {
+    norm_columns<T, 1024>(a, blockIdx.x, 0, a.rows);
+  }
 }
 
 // A row is kept as it was loaded until it is done: unpacking it twice is
@@ -596,8 +600,8 @@ hipError_t bwd(const NormArgs &a, hipStream_t s) {
   if (parts == 0) b.part = nullptr;
   if ((a.dw || a.db) && (a.rows == 0 || sh.lpr == 0)) {   // (before dx, which may lie over x or dy)
     const int strips = column_blocks<T, 1024>(a.n);
-    if (b.part) norm_columns_kernel<T, true><<<dim3(strips, parts), 1024, 0, s>>>(b);
-    else norm_columns_kernel<T, false><<<strips, 1024, 0, s>>>(b);
+    if (b.part) norm_columns_kernel<T, true><<<dim3(strips, parts), 1024, 0, s>>>(b, ((uint32_t)a.rows + parts - 1) / parts);
+    else norm_columns_kernel<T, false><<<strips, 1024, 0, s>>>(b, 0);
     e = hipGetLastError();
   }
   if (e != hipSuccess || a.rows == 0) return e;
