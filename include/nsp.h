@@ -503,7 +503,8 @@ typedef enum { NSP_ROTARY_HALF = 0, NSP_ROTARY_PAIRS = 1 } nsp_rotary_layout;
  * position ids restart at every packed sequence), before nsp_ulysses_pack or
  * the attention.  For token t and pair i < rot_dim / 2, with
  * a = positions[t] * freqs[i] radians (the product and its reduction to a
- * turn in 64 bits: positions of any context are as exact as the first):
+ * turn in 64 bits, off by 2^-51 of a at most: up to angles of 2^27 that is less
+ * than float32's rounding, so far positions are as exact as the first):
  *     (x1, x2) = (x[i], x[i + rot_dim / 2])   NSP_ROTARY_HALF
  *                (x[2 i], x[2 i + 1])         NSP_ROTARY_PAIRS
  *     y1 = scale (x1 cos a - x2 sin a),  y2 = scale (x2 cos a + x1 sin a)
@@ -568,7 +569,8 @@ typedef enum { NSP_NORM_LAYER = 0, NSP_NORM_RMS = 1 } nsp_norm_kind;
  *   eps         finite, >= 0.  The squares are float32's: below 2^-126 they keep
  *               fewer bits (v is off by up to 2^-149, and 0 where all differences are
  *               below 2^-75), and where their sum passes 2^128 (differences of some 1e19)
- *               v is infinite and rstd 0
+ *               v is infinite and rstd 0.  Where v + eps is 0, rstd is infinite
+ *               and the row's y NaN
  *   y           in place allowed
  *   mean, rstd  float32 [n_tokens * n_heads] in row order (t, then h), for the
  *               backward; either may be NULL (mean is not written by NSP_NORM_RMS)

@@ -16,8 +16,8 @@
 // half a head, left half-used lines behind: heads of 96, 3.0 TB/s.)
 //
 // 65536 tokens x 36 heads of 128 bf16: 200 us, 6.0 TB/s (a copy: 5.7); half of
-// each head rotated 198, float32 5.6 TB/s, heads of 80 with 20 rotated (no whole
-// vectors) 84 us, 3.8; 24 tokens 4 us.
+// each head rotated 198, float32 5.6 TB/s, 15 heads of 80 with 20 rotated (no whole
+// vectors) 94 us in halves, 81 in pairs, 3.4 and 3.9; 24 tokens 4 us.
 #include "nsp_internal.hpp"
 #include "row_common.hpp"
 
