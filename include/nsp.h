@@ -671,6 +671,165 @@ nsp_status nsp_token_logp_bwd(nsp_dtype dtype, int64_t n_tokens, int32_t vocab, 
                               void *dlogits, int64_t d_row_stride, hipStream_t stream);
 
 /*
+ * The vocabulary's two ends of a packed step: the embedding of its tokens, log
+ * probabilities of the targets straight from the last hidden rows (at the sizes
+ * of a long-context step the logits do not fit: 393216 rows of 151643 are 119 GB in
+ * bf16), and the loss against a teacher's top alternatives.  They share the row
+ * operators' conventions (rows, in place, overlaps, graphs, workspaces, fixed order
+ * of sums), and:
+ *   - A token or target outside 0 .. vocab - 1 (padding) counts for nothing.
+ *   - dw of a tied weight is the sum of both ends': nsp_embedding_bwd and
+ *     nsp_linear_logp_bwd write into buffers of their own.
+ */
+
+/* Bytes of device workspace of nsp_linear_logp_fwd and _bwd (0 for invalid
+ * sizes and no tokens).  Forward: 16 bytes a token and 256 vocabulary rows, of
+ * 32768 tokens at most.  Backward: the hidden rows gathered (2 n_tokens dim bytes),
+ * the gradient of the logits of one piece of the vocabulary (about 512 MB, more
+ * from 65536 tokens on: 8192 bytes a token), and float32 sums (4 n_tokens dim bytes
+ * with more than one piece, up to 64 times that, 256 MB about, where few
+ * tiles have to be split). */
+size_t nsp_linear_logp_fwd_workspace(int64_t n_tokens, int32_t dim, int32_t vocab);
+size_t nsp_linear_logp_bwd_workspace(int64_t n_tokens, int32_t dim, int32_t vocab);
+
+/*
+ * nsp_token_logp_fwd for logits a[t][v] = <x[t], w[v]> that are not stored
+ * (products of bf16, float32 sums):  with z = scale a[t], p = exp(z - lse)
+ *     lse[t]     = log sum_v exp(z_v)
+ *     logp[t]    = z[targets[t]] - lse[t]
+ *     entropy[t] = lse[t] - sum_v p_v z_v
+ * An ignored target has logp 0.  Logits of -inf have p = 0; a row of nothing
+ * else has lse = -inf, entropy 0 and, unless its target is ignored, logp = -inf.
+ * A row with a NaN or +inf among its logits, or whose lse passes float32, has lse
+ * and entropy NaN, and logp unless its target is ignored.  A row's results depend
+ * on that row of x (and n_tokens) alone.
+ *   x           bf16 [n_tokens] rows of dim elements; w: bf16 [vocab] rows
+ *               (16-byte aligned, strides multiples of 8, up to 2^20)
+ *   n_tokens    up to 2^22; dim: a multiple of 8 up to 65536; vocab: up to 2^24
+ *   targets     DEVICE, n_tokens int64; NULL with logp NULL
+ *   scale       2^-64 .. 2^64
+ *   logp, entropy   float32 [n_tokens]; either may be NULL.  lse: float32
+ *               [n_tokens], needed by the backward
+ *   workspace   nsp_linear_logp_fwd_workspace bytes, 256-byte aligned
+ * Errors: NSP_EINVAL, NSP_EUNSUPPORTED (sizes, strides), NSP_EWORKSPACE, NSP_EHIP.
+ */
+nsp_status nsp_linear_logp_fwd(int64_t n_tokens, int32_t dim, int32_t vocab, const nsp_rows *x, const nsp_rows *w,
+                               const int64_t *targets, float scale, float *logp, float *lse, float *entropy,
+                               void *workspace, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Gradient of the above with respect to x and w, from the gradients of logp,
+ * lse and entropy (float32 [n_tokens]; NULL: zeros).  The logits are made again,
+ * piece by piece of the vocabulary:
+ *     da_v = scale (g_logp (1[v = target] - p_v) + g_lse p_v
+ *                   - g_entropy p_v (z_v - lse + entropy))
+ *     dx[t] = sum_v da[t][v] w[v],   dw[v] = sum_t da[t][v] x[t]
+ * da is rounded to bf16 (half a step of it, 2^-9, an element) for the matrix
+ * cores; sums are float32, rounded once to grad_dtype.  A token whose gradients are
+ * all 0 (an ignored target takes g_logp as 0), or whose lse is -inf, takes no part,
+ * whatever its row of x holds, and has dx = 0.  An lse of NaN or +inf makes the
+ * token's dx and all of dw NaN.
+ *   lse         the forward's; entropy too, needed with g_entropy
+ *   dx, dw      [n_tokens] and [vocab] rows of dim elements of grad_dtype (16-byte
+ *               aligned, strides multiples of 16 bytes); either may be NULL (not
+ *               computed).  They lie apart from each other and from x and w.  With no
+ *               tokens dw is zeros
+ *   workspace   nsp_linear_logp_bwd_workspace bytes, 256-byte aligned
+ * Errors: NSP_EINVAL, NSP_EUNSUPPORTED (sizes, strides), NSP_EWORKSPACE, NSP_EHIP.
+ */
+nsp_status nsp_linear_logp_bwd(nsp_dtype grad_dtype, int64_t n_tokens, int32_t dim, int32_t vocab, const nsp_rows *x,
+                               const nsp_rows *w, const int64_t *targets, float scale, const float *lse,
+                               const float *entropy, const float *g_logp, const float *g_lse, const float *g_entropy,
+                               const nsp_rows *dx, const nsp_rows *dw, void *workspace, size_t ws_bytes,
+                               hipStream_t stream);
+
+#define NSP_DISTILL_MAX_TOP 256
+typedef enum { NSP_DISTILL_GIVEN = 0, NSP_DISTILL_NORMALIZED = 1 } nsp_distill_kind;
+
+/* Bytes of device workspace nsp_distill_fwd needs (0 for invalid sizes, and
+ * for calls of many rows, which need none); at most 520 KB. */
+size_t nsp_distill_fwd_workspace(int64_t n_tokens, int32_t vocab);
+
+/*
+ * Divergence of a row of logits from a teacher's top alternatives (Kullback and
+ * Leibler's, from the teacher's side), as nsp_token_logp_fwd gives them of
+ * the teacher's logits.  For row t, alternatives i_k = index[t][k] with log
+ * probabilities t_k = teacher_logp[t][k]:
+ *     q_k  = exp(t_k - c),  c = 0 (NSP_DISTILL_GIVEN: what the alternatives leave
+ *            of 1 counts for nothing) or log sum_k exp(t_k) (NSP_DISTILL_NORMALIZED)
+ *     lse  = log sum_v exp(z_v),  z = scale * logits[t]
+ *     loss = sum_k q_k (t_k - c - (z[i_k] - lse))
+ * An index outside 0 .. vocab - 1 or a t_k of -2^126 and below (-inf among them)
+ * is no alternative; a row without any has loss 0 and gradient 0.  An index may
+ * come more than once.  Terms with q_k = 0 are 0.  A t_k of NaN or +inf makes the
+ * row's loss and gradient NaN.  Masked logits, rows of nothing else and rows
+ * without an lse are as in nsp_token_logp_fwd: a masked logit that is an
+ * alternative (of q_k > 0) makes the loss +inf; lse NaN makes it NaN.
+ *   dtype       of the logits (NSP_BF16 or NSP_F32), rows row_stride elements apart
+ *   top         1 .. NSP_DISTILL_MAX_TOP; index int64, teacher_logp float32
+ *               [n_tokens][top], DEVICE
+ *   scale       2^-64 .. 2^64 (the student's inverse temperature; the teacher's
+ *               is in its log probabilities)
+ *   loss        float32 [n_tokens] or NULL;  lse: float32 [n_tokens], needed by
+ *               the backward
+ *   workspace   nsp_distill_fwd_workspace bytes, 256-byte aligned
+ * Errors: NSP_EINVAL, NSP_EUNSUPPORTED (vocab > 2^30, top), NSP_EWORKSPACE, NSP_EHIP.
+ */
+nsp_status nsp_distill_fwd(nsp_dtype dtype, int64_t n_tokens, int32_t vocab, const void *logits, int64_t row_stride,
+                           int32_t top, const int64_t *index, const float *teacher_logp, nsp_distill_kind kind,
+                           float scale, float *loss, float *lse, void *workspace, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * Gradient of the loss with respect to the logits, from g_loss (float32
+ * [n_tokens]; a token's weight):
+ *     dlogits_v = scale g_loss (p_v sum_k q_k - sum of the q_k with i_k = v)
+ * in float32, rounded once, with p = exp(z - lse) of the lse given.  A row with
+ * g_loss 0, without alternatives or with an lse of -inf has gradient 0, whatever its
+ * logits; another with an lse of NaN or +inf has NaN.
+ *   dlogits     rows of `vocab` elements of dtype, d_row_stride (>= vocab, unless
+ *               one row) apart; in place allowed; what lies between the rows is
+ *               left as it is
+ * Errors: NSP_EINVAL, NSP_EUNSUPPORTED (vocab, top), NSP_EHIP.
+ */
+nsp_status nsp_distill_bwd(nsp_dtype dtype, int64_t n_tokens, int32_t vocab, const void *logits, int64_t row_stride,
+                           int32_t top, const int64_t *index, const float *teacher_logp, nsp_distill_kind kind,
+                           float scale, const float *lse, const float *g_loss, void *dlogits, int64_t d_row_stride,
+                           hipStream_t stream);
+
+/*
+ * Rows of an embedding table: y[t] = scale * w[tokens[t]], in float32, rounded
+ * once to dtype; zeros for a token outside 0 .. vocab - 1.
+ *   w_dtype, dtype   of w and of y (each NSP_BF16 or NSP_F32)
+ *   n_tokens    up to 2^26; dim: 1 .. 2^20; vocab: up to 2^30
+ *   tokens      DEVICE, n_tokens int64
+ *   w           [vocab] rows of dim elements; y: [n_tokens] rows, apart from w
+ *   scale       finite
+ * Errors: NSP_EINVAL, NSP_EUNSUPPORTED (sizes), NSP_EHIP.
+ */
+nsp_status nsp_embedding_fwd(nsp_dtype w_dtype, nsp_dtype dtype, int64_t n_tokens, int32_t dim, int32_t vocab,
+                             const int64_t *tokens, const nsp_rows *w, float scale, const nsp_rows *y,
+                             hipStream_t stream);
+
+/* Bytes of device workspace nsp_embedding_bwd needs (0 for invalid sizes and
+ * no tokens): the tokens sorted by their ids (16 bytes each), a byte a table row,
+ * and float32 sums (8 dim bytes for every 8 to 128 tokens). */
+size_t nsp_embedding_bwd_workspace(int64_t n_tokens, int32_t dim, int32_t vocab);
+
+/*
+ * Gradient of the table: dw[v] = scale * sum of dy[t] over the tokens t of id v,
+ * in float32, in a fixed order (the tokens' own, in chunks), rounded once to
+ * w_dtype; every row of dw is written, those of ids without a token with zeros.
+ * dy of tokens outside the vocabulary is not read.
+ *   dy          [n_tokens] rows of dim elements of dtype;  dw: [vocab] rows of
+ *               w_dtype, apart from dy
+ *   workspace   nsp_embedding_bwd_workspace bytes, 256-byte aligned
+ * Errors: NSP_EINVAL, NSP_EUNSUPPORTED (sizes), NSP_EWORKSPACE, NSP_EHIP.
+ */
+nsp_status nsp_embedding_bwd(nsp_dtype w_dtype, nsp_dtype dtype, int64_t n_tokens, int32_t dim, int32_t vocab,
+                             const int64_t *tokens, const nsp_rows *dy, float scale, const nsp_rows *dw,
+                             void *workspace, size_t ws_bytes, hipStream_t stream);
+
+/*
  * Kernel timing (instrumentation, off by default).  While enabled, every
  * kernel this library launches is bracketed by a pair of hipEvents recorded
  * on the launch's stream, so the measured time is the device time of that
@@ -678,8 +837,9 @@ nsp_status nsp_token_logp_bwd(nsp_dtype dtype, int64_t n_tokens, int32_t vocab, 
  * into per-kernel totals and returns the launch count and total milliseconds
  * since the last nsp_timing_reset for one kernel name: "attn_fwd",
  * "bwd_preprocess", "bwd_dkdv", "bwd_dq" or "relayout", or a row operator:
- * "rotary", "norm_fwd", "norm_bwd", "token_logp_fwd" or "token_logp_bwd" (its
- * launches together).  (An attention backward runs
+ * "rotary", "norm_fwd", "norm_bwd", "token_logp_fwd", "token_logp_bwd",
+ * "linear_logp_fwd", "linear_logp_bwd", "distill_fwd", "distill_bwd",
+ * "embedding_fwd" or "embedding_bwd" (its launches together).  (An attention backward runs
  * "bwd_preprocess", "bwd_dkdv" with the sums of a split pass, "bwd_dq"; lists of
  * shorter items "bwd_dq", which takes in the preprocess, then "bwd_dkdv"; small
  * lists "bwd_preprocess", then both passes in one launch, counted as "bwd_dkdv".)

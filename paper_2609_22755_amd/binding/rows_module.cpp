@@ -1,5 +1,6 @@
-// The row operators' calls (rotary positions, norms of rows, token log
-// probabilities) on torch tensors, as functions of a Python module.
+// The calls on rows (rotary positions, norms of rows, token log probabilities,
+// embedding, log probabilities from hidden rows, distillation) on torch tensors, as
+// functions of a Python module.
 //
 // A small call's time is its binding's: looked at from Python, the tensors of
 // one call cost 5 us and its ctypes arguments 2 more, where the GPU takes 4.
@@ -224,8 +225,8 @@ PyObject *launch(const char *name, const Place &at, PyObject *stream, F call) {
 struct Signature {
   const char *function;
   int required, n;
-  const char *names[12];
-  PyObject *interned[12];
+  const char *names[13];
+  PyObject *interned[13];
 };
 
 void bind(const Signature &f, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames, PyObject **out) {
@@ -255,6 +256,17 @@ Signature k_logp_fwd = {"nsp_token_logp_fwd", 4, 10,
                         {"logits", "targets", "logp", "lse", "entropy", "top_logp", "top_index", "workspace", "scale", "stream"}, {}};
 Signature k_logp_bwd = {"nsp_token_logp_bwd", 4, 10,
                         {"logits", "targets", "lse", "dlogits", "g_logp", "g_entropy", "entropy", "g_lse", "scale", "stream"}, {}};
+Signature k_linear_fwd = {"nsp_linear_logp_fwd", 5, 9,
+                          {"x", "weight", "targets", "logp", "lse", "entropy", "workspace", "scale", "stream"}, {}};
+Signature k_linear_bwd = {"nsp_linear_logp_bwd", 7, 13,
+                          {"x", "weight", "targets", "lse", "dx", "dweight", "workspace", "g_logp", "g_entropy", "entropy", "g_lse", "scale", "stream"},
+                          {}};
+Signature k_distill_fwd = {"nsp_distill_fwd", 5, 9,
+                           {"logits", "index", "teacher_logp", "loss", "lse", "workspace", "kind", "scale", "stream"}, {}};
+Signature k_distill_bwd = {"nsp_distill_bwd", 6, 9,
+                           {"logits", "index", "teacher_logp", "lse", "g_loss", "dlogits", "kind", "scale", "stream"}, {}};
+Signature k_embed_fwd = {"nsp_embedding_fwd", 3, 5, {"tokens", "weight", "y", "scale", "stream"}, {}};
+Signature k_embed_bwd = {"nsp_embedding_bwd", 4, 6, {"tokens", "dy", "dweight", "workspace", "scale", "stream"}, {}};
 
 PyObject *rotary(const Signature &f, bool bwd, PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames) {
   PyObject *a[9];
@@ -407,6 +419,158 @@ PyObject *logp_bwd(PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames) {
   });
 }
 
+// A [rows, dim] tensor's sizes and type.
+struct Matrix {
+  Dims shape;
+  PyObject *dtype;
+  Matrix(PyObject *t, const char *name, const char *wanted) : dtype(dtype_of(t, name)) {
+    shape = shape_of(t);
+    if (shape.n != 2) fail(PyExc_TypeError, std::string(name) + ": " + wanted + " is needed (got " + shown(t) + ")");
+    if (shape.d[1] > INT32_MAX) fail(PyExc_ValueError, std::string(name) + ": sizes past 2^31 - 1");
+  }
+};
+
+// Hidden rows and the vocabulary's weight.
+struct LinearSizes {
+  Matrix x, w;
+  nsp_rows rx, rw;
+  LinearSizes(PyObject *tx, PyObject *tw, Place &at) : x(tx, "x", "[tokens, dim]"), w(tw, "weight", "[vocab, dim]") {
+    if (w.shape.d[1] != x.shape.d[1] || w.shape.d[0] > INT32_MAX)
+      fail(PyExc_TypeError, "weight: [vocab, " + std::to_string(x.shape.d[1]) + "] is needed (got " + shown(tw) + ")");
+    rx = rows(tx, x.shape, g_bf16, at, "x");
+    rw = rows(tw, w.shape, g_bf16, at, "weight");
+  }
+  long long tokens() const { return x.shape.d[0]; }
+  int32_t dim() const { return (int32_t)x.shape.d[1]; }
+  int32_t vocab() const { return (int32_t)w.shape.d[0]; }
+};
+
+PyObject *linear_fwd(PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames) {
+  PyObject *a[9];
+  bind(k_linear_fwd, args, nargs, kwnames, a);
+  Place at;
+  const LinearSizes z(a[0], a[1], at);
+  const long long T = z.tokens();
+  need(a[4], "lse");
+  const auto *y = static_cast<const int64_t *>(array(a[2], T, g_i64, at, "targets"));
+  auto *logp = static_cast<float *>(array(a[3], T, g_f32, at, "logp")), *lse = static_cast<float *>(array(a[4], T, g_f32, at, "lse")),
+       *ent = static_cast<float *>(array(a[5], T, g_f32, at, "entropy"));
+  const Workspace ws(a[6], at);
+  const float scale = real(a[7], 1.f);
+  return launch("nsp_linear_logp_fwd", at, a[8], [&](hipStream_t s) {
+    return nsp_linear_logp_fwd(T, z.dim(), z.vocab(), &z.rx, &z.rw, y, scale, logp, lse, ent, ws.data, ws.bytes, s);
+  });
+}
+
+PyObject *linear_bwd(PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames) {
+  PyObject *a[13];
+  bind(k_linear_bwd, args, nargs, kwnames, a);
+  Place at;
+  const LinearSizes z(a[0], a[1], at);
+  const long long T = z.tokens();
+  need(a[3], "lse");
+  const auto *y = static_cast<const int64_t *>(array(a[2], T, g_i64, at, "targets"));
+  const auto f = [&](int i) { return static_cast<const float *>(array(a[i], T, g_f32, at, k_linear_bwd.names[i])); };
+  const float *lse = f(3), *gl = f(7), *ge = f(8), *ent = f(9), *gs = f(10);
+  PyObject *gd = has(a[4]) ? dtype_of(a[4], "dx") : has(a[5]) ? dtype_of(a[5], "dweight") : g_bf16;
+  nsp_rows dx{}, dw{};
+  if (has(a[4])) dx = rows(a[4], z.x.shape, gd, at, "dx");
+  if (has(a[5])) dw = rows(a[5], z.w.shape, gd, at, "dweight");
+  const Workspace ws(a[6], at);
+  const nsp_dtype c = code(gd, "dx");
+  const float scale = real(a[11], 1.f);
+  return launch("nsp_linear_logp_bwd", at, a[12], [&](hipStream_t s) {
+    return nsp_linear_logp_bwd(c, T, z.dim(), z.vocab(), &z.rx, &z.rw, y, scale, lse, ent, gl, gs, ge, has(a[4]) ? &dx : nullptr,
+                               has(a[5]) ? &dw : nullptr, ws.data, ws.bytes, s);
+  });
+}
+
+// A teacher's alternatives: their number a token.
+long long alternatives(PyObject *index, long long T) {
+  const Matrix m(index, "index", "[tokens, top]");
+  if (m.shape.d[0] != T) fail(PyExc_TypeError, "index: [" + std::to_string(T) + ", top] is needed (got " + shown(index) + ")");
+  return m.shape.d[1];
+}
+
+PyObject *distill_fwd(PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames) {
+  PyObject *a[9];
+  bind(k_distill_fwd, args, nargs, kwnames, a);
+  const LogitSizes z(a[0]);
+  const long long T = z.shape.d[0];
+  Place at;
+  const nsp_rows x = rows(a[0], z.shape, z.dtype, at, "logits");
+  const long long k = alternatives(a[1], T);
+  need(a[2], "teacher_logp");
+  need(a[4], "lse");
+  const auto *index = static_cast<const int64_t *>(array(a[1], T * k, g_i64, at, "index"));
+  const auto *teacher = static_cast<const float *>(array(a[2], T * k, g_f32, at, "teacher_logp"));
+  auto *loss = static_cast<float *>(array(a[3], T, g_f32, at, "loss")), *lse = static_cast<float *>(array(a[4], T, g_f32, at, "lse"));
+  const Workspace ws(a[5], at);
+  const nsp_dtype c = code(z.dtype, "logits");
+  const auto kind = (nsp_distill_kind)whole(a[6], NSP_DISTILL_GIVEN, "kind");
+  const float scale = real(a[7], 1.f);
+  return launch("nsp_distill_fwd", at, a[8], [&](hipStream_t s) {
+    return nsp_distill_fwd(c, T, (int32_t)z.shape.d[1], x.data, x.token_stride, (int32_t)k, index, teacher, kind, scale, loss, lse, ws.data, ws.bytes, s);
+  });
+}
+
+PyObject *distill_bwd(PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames) {
+  PyObject *a[9];
+  bind(k_distill_bwd, args, nargs, kwnames, a);
+  const LogitSizes z(a[0]);
+  const long long T = z.shape.d[0];
+  Place at;
+  const nsp_rows x = rows(a[0], z.shape, z.dtype, at, "logits"), d = rows(a[5], z.shape, z.dtype, at, "dlogits");
+  const long long k = alternatives(a[1], T);
+  need(a[2], "teacher_logp");
+  need(a[3], "lse");
+  need(a[4], "g_loss");
+  const auto *index = static_cast<const int64_t *>(array(a[1], T * k, g_i64, at, "index"));
+  const auto f = [&](int i, long long n) { return static_cast<const float *>(array(a[i], n, g_f32, at, k_distill_bwd.names[i])); };
+  const float *teacher = f(2, T * k), *lse = f(3, T), *g = f(4, T);
+  const nsp_dtype c = code(z.dtype, "logits");
+  const auto kind = (nsp_distill_kind)whole(a[6], NSP_DISTILL_GIVEN, "kind");
+  const float scale = real(a[7], 1.f);
+  return launch("nsp_distill_bwd", at, a[8], [&](hipStream_t s) {
+    return nsp_distill_bwd(c, T, (int32_t)z.shape.d[1], x.data, x.token_stride, (int32_t)k, index, teacher, kind, scale, lse, g, d.data,
+                           d.token_stride, s);
+  });
+}
+
+// tokens, table rows, the tokens' rows
+PyObject *embedding(const Signature &f, bool bwd, PyObject *tokens, PyObject *table, PyObject *out, PyObject *workspace, PyObject *scaling,
+                    PyObject *stream) {
+  const char *const table_name = bwd ? "dweight" : "weight", *const out_name = bwd ? "dy" : "y";
+  const Matrix w(table, table_name, "[vocab, dim]"), y(out, out_name, "[tokens, dim]");
+  const long long T = y.shape.d[0];
+  if (w.shape.d[1] != y.shape.d[1] || w.shape.d[0] > INT32_MAX)
+    fail(PyExc_TypeError, std::string(table_name) + ": [vocab, " + std::to_string(y.shape.d[1]) + "] is needed (got " + shown(table) + ")");
+  Place at;
+  const nsp_rows rw = rows(table, w.shape, w.dtype, at, table_name), ry = rows(out, y.shape, y.dtype, at, out_name);
+  need(tokens, "tokens");
+  const auto *ids = static_cast<const int64_t *>(array(tokens, T, g_i64, at, "tokens"));
+  const Workspace ws(workspace, at);
+  const nsp_dtype cw = code(w.dtype, table_name), cy = code(y.dtype, out_name);
+  const float scale = real(scaling, 1.f);
+  const int32_t dim = (int32_t)w.shape.d[1], vocab = (int32_t)w.shape.d[0];
+  return launch(f.function, at, stream, [&](hipStream_t s) {
+    return bwd ? nsp_embedding_bwd(cw, cy, T, dim, vocab, ids, &ry, scale, &rw, ws.data, ws.bytes, s)
+               : nsp_embedding_fwd(cw, cy, T, dim, vocab, ids, &rw, scale, &ry, s);
+  });
+}
+
+PyObject *embed_fwd(PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames) {
+  PyObject *a[5];
+  bind(k_embed_fwd, args, nargs, kwnames, a);
+  return embedding(k_embed_fwd, false, a[0], a[1], a[2], nullptr, a[3], a[4]);
+}
+
+PyObject *embed_bwd(PyObject *const *args, Py_ssize_t nargs, PyObject *kwnames) {
+  PyObject *a[6];
+  bind(k_embed_bwd, args, nargs, kwnames, a);
+  return embedding(k_embed_bwd, true, a[0], a[2], a[1], a[3], a[4], a[5]);
+}
+
 // No C++ exception leaves the module.
 template <class F>
 PyObject *guarded(F f) {
@@ -430,6 +594,12 @@ FUNCTION(norm_fwd, norm_fwd(args, nargs, kwnames))
 FUNCTION(norm_bwd, norm_bwd(args, nargs, kwnames))
 FUNCTION(logp_fwd, logp_fwd(args, nargs, kwnames))
 FUNCTION(logp_bwd, logp_bwd(args, nargs, kwnames))
+FUNCTION(linear_fwd, linear_fwd(args, nargs, kwnames))
+FUNCTION(linear_bwd, linear_bwd(args, nargs, kwnames))
+FUNCTION(distill_fwd, distill_fwd(args, nargs, kwnames))
+FUNCTION(distill_bwd, distill_bwd(args, nargs, kwnames))
+FUNCTION(embed_fwd, embed_fwd(args, nargs, kwnames))
+FUNCTION(embed_bwd, embed_bwd(args, nargs, kwnames))
 
 #define METHOD(name, f, doc) \
   {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL | METH_KEYWORDS, doc}
@@ -457,9 +627,32 @@ PyMethodDef g_methods[] = {
            "nsp_token_logp_bwd(logits, targets, lse, dlogits, g_logp=None, g_entropy=None, entropy=None, g_lse=None, scale=1.0, stream=None)\n\n"
            "Gradient of nsp_token_logp_fwd's logp, entropy and lse (float32\n[tokens] each, or None) with respect to the logits, into dlogits (the\n"
            "logits themselves: in place)."),
+    METHOD("nsp_linear_logp_fwd", py_linear_fwd,
+           "nsp_linear_logp_fwd(x, weight, targets, logp, lse, entropy=None, workspace=None, scale=1.0, stream=None)\n\n"
+           "nsp_token_logp_fwd for logits x @ weight.T that are not stored: x bfloat16\n[tokens, dim], weight bfloat16 [vocab, dim]; targets int64 "
+           "[tokens] (outside\nthe vocabulary: ignored), logp, lse, entropy float32 [tokens].  targets with\nlogp, and entropy, may be None."),
+    METHOD("nsp_linear_logp_bwd", py_linear_bwd,
+           "nsp_linear_logp_bwd(x, weight, targets, lse, dx, dweight, workspace, g_logp=None, g_entropy=None, entropy=None, g_lse=None, scale=1.0, "
+           "stream=None)\n\n"
+           "Gradient of nsp_linear_logp_fwd's logp, entropy and lse (float32 [tokens]\neach, or None) with respect to x and weight, into dx and "
+           "dweight (both\nbfloat16 or both float32; None: not computed)."),
+    METHOD("nsp_distill_fwd", py_distill_fwd,
+           "nsp_distill_fwd(logits, index, teacher_logp, loss, lse, workspace=None, kind=NSP_DISTILL_GIVEN, scale=1.0, stream=None)\n\n"
+           "Divergence of the rows of logits [tokens, vocab] from a teacher's top\nalternatives (index int64, teacher_logp float32, [tokens, top], as\n"
+           "nsp_token_logp_fwd gives them): loss (or None) and lse, float32 [tokens]."),
+    METHOD("nsp_distill_bwd", py_distill_bwd,
+           "nsp_distill_bwd(logits, index, teacher_logp, lse, g_loss, dlogits, kind=NSP_DISTILL_GIVEN, scale=1.0, stream=None)\n\n"
+           "Gradient of nsp_distill_fwd's loss, times g_loss (float32 [tokens]), with\nrespect to the logits, into dlogits (the logits themselves: in "
+           "place)."),
+    METHOD("nsp_embedding_fwd", py_embed_fwd,
+           "nsp_embedding_fwd(tokens, weight, y, scale=1.0, stream=None)\n\n"
+           "Rows of weight [vocab, dim] of the tokens (int64 [tokens]; outside the\nvocabulary: zeros), times scale, into y [tokens, dim]."),
+    METHOD("nsp_embedding_bwd", py_embed_bwd,
+           "nsp_embedding_bwd(tokens, dy, dweight, workspace, scale=1.0, stream=None)\n\n"
+           "Gradient of nsp_embedding_fwd with respect to the table, into dweight\n[vocab, dim] (all rows are written)."),
     {nullptr, nullptr, 0, nullptr}};
 
-PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_rows", "The row operators' calls on torch tensors.", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
+PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_rows", "The calls on rows, on torch tensors.", -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
 
@@ -469,7 +662,8 @@ PyMODINIT_FUNC PyInit__rows() {
                         {&s_get_device, "get_device"}, {&s_numel, "numel"}, {&s_is_contiguous, "is_contiguous"},
                         {&s_element_size, "element_size"}, {&s_cuda_stream, "cuda_stream"}, {&s_device_index, "device_index"}})
       if (!(*p = PyUnicode_InternFromString(s))) throw Failed();
-    for (Signature *f : {&k_rotary_fwd, &k_rotary_bwd, &k_norm_fwd, &k_norm_bwd, &k_logp_fwd, &k_logp_bwd})
+    for (Signature *f : {&k_rotary_fwd, &k_rotary_bwd, &k_norm_fwd, &k_norm_bwd, &k_logp_fwd, &k_logp_bwd, &k_linear_fwd, &k_linear_bwd, &k_distill_fwd, &k_distill_bwd,
+                         &k_embed_fwd, &k_embed_bwd})
       for (int i = 0; i < f->n; ++i)
         if (!(f->interned[i] = PyUnicode_InternFromString(f->names[i]))) throw Failed();
     Ref torch(PyImport_ImportModule("torch")), nsp(PyImport_ImportModule("paper_2609_22755_amd.nsp")),

@@ -35,7 +35,7 @@ CXXFLAGS = [
 # masked scores are -inf): lets max/min skip operand canonicalisation.
 # Infinities are kept.  The row operators hand a NaN on.
 NO_NANS = "-fno-honor-nans"
-KEEP_NANS = ("rotary.hip", "norm.hip", "token_logp.hip", "row_ops.cpp")
+KEEP_NANS = ("rotary.hip", "norm.hip", "token_logp.hip", "row_ops.cpp", "linear_logp.hip", "distill.hip", "embedding.hip", "vocab_ops.cpp")
 
 
 def hipcc() -> str:

@@ -1,0 +1,552 @@
+// Log probabilities of given tokens straight from hidden rows and the
+// vocabulary's weight, and their gradients, for gfx950: the logits
+// a[t][v] = <x[t], w[v]> exist a tile at a time.
+//
+// Bound by the matrix cores: 2 T dim V operations forward, three times that
+// backward (the logits are made again, dx and dw are a product each).
+//
+// Forward: a tile of 256 vocabulary rows and up to 256 tokens.  A lane holds one
+// token of it, so the tile's maximum, sum and weighted sum of a token are made
+// in registers and leave as 16 bytes a token and tile; a second kernel joins a
+// token's tiles.
+//
+// Backward: the tokens whose gradient is not zero (ignored targets drop out) are
+// gathered into rows side by side; then, piece by piece of the vocabulary,
+//     dl = scale (k0 p + k1 p ln p + 1[target]) of the piece's logits, bf16
+//     dw[piece] = dl^T x,   dx += dl w[piece]
+// dl is rounded to bf16 (half a step, 2^-9 of each term at most, as independent
+// signs: next to the result's own rounding), which the matrix instructions take;
+// sums are float32, over pieces too.
+#include "gemm_tile.hpp"
+#include "row_common.hpp"
+#include "vocab_internal.hpp"
+
+namespace nsp {
+namespace {
+
+using tile::kAcross;
+using tile::kAlong;
+using tile::Product;
+
+constexpr float kNegInf = -__builtin_inff();
+constexpr float kNan = __builtin_nanf("");
+constexpr float kLowest = -3.402823466e38f;
+constexpr int kGroup = 8;      // neighbouring tiles of p that share q's in an L2
+
+// A tile of logits: 256 vocabulary rows, NQ tokens.
+template <int NQ>
+struct LogitTile;
+template <>
+struct LogitTile<256> { typedef Product<kAlong, kAlong, 256, 256, 2, 4> P; };
+template <>
+struct LogitTile<128> { typedef Product<kAlong, kAlong, 256, 128, 2, 4> P; };
+template <>
+struct LogitTile<64> { typedef Product<kAlong, kAlong, 256, 64, 4, 2> P; };
+template <>
+struct LogitTile<32> { typedef Product<kAlong, kAlong, 256, 32, 8, 1> P; };
+
+// Workgroups of a compute unit by what their stages leave of its LDS.
+template <class P>
+constexpr int kWavesPerSimd = P::kLds > 80 * 1024 ? 2 : 4;
+
+// The p of element i of a block, from the block's first.
+__device__ __forceinline__ int p_of(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
+
+// ----------------------------------------------------------------- forward --
+
+struct FwdTiles {
+  LinearArgs a;
+  int64_t t0;                  // first token of the panel
+  int64_t panel;
+  int n;                       // its tokens
+  int tiles_p, tiles_q;
+  float4 *part;                // [tile of p][panel]: largest, sum, weighted sum
+  float *at_target;            // [panel]
+};
+
+template <int NQ>
+__global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void linear_logp_tiles_kernel(FwdTiles f) {
+  typedef typename LogitTile<NQ>::P P;
+  __shared__ __attribute__((aligned(1024))) char smem[P::kLds];
+  int tp, tq;
+  if (!tile::place(blockIdx.x, f.tiles_p, f.tiles_q, kGroup, tp, tq)) return;
+  P x;
+  const int v0 = tp * P::NP, q0 = tq * NQ;
+  const LinearArgs &a = f.a;
+  x.run(smem, typename P::LoadP(a.w, a.w_stride, v0, a.vocab, 0, x.wave, x.lane),
+        typename P::LoadQ(a.x, a.x_stride, f.t0 + q0, f.t0 + f.n, 0, x.wave, x.lane), a.dim);
+  const int l32 = x.lane & 31, h = x.lane >> 5;
+  const float c = a.scale * kLog2e;
+  float4 *stat = (float4 *)smem;                 // [WP][NQ]
+  const int vw = v0 + x.p0();
+#pragma unroll
+  for (int q = 0; q < P::BQ; ++q) {
+    const int tok = q0 + x.q0() + 32 * q + l32;
+    if (v0 + P::NP > a.vocab) {
+#pragma unroll
+      for (int p = 0; p < P::BP; ++p)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (vw + 32 * p + p_of(i, h) >= a.vocab) x.acc[q][p][i] = kNegInf;
+    }
+    const int64_t y = a.logp && tok < f.n ? a.targets[f.t0 + tok] : -1;
+    const bool mine = y >= vw && y < vw + 32 * P::BP && y < a.vocab;
+    if (__any(mine)) {
+      const int e = mine ? (int)(y - vw) : -1;
+#pragma unroll
+      for (int p = 0; p < P::BP; ++p)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (e == 32 * p + p_of(i, h)) f.at_target[tok] = x.acc[q][p][i];
+    }
+    float m = kLowest;
+#pragma unroll
+    for (int p = 0; p < P::BP; ++p)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) m = fmaxf(m, x.acc[q][p][i]);
+    m = wave_max_halves(m);
+    float s = 0.f, u = 0.f;
+#pragma unroll
+    for (int p = 0; p < P::BP; ++p)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float d = (x.acc[q][p][i] - m) * c, e = fast_exp2(d);
+        s += e;
+        u = fmaf(e, fmaxf(d, -200.f), u);
+      }
+    s = wave_sum_halves(s);
+    u = wave_sum_halves(u);
+    if (h == 0) stat[x.wp * NQ + x.q0() + 32 * q + l32] = make_float4(m, s, u, 0.f);
+  }
+  __syncthreads();
+  const int tok = (int)threadIdx.x;
+  if (tok < NQ && q0 + tok < f.n) {
+    float4 r = stat[tok];
+#pragma unroll
+    for (int w = 1; w < P::WP; ++w) {
+      const float4 o = stat[w * NQ + tok];
+      const float m = fmaxf(r.x, o.x), dr = fmaxf((r.x - m) * c, -1e4f), dd = fmaxf((o.x - m) * c, -1e4f);
+      const float er = fast_exp2(dr), eo = fast_exp2(dd);
+      r.z = er * (r.z + dr * r.y) + eo * (o.z + dd * o.y);
+      r.y = er * r.y + eo * o.y;
+      r.x = m;
+    }
+    f.part[tp * f.panel + q0 + tok] = r;
+  }
+}
+
+// The tiles of 64 tokens a workgroup, 16 strands of tiles.
+constexpr int kJoinStrands = 16;
+__global__ __launch_bounds__(1024) void linear_logp_join_kernel(FwdTiles f) {
+  __shared__ float4 sh[kJoinStrands][64];
+  const int lane = threadIdx.x & 63, strand = threadIdx.x >> 6;
+  const int tok = (int)blockIdx.x * 64 + lane;
+  const float c = f.a.scale * kLog2e;
+  float m = kLowest, s = 0.f, u = 0.f;
+  const auto add = [&](const float4 &o) {
+    const float to = fmaxf(m, o.x), d = fmaxf((m - to) * c, -1e4f), e = fmaxf((o.x - to) * c, -1e4f);
+    const float fd = fast_exp2(d), fe = fast_exp2(e);
+    u = fd * (u + d * s) + fe * (o.z + e * o.y);
+    s = fd * s + fe * o.y;
+    m = to;
+  };
+  if (tok < f.n) {
+    int t = strand;
+    for (; t + 7 * kJoinStrands < f.tiles_p; t += 8 * kJoinStrands) {
+      float4 o[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = f.part[(t + i * kJoinStrands) * f.panel + tok];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) add(o[i]);
+    }
+    for (; t < f.tiles_p; t += kJoinStrands) add(f.part[t * f.panel + tok]);
+  }
+  sh[strand][lane] = make_float4(m, s, u, 0.f);
+  __syncthreads();
+  if (strand != 0 || tok >= f.n) return;
+  for (int w = 1; w < kJoinStrands; ++w) add(sh[w][lane]);
+  const int64_t t = f.t0 + tok;
+  const bool none = s == 0.f;                    // logits of -inf alone
+  const float log_s = log2f(s) * kLn2, top = m * f.a.scale;
+  float lse = none ? kNegInf : top + log_s;
+  const bool lost = !none && !(fabsf(lse) < -kNegInf);
+  if (lost) lse = kNan;
+  f.a.lse[t] = lse;
+  if (f.a.entropy) f.a.entropy[t] = none ? 0.f : lost ? kNan : log_s - u / s * kLn2;
+  if (f.a.logp) {
+    const int64_t y = f.a.targets[t];
+    float r = 0.f;
+    if (y >= 0 && y < f.a.vocab) {
+      const float z = f.at_target[tok];
+      r = none ? kNegInf : lost ? kNan : (z - m) * f.a.scale - log_s;
+    }
+    f.a.logp[t] = r;
+  }
+}
+
+// ---------------------------------------------------------------- backward --
+
+struct BwdTiles {
+  LinearArgs a;
+  plan::LinearBwd f;
+  int *count;                  // rows gathered
+  int *order;                  // [rows]: their tokens
+  int *place;                  // [tokens]: a token's row, -1: it has no gradient
+  float4 *coef;                // [rows]: lse, k0, k1, the target's
+  int *target;                 // [rows], -1: none
+  char *x;                     // gathered rows
+  char *dl;                    // [rows][piece]
+  float *sum_x, *sum_w;        // [split][rows][dim], [split][piece][dim]
+  int v0, n_v;                 // the piece
+  bool first, last;
+};
+
+// Which tokens have a gradient, in order, and the coefficients of their rows.
+__global__ __launch_bounds__(1024) void linear_rows_kernel(BwdTiles b) {
+  __shared__ int sums[16];
+  __shared__ int base;
+  const LinearArgs &a = b.a;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (threadIdx.x == 0) base = 0;
+  __syncthreads();
+  for (int64_t t0 = 0; t0 < a.n_tokens; t0 += 1024) {
+    const int64_t t = t0 + threadIdx.x;
+    bool some = false;
+    float lse = 0.f, k0 = 0.f, k1 = 0.f, at = 0.f;
+    int y = -1;
+    if (t < a.n_tokens) {
+      const int64_t target = a.g_logp ? a.targets[t] : -1;
+      const bool given = target >= 0 && target < a.vocab;
+      const float gl = given ? a.g_logp[t] : 0.f, gs = a.g_lse ? a.g_lse[t] : 0.f, ge = a.g_entropy ? a.g_entropy[t] : 0.f;
+      lse = a.lse_in[t];
+      some = !(lse == kNegInf || (gl == 0.f && gs == 0.f && ge == 0.f));
+      k0 = a.scale * (gs - gl - (ge != 0.f ? ge * a.entropy_in[t] : 0.f)) + (lse < -kNegInf ? 0.f : kNan);
+      k1 = -a.scale * ge * kLn2;
+      at = a.scale * gl;
+      y = given ? (int)target : -1;
+    }
+    const uint64_t in = __ballot(some);
+    const int before = __popcll(in & ((uint64_t(1) << lane) - 1));
+    if (lane == 0) sums[wave] = __popcll(in);
+    __syncthreads();
+    int at_row = base + before;
+    for (int w = 0; w < wave; ++w) at_row += sums[w];
+    if (t < a.n_tokens) b.place[t] = some ? at_row : -1;
+    if (some) {
+      b.order[at_row] = (int)t;
+      b.coef[at_row] = make_float4(lse, k0, k1, at);
+      b.target[at_row] = y;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      int n = 0;
+      for (int w = 0; w < 16; ++w) n += sums[w];
+      base += n;
+    }
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) *b.count = base;
+}
+
+// A token's hidden row to its place; dx of the others is zero.
+__global__ __launch_bounds__(256) void linear_gather_kernel(BwdTiles b) {
+  const LinearArgs &a = b.a;
+  const int wave = (int)threadIdx.x >> 6, lane = threadIdx.x & 63;
+  for (int64_t t = (int64_t)blockIdx.x * 4 + wave; t < a.n_tokens; t += (int64_t)gridDim.x * 4) {
+    const int at = b.place[t];
+    if (at >= 0) {
+      const u32x4 *from = (const u32x4 *)(a.x + 2 * t * a.x_stride);
+      u32x4 *to = (u32x4 *)(b.x + 2 * (int64_t)at * a.dim);
+      for (int i = lane; i < a.dim / 8; i += 64) to[i] = from[i];
+    } else if (a.dx) {
+      u32x4 *to = (u32x4 *)(a.dx + (a.g_f32 ? 4 : 2) * t * a.dx_stride);
+      for (int i = lane; i < a.dim / (a.g_f32 ? 4 : 8); i += 64) to[i] = u32x4{};
+    }
+  }
+}
+
+// 32 q's (one a lane pair) of 32 * NB p's, of a wave's sums, as rows of p: through
+// LDS (32 * 32 * NB elements of the wave's own), 16 bytes a lane.  put(row, byte,
+// 16 bytes) for rows below `rows`, elements below `cols`.
+template <int NB, bool F32, class Put>
+__device__ __forceinline__ void put_rows(const f32x16 *acc, char *lds, int rows, int cols, int lane_, Put put) {
+  const int lane = hidden(lane_);
+  constexpr int CH = NB * (F32 ? 8 : 4), PER = F32 ? 4 : 8;
+  const int l32 = lane & 31, h = lane >> 5;
+#pragma unroll
+  for (int mb = 0; mb < NB; ++mb)
+#pragma unroll
+    for (int gq = 0; gq < 4; ++gq) {
+      const f32x4 v = {acc[mb][4 * gq], acc[mb][4 * gq + 1], acc[mb][4 * gq + 2], acc[mb][4 * gq + 3]};
+      const int c = F32 ? 8 * mb + 2 * gq + h : 4 * mb + gq;
+      char *p = lds + 16 * (l32 * CH + (c ^ (l32 & (CH - 1))));
+      if constexpr (F32) *(f32x4 *)p = v;
+      else *(bf16x4 *)(p + 8 * h) = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
+    }
+#pragma unroll
+  for (int j = 0; j < CH / 2; ++j) {
+    const int row = (64 * j + lane) / CH, c = (64 * j + lane) % CH;
+    const f32x4 v = *(const f32x4 *)(lds + 16 * (row * CH + (c ^ (row & (CH - 1)))));
+    if (row < rows && c * PER < cols) put(row, 16 * c, v);
+  }
+}
+
+// dl of a piece.
+template <int NQ>
+__global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void linear_dl_kernel(BwdTiles b, int tiles_p) {
+  typedef typename LogitTile<NQ>::P P;
+  static_assert(P::kLds >= 512 * 32 * P::BP, "room for the rows that are stored");
+  __shared__ __attribute__((aligned(1024))) char smem[P::kLds];
+  const int n = *b.count;
+  int tp, tq;
+  if (!tile::place(blockIdx.x, tiles_p, (n + NQ - 1) / NQ, kGroup, tp, tq)) return;
+  P x;
+  const int v0 = tp * P::NP, q0 = tq * NQ;     // (of the piece)
+  const LinearArgs &a = b.a;
+  x.run(smem, typename P::LoadP(a.w, a.w_stride, b.v0 + v0, b.v0 + b.n_v, 0, x.wave, x.lane),
+        typename P::LoadQ(b.x, a.dim, q0, n, 0, x.wave, x.lane), a.dim);
+  const int l32 = x.lane & 31, h = x.lane >> 5;
+  const int vw = v0 + x.p0();
+#pragma unroll
+  for (int q = 0; q < P::BQ; ++q) {
+    const int r0 = q0 + x.q0() + 32 * q, r = r0 + l32;
+    const bool there = r < n;
+    const float4 k = there ? b.coef[r] : make_float4(0.f, 0.f, 0.f, 0.f);
+    const int y = there ? b.target[r] - b.v0 - vw : -1;
+#pragma unroll
+    for (int p = 0; p < P::BP; ++p)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const float d = (x.acc[q][p][i] * a.scale - k.x) * kLog2e;
+        float g = fast_exp2(fminf(d, 0.f)) * (k.y + k.z * fmaxf(d, -200.f));
+        const int e = 32 * p + p_of(i, h);
+        if (e == y) g += k.w;
+        x.acc[q][p][i] = there && vw + e < b.n_v ? g : 0.f;
+      }
+    char *out = b.dl + 2 * ((int64_t)r0 * b.f.piece + vw);
+    put_rows<P::BP, false>(x.acc[q], smem + x.wave * (2048 * P::BP), 32, 32 * P::BP, x.lane,
+                           [&](int row, int byte, f32x4 v) { *(f32x4 *)(out + (int64_t)row * 2 * b.f.piece + byte) = v; });
+  }
+}
+
+// Where a product's rows go.
+enum Out { kBf16, kF32, kSums };
+
+// Sums of one part: [rows][dim] of its own, added to with a piece after the first.
+template <class P, Out OUT, class Row>
+__device__ __forceinline__ void put_product(P &x, char *smem, int p0, int q_base, int n_q, int dim, bool add, Row row_of) {
+  static_assert(P::kLds >= P::NW * 4096 * P::BP, "room for the rows that are stored");
+#pragma unroll
+  for (int q = 0; q < P::BQ; ++q) {
+    const int r0 = q_base + x.q0() + 32 * q, pw = p0 + x.p0();
+    put_rows<P::BP, OUT != kBf16>(x.acc[q], smem + x.wave * (4096 * P::BP), n_q - r0, dim - pw, x.lane, [&](int row, int byte, f32x4 v) {
+      char *to = row_of(r0 + row) + (int64_t)pw * (OUT == kBf16 ? 2 : 4) + byte;
+      if constexpr (OUT == kSums) {
+        if (add) {
+          const f32x4 o = *(const f32x4 *)to;
+          v += o;
+        }
+      }
+      *(f32x4 *)to = v;
+    });
+  }
+}
+
+// dx of a piece: p: columns, q: gathered rows, k: the piece's vocabulary rows.
+template <int NQ>
+struct DxTile;
+template <>
+struct DxTile<256> { typedef Product<kAcross, kAlong, 256, 256, 2, 4> P; };
+template <>
+struct DxTile<64> { typedef Product<kAcross, kAlong, 256, 64, 4, 2> P; };
+
+template <int NQ, Out OUT>
+__global__ __launch_bounds__(512, kWavesPerSimd<typename DxTile<NQ>::P>) void linear_dx_kernel(BwdTiles b, int tiles_p) {
+  typedef typename DxTile<NQ>::P P;
+  __shared__ __attribute__((aligned(1024))) char smem[P::kLds];
+  const int n = *b.count;
+  int tp, tq;
+  if (!tile::place(blockIdx.x, tiles_p, (n + NQ - 1) / NQ, kGroup, tp, tq)) return;
+  P x;
+  const int part = blockIdx.y;
+  const int len = (int)plan::round_up(plan::ceil_div(b.f.piece, b.f.split_x), tile::kStep);
+  const int k0 = part * len, n_k = max(0, min(b.n_v - k0, len));
+  const int p0 = tp * P::NP, q0 = tq * NQ, dim = b.a.dim;
+  x.run(smem, typename P::LoadP(b.a.w, b.a.w_stride, p0, dim, b.v0 + k0, x.wave, x.lane),
+        typename P::LoadQ(b.dl, b.f.piece, q0, n, k0, x.wave, x.lane), n_k);
+  if constexpr (OUT == kSums) {
+    float *sums = b.sum_x + (int64_t)part * b.f.rows * dim;
+    put_product<P, OUT>(x, smem, p0, q0, n, dim, !b.first, [&](int r) { return (char *)(sums + (int64_t)r * dim); });
+  } else {
+    put_product<P, OUT>(x, smem, p0, q0, n, dim, false,
+                        [&](int r) { return b.a.dx + (int64_t)b.order[r] * b.a.dx_stride * (OUT == kF32 ? 4 : 2); });
+  }
+}
+
+// dw of a piece: p: columns, q: the piece's vocabulary rows, k: gathered rows.
+typedef Product<kAcross, kAcross, 256, 256, 2, 4> DwTile;
+template <Out OUT>
+__global__ __launch_bounds__(512, 2) void linear_dw_kernel(BwdTiles b, int tiles_p) {
+  typedef DwTile P;
+  __shared__ __attribute__((aligned(1024))) char smem[P::kLds];
+  int tp, tq;
+  if (!tile::place(blockIdx.x, tiles_p, (int)plan::ceil_div(b.n_v, P::NQ), kGroup, tp, tq)) return;
+  P x;
+  const int n = *b.count, part = blockIdx.y;
+  const int len = (int)plan::round_up(plan::ceil_div(n, b.f.split_w), tile::kStep);
+  const int k0 = part * len, n_k = max(0, min(n - k0, len));
+  const int p0 = tp * P::NP, q0 = tq * P::NQ, dim = b.a.dim;
+  x.run(smem, P::LoadP(b.x, dim, p0, dim, k0, x.wave, x.lane), P::LoadQ(b.dl, b.f.piece, q0, b.n_v, k0, x.wave, x.lane), n_k);
+  if constexpr (OUT == kSums) {
+    float *sums = b.sum_w + (int64_t)part * b.f.piece * dim;
+    put_product<P, OUT>(x, smem, p0, q0, b.n_v, dim, false, [&](int r) { return (char *)(sums + (int64_t)r * dim); });
+  } else {
+    put_product<P, OUT>(x, smem, p0, q0, b.n_v, dim, false,
+                        [&](int r) { return b.a.dw + (int64_t)(b.v0 + r) * b.a.dw_stride * (OUT == kF32 ? 4 : 2); });
+  }
+}
+
+// The parts' sums, in order, as rows of the gradient.
+template <bool F32, bool DX>
+__global__ __launch_bounds__(256) void linear_sums_kernel(BwdTiles b) {
+  const int rows = DX ? *b.count : b.n_v, dim = b.a.dim, parts = DX ? b.f.split_x : b.f.split_w;
+  const int64_t per = (DX ? b.f.rows : (int64_t)b.f.piece) * dim;
+  const float *sums = DX ? b.sum_x : b.sum_w;
+  const int vecs = dim / 8;
+  const int64_t n = (int64_t)rows * vecs;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int r = (int)(i / vecs), c = (int)(i - (int64_t)r * vecs) * 8;
+    const float *from = sums + (int64_t)r * dim + c;
+    f32x4 lo = *(const f32x4 *)from, hi = *(const f32x4 *)(from + 4);
+    for (int p = 1; p < parts; ++p) {
+      lo += *(const f32x4 *)(from + p * per);
+      hi += *(const f32x4 *)(from + p * per + 4);
+    }
+    char *row = DX ? b.a.dx + (int64_t)b.order[r] * b.a.dx_stride * (F32 ? 4 : 2) : b.a.dw + (int64_t)(b.v0 + r) * b.a.dw_stride * (F32 ? 4 : 2);
+    if constexpr (F32) {
+      *(f32x4 *)(row + 4 * c) = lo;
+      *(f32x4 *)(row + 4 * c + 16) = hi;
+    } else {
+      const u32x4 v = {pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3])};
+      *(u32x4 *)(row + 2 * c) = v;
+    }
+  }
+}
+
+// dw of no tokens.
+__global__ __launch_bounds__(256) void linear_zero_kernel(char *dw, int64_t row_bytes, int vecs, int vocab) {
+  for (int v = (int)blockIdx.x; v < vocab; v += (int)gridDim.x)
+    for (int i = (int)threadIdx.x; i < vecs; i += 256) *(u32x4 *)(dw + v * row_bytes + 16 * i) = u32x4{};
+}
+
+// Workgroups of `tiles` tiles: as many for each XCD.
+int grid_of(int64_t tiles) { return (int)plan::round_up(tiles, kXcdQueues); }
+
+template <int NQ>
+hipError_t fwd_tiles(const FwdTiles &f, hipStream_t s) {
+  linear_logp_tiles_kernel<NQ><<<grid_of((int64_t)f.tiles_p * f.tiles_q), 512, 0, s>>>(f);
+  return hipGetLastError();
+}
+
+template <int NQ>
+hipError_t dl_tiles(const BwdTiles &b, hipStream_t s) {
+  const int tiles_p = (int)plan::ceil_div(b.n_v, plan::kTileP);
+  linear_dl_kernel<NQ><<<grid_of(tiles_p * (b.f.rows / NQ)), 512, 0, s>>>(b, tiles_p);
+  return hipGetLastError();
+}
+
+template <int NQ>
+hipError_t dx_tiles(const BwdTiles &b, bool sums, hipStream_t s) {
+  const int tiles_p = (int)plan::ceil_div(b.a.dim, plan::kTileP);
+  const dim3 grid(grid_of(tiles_p * plan::ceil_div(b.f.rows, NQ)), b.f.split_x);
+  if (sums) linear_dx_kernel<NQ, kSums><<<grid, 512, 0, s>>>(b, tiles_p);
+  else if (b.a.g_f32) linear_dx_kernel<NQ, kF32><<<grid, 512, 0, s>>>(b, tiles_p);
+  else linear_dx_kernel<NQ, kBf16><<<grid, 512, 0, s>>>(b, tiles_p);
+  return hipGetLastError();
+}
+
+hipError_t dw_tiles(const BwdTiles &b, hipStream_t s) {
+  const int tiles_p = (int)plan::ceil_div(b.a.dim, plan::kTileP);
+  const dim3 grid(grid_of(tiles_p * plan::ceil_div(b.n_v, DwTile::NQ)), b.f.split_w);
+  if (b.f.split_w > 1) linear_dw_kernel<kSums><<<grid, 512, 0, s>>>(b, tiles_p);
+  else if (b.a.g_f32) linear_dw_kernel<kF32><<<grid, 512, 0, s>>>(b, tiles_p);
+  else linear_dw_kernel<kBf16><<<grid, 512, 0, s>>>(b, tiles_p);
+  return hipGetLastError();
+}
+
+template <bool DX>
+hipError_t join_sums(const BwdTiles &b, hipStream_t s) {
+  const int64_t vecs = (DX ? b.f.rows : (int64_t)b.n_v) * (b.a.dim / 8);
+  const int64_t want = plan::ceil_div(vecs, 256);
+  const int grid = (int)(want < 8192 ? want : 8192);
+  if (b.a.g_f32) linear_sums_kernel<true, DX><<<grid, 256, 0, s>>>(b);
+  else linear_sums_kernel<false, DX><<<grid, 256, 0, s>>>(b);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_linear_logp_fwd(const LinearArgs &a, hipStream_t s) {
+  const plan::LinearFwd p = plan::linear_fwd(a.n_tokens, a.vocab);
+  FwdTiles f{};
+  f.a = a;
+  f.panel = p.panel;
+  f.tiles_p = (int)p.tiles_p;
+  f.part = (float4 *)(a.ws + p.part_off);
+  f.at_target = (float *)(a.ws + p.target_off);
+  for (int64_t t0 = 0; t0 < a.n_tokens; t0 += p.panel) {
+    f.t0 = t0;
+    f.n = (int)(a.n_tokens - t0 < p.panel ? a.n_tokens - t0 : p.panel);
+    f.tiles_q = (int)plan::ceil_div(f.n, p.tile);
+    hipError_t e = p.tile == 32 ? fwd_tiles<32>(f, s) : p.tile == 64 ? fwd_tiles<64>(f, s) : p.tile == 128 ? fwd_tiles<128>(f, s) : fwd_tiles<256>(f, s);
+    if (e != hipSuccess) return e;
+    linear_logp_join_kernel<<<(f.n + 63) / 64, 1024, 0, s>>>(f);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_linear_logp_bwd(const LinearArgs &a, hipStream_t s) {
+  if (a.n_tokens == 0) {
+    if (!a.dw) return hipSuccess;
+    const int es = a.g_f32 ? 4 : 2;
+    linear_zero_kernel<<<a.vocab < 65536 ? a.vocab : 65536, 256, 0, s>>>(a.dw, a.dw_stride * es, a.dim * es / 16, a.vocab);
+    return hipGetLastError();
+  }
+  BwdTiles b{};
+  b.a = a;
+  b.f = plan::linear_bwd(a.n_tokens, a.dim, a.vocab);
+  b.count = (int *)(a.ws + b.f.count_off);
+  b.order = (int *)(a.ws + b.f.order_off);
+  b.place = (int *)(a.ws + b.f.place_off);
+  b.coef = (float4 *)(a.ws + b.f.coef_off);
+  b.target = (int *)(a.ws + b.f.target_off);
+  b.x = a.ws + b.f.x_off;
+  b.dl = a.ws + b.f.dl_off;
+  b.sum_x = (float *)(a.ws + b.f.sum_x_off);
+  b.sum_w = (float *)(a.ws + b.f.sum_w_off);
+  linear_rows_kernel<<<1, 1024, 0, s>>>(b);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t groups = plan::ceil_div(a.n_tokens, 4);
+  linear_gather_kernel<<<(int)(groups < 65536 ? groups : 65536), 256, 0, s>>>(b);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const bool sums = b.f.pieces > 1 || b.f.split_x > 1;
+  for (int p = 0; p < b.f.pieces; ++p) {
+    b.v0 = p * b.f.piece;
+    b.n_v = a.vocab - b.v0 < b.f.piece ? a.vocab - b.v0 : b.f.piece;
+    b.first = p == 0;
+    b.last = p == b.f.pieces - 1;
+    e = b.f.tile == 32 ? dl_tiles<32>(b, s) : b.f.tile == 64 ? dl_tiles<64>(b, s) : b.f.tile == 128 ? dl_tiles<128>(b, s) : dl_tiles<256>(b, s);
+    if (e == hipSuccess && a.dw) e = dw_tiles(b, s);
+    if (e == hipSuccess && a.dw && b.f.split_w > 1) e = join_sums<false>(b, s);
+    if (e == hipSuccess && a.dx) e = b.f.tile <= 64 ? dx_tiles<64>(b, sums, s) : dx_tiles<256>(b, sums, s);
+    if (e == hipSuccess && a.dx && b.last && sums) e = join_sums<true>(b, s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+}  // namespace nsp

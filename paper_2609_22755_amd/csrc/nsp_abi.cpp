@@ -1209,7 +1209,8 @@ using nsp::K_DQ;
 using nsp::K_RELAYOUT;
 const char *const kKernelNames[] = {"attn_fwd", "bwd_preprocess", "bwd_dkdv",      "bwd_dq",
                                     "relayout", "rotary",         "norm_fwd",      "norm_bwd",
-                                    "token_logp_fwd", "token_logp_bwd"};
+                                    "token_logp_fwd", "token_logp_bwd", "linear_logp_fwd", "linear_logp_bwd",
+                                    "distill_fwd", "distill_bwd", "embedding_fwd", "embedding_bwd"};
 static_assert(sizeof(kKernelNames) / sizeof(kKernelNames[0]) == kNumKernels, "a name for every kernel");
 
 struct TimingState {

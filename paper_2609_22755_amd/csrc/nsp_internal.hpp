@@ -148,7 +148,8 @@ int32_t set_error(int32_t status, const char *fmt, ...);
 
 // Kernels by the names of nsp_timing_query.
 enum KernelId {
-  K_FWD = 0, K_PRE, K_DKDV, K_DQ, K_RELAYOUT, K_ROTARY, K_NORM_FWD, K_NORM_BWD, K_LOGP_FWD, K_LOGP_BWD, kNumKernels
+  K_FWD = 0, K_PRE, K_DKDV, K_DQ, K_RELAYOUT, K_ROTARY, K_NORM_FWD, K_NORM_BWD, K_LOGP_FWD, K_LOGP_BWD,
+  K_LINEAR_FWD, K_LINEAR_BWD, K_DISTILL_FWD, K_DISTILL_BWD, K_EMBED_FWD, K_EMBED_BWD, kNumKernels
 };
 
 // launch(ctx) on `stream`, bracketed by timing events when timing is on.

@@ -1,0 +1,138 @@
+// How the vocabulary's operators divide their work: tiles, pieces and parts.
+// Rules of the host, without HIP, on sizes and types alone.
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+
+namespace nsp {
+namespace plan {
+
+constexpr int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
+constexpr size_t pad256(size_t x) { return (x + 255) & ~size_t(255); }
+
+// ----------------------------------- log probabilities from hidden rows --
+
+constexpr int64_t kLinearMaxTokens = 1 << 22;
+constexpr int kLinearMaxDim = 1 << 16, kLinearMaxVocab = 1 << 24;
+constexpr int64_t kLinearMaxStride = 1 << 20;   // offsets within a tile stay below 2^31 bytes
+constexpr int kTileP = 256;                     // vocabulary rows, or columns of a gradient, of a tile
+
+// Tokens of a tile of logits.
+constexpr int linear_tile(int64_t n_tokens) { return n_tokens <= 32 ? 32 : n_tokens <= 64 ? 64 : n_tokens <= 128 ? 128 : 256; }
+
+// Tokens of the forward that are worked on together: their statistics per tile
+// of the vocabulary (16 bytes) stay below some hundred MB.
+constexpr int64_t kLinearPanel = 32768;
+
+struct LinearFwd {
+  int tile;
+  int64_t panel;               // tokens, a multiple of the tile or all of them
+  int64_t tiles_p;
+  size_t part_off, target_off, bytes;
+};
+constexpr LinearFwd linear_fwd(int64_t n_tokens, int vocab) {
+  LinearFwd f{};
+  f.tile = linear_tile(n_tokens);
+  f.panel = n_tokens < kLinearPanel ? round_up(n_tokens, f.tile) : kLinearPanel;
+  f.tiles_p = ceil_div(vocab, kTileP);
+  f.part_off = 0;
+  f.target_off = pad256((size_t)f.tiles_p * f.panel * 16);
+  f.bytes = f.target_off + pad256((size_t)f.panel * 4);
+  return f;
+}
+
+// Compute units that a product's tiles should keep busy.
+constexpr int kUnits = 256;
+// Parts of a product's sums over k, where its tiles are too few: of 512 k at least.
+constexpr int linear_split(int64_t tiles, int64_t n_k) {
+  int64_t s = tiles > 0 ? kUnits / tiles : 1;
+  const int64_t most = n_k / 512;
+  s = s < most ? s : most;
+  return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+}
+
+struct LinearBwd {
+  int tile;                    // tokens of a tile
+  int64_t rows;                // tokens, in whole tiles
+  int piece;                   // vocabulary rows of a piece, in whole tiles
+  int pieces;
+  int split_x, split_w;        // parts of dx's and dw's sums
+  size_t count_off, order_off, place_off, coef_off, target_off, x_off, dl_off, sum_x_off, sum_w_off, bytes;
+};
+// The gradient of the logits is kept for one piece of the vocabulary at a time,
+// some 2^28 elements of it (512 MB): large enough that adding dx's float32 sums
+// of one piece to the next costs little (a read and a write of T dim against
+// 6 T dim piece operations: 2% at pieces of 32768).
+constexpr LinearBwd linear_bwd(int64_t n_tokens, int dim, int vocab) {
+  LinearBwd f{};
+  f.tile = linear_tile(n_tokens);
+  f.rows = round_up(n_tokens, f.tile);
+  const int64_t all = round_up(vocab, kTileP);
+  int64_t piece = (int64_t(1) << 28) / (f.rows > 0 ? f.rows : 1) / kTileP * kTileP;
+  piece = piece < 4096 ? 4096 : piece;
+  f.pieces = (int)(piece >= all ? 1 : ceil_div(all, piece));
+  f.piece = (int)round_up(ceil_div(all, f.pieces), kTileP);
+  f.pieces = (int)ceil_div(all, f.piece);
+  const int64_t cols = ceil_div(dim, kTileP);
+  f.split_x = linear_split(cols * (f.rows / f.tile), f.piece);
+  f.split_w = linear_split(cols * (f.piece / kTileP), n_tokens);
+  size_t at = 0;
+  f.count_off = at, at += 256;
+  f.order_off = at, at += pad256((size_t)f.rows * 4);
+  f.place_off = at, at += pad256((size_t)f.rows * 4);
+  f.coef_off = at, at += pad256((size_t)f.rows * 16);
+  f.target_off = at, at += pad256((size_t)f.rows * 4);
+  f.x_off = at, at += pad256((size_t)f.rows * dim * 2);
+  f.dl_off = at, at += pad256((size_t)f.rows * f.piece * 2);
+  f.sum_x_off = at;
+  if (f.pieces > 1 || f.split_x > 1) at += pad256((size_t)f.split_x * f.rows * dim * 4);
+  f.sum_w_off = at;
+  if (f.split_w > 1) at += pad256((size_t)f.split_w * f.piece * dim * 4);
+  f.bytes = n_tokens > 0 ? at : 0;
+  return f;
+}
+
+// --------------------------------------------------------------- embedding --
+
+constexpr int64_t kEmbedMaxTokens = 1 << 26;
+constexpr int kEmbedMaxVocab = 1 << 30, kEmbedMaxDim = 1 << 20;
+constexpr int kSortBlock = 4096;                // tokens that a workgroup sorts at a time
+
+struct EmbedBwd {
+  int chunk, chunks;           // sorted tokens of a chunk
+  int passes, bits;            // of the sort: digits of so many bits (a token id, or vocab for none)
+  int blocks;                  // workgroups of a pass; 1: all of it in one
+  size_t key_off[2], token_off[2], hist_off, flag_off, part_off, bytes;
+};
+// A chunk's sorted tokens are summed by one wave a strip of columns; what a
+// token's rows come to in a chunk they do not end in is kept in float32.  Longer
+// chunks keep less (two rows each), shorter ones leave more waves.
+constexpr EmbedBwd embed_bwd(int64_t n_tokens, int dim, int vocab) {
+  EmbedBwd f{};
+  if (n_tokens <= 0) return f;
+  f.chunk = 8;
+  while (f.chunk < 128 && n_tokens / (2 * f.chunk) >= 1024) f.chunk *= 2;
+  f.chunks = (int)ceil_div(n_tokens, f.chunk);
+  int width = 1;
+  while (width < 31 && (int64_t(1) << width) <= vocab) ++width;
+  f.passes = (width + 9) / 10;
+  f.bits = (width + f.passes - 1) / f.passes;
+  f.blocks = (int)ceil_div(n_tokens, kSortBlock);
+  size_t at = 0;
+  for (int i = 0; i < 2; ++i) {
+    f.key_off[i] = at, at += pad256((size_t)n_tokens * 4);
+    f.token_off[i] = at, at += pad256((size_t)n_tokens * 4);
+  }
+  f.hist_off = at;
+  if (f.blocks > 1) at += pad256(((size_t)f.blocks << f.bits) * 4);
+  f.flag_off = at, at += pad256((size_t)vocab);
+  f.part_off = at;
+  if (f.chunks > 1) at += pad256((size_t)f.chunks * 2 * dim * 4);
+  f.bytes = at;
+  return f;
+}
+
+}  // namespace plan
+}  // namespace nsp

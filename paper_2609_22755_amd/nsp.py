@@ -54,6 +54,16 @@ EXPORTED = (
     "nsp_token_logp_workspace",
     "nsp_token_logp_fwd",
     "nsp_token_logp_bwd",
+    "nsp_linear_logp_fwd_workspace",
+    "nsp_linear_logp_bwd_workspace",
+    "nsp_linear_logp_fwd",
+    "nsp_linear_logp_bwd",
+    "nsp_distill_fwd_workspace",
+    "nsp_distill_fwd",
+    "nsp_distill_bwd",
+    "nsp_embedding_fwd",
+    "nsp_embedding_bwd_workspace",
+    "nsp_embedding_bwd",
 )
 
 
@@ -208,6 +218,19 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.nsp_token_logp_fwd.restype = i32
     lib.nsp_token_logp_bwd.argtypes = [i32, i64, i32, p, i64, p, f32, p, p, p, p, p, p, i64, p]
     lib.nsp_token_logp_bwd.restype = i32
+    for name in ("nsp_linear_logp_fwd_workspace", "nsp_linear_logp_bwd_workspace", "nsp_embedding_bwd_workspace"):
+        getattr(lib, name).argtypes = [i64, i32, i32]
+        getattr(lib, name).restype = sz
+    lib.nsp_distill_fwd_workspace.argtypes = [i64, i32]
+    lib.nsp_distill_fwd_workspace.restype = sz
+    lib.nsp_linear_logp_fwd.argtypes = [i64, i32, i32, rows, rows, p, f32, p, p, p, p, sz, p]
+    lib.nsp_linear_logp_bwd.argtypes = [i32, i64, i32, i32, rows, rows, p, f32, p, p, p, p, p, rows, rows, p, sz, p]
+    lib.nsp_distill_fwd.argtypes = [i32, i64, i32, p, i64, i32, p, p, i32, f32, p, p, p, sz, p]
+    lib.nsp_distill_bwd.argtypes = [i32, i64, i32, p, i64, i32, p, p, i32, f32, p, p, p, i64, p]
+    lib.nsp_embedding_fwd.argtypes = [i32, i32, i64, i32, i32, p, rows, f32, rows, p]
+    lib.nsp_embedding_bwd.argtypes = [i32, i32, i64, i32, i32, p, rows, f32, rows, p, sz, p]
+    for name in ("nsp_linear_logp_fwd", "nsp_linear_logp_bwd", "nsp_distill_fwd", "nsp_distill_bwd", "nsp_embedding_fwd", "nsp_embedding_bwd"):
+        getattr(lib, name).restype = i32
     _lib = lib
     return lib
 
@@ -501,11 +524,34 @@ def nsp_token_logp_workspace(n_tokens: int, vocab: int, top: int = 0) -> int:
     return int(load_library().nsp_token_logp_workspace(int(n_tokens), int(vocab), int(top)))
 
 
-_ROW_CALLS = ("nsp_rotary_fwd", "nsp_rotary_bwd", "nsp_norm_fwd", "nsp_norm_bwd", "nsp_token_logp_fwd", "nsp_token_logp_bwd")
+# ------------------------------------------- the vocabulary's two ends --
+
+NSP_DISTILL_GIVEN, NSP_DISTILL_NORMALIZED = 0, 1
+NSP_DISTILL_MAX_TOP = 256
+
+
+def nsp_linear_logp_fwd_workspace(n_tokens: int, dim: int, vocab: int) -> int:
+    return int(load_library().nsp_linear_logp_fwd_workspace(int(n_tokens), int(dim), int(vocab)))
+
+
+def nsp_linear_logp_bwd_workspace(n_tokens: int, dim: int, vocab: int) -> int:
+    return int(load_library().nsp_linear_logp_bwd_workspace(int(n_tokens), int(dim), int(vocab)))
+
+
+def nsp_distill_fwd_workspace(n_tokens: int, vocab: int) -> int:
+    return int(load_library().nsp_distill_fwd_workspace(int(n_tokens), int(vocab)))
+
+
+def nsp_embedding_bwd_workspace(n_tokens: int, dim: int, vocab: int) -> int:
+    return int(load_library().nsp_embedding_bwd_workspace(int(n_tokens), int(dim), int(vocab)))
+
+
+_ROW_CALLS = ("nsp_rotary_fwd", "nsp_rotary_bwd", "nsp_norm_fwd", "nsp_norm_bwd", "nsp_token_logp_fwd", "nsp_token_logp_bwd",
+              "nsp_linear_logp_fwd", "nsp_linear_logp_bwd", "nsp_distill_fwd", "nsp_distill_bwd", "nsp_embedding_fwd", "nsp_embedding_bwd")
 
 
 def __getattr__(name):
-    """The row operators' calls, which need torch, on their first use (the
+    """The calls on rows, which need torch, on their first use (the
     planner and the schedule queries do without it)."""
     if name in _ROW_CALLS:
         from . import rows
@@ -516,6 +562,7 @@ def __getattr__(name):
 
 
 ROW_KERNELS = ("rotary", "norm_fwd", "norm_bwd", "token_logp_fwd", "token_logp_bwd")
+VOCAB_KERNELS = ("linear_logp_fwd", "linear_logp_bwd", "distill_fwd", "distill_bwd", "embedding_fwd", "embedding_bwd")
 KERNELS = ("attn_fwd", "bwd_preprocess", "bwd_dkdv", "bwd_dq", "relayout")
 
 

@@ -1,5 +1,6 @@
-"""The row operators' calls (rotary positions, norms of rows, token log
-probabilities) on torch tensors: the part of the binding that
+"""The calls on rows (rotary positions, norms of rows, token log probabilities,
+embedding, log probabilities from hidden rows, distillation) on torch tensors: the
+part of the binding that
 ``paper_2609_22755_amd.nsp`` offers under the same names, compiled
 (binding/rows_module.cpp) because a small call's time is its binding's.
 
@@ -21,7 +22,8 @@ def _current_stream(dev: int) -> int:
 raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream)
 
 try:
-    from ._rows import (nsp_norm_bwd, nsp_norm_fwd, nsp_rotary_bwd, nsp_rotary_fwd, nsp_token_logp_bwd,  # noqa: E402,F401
-                        nsp_token_logp_fwd)
+    from ._rows import (nsp_distill_bwd, nsp_distill_fwd, nsp_embedding_bwd, nsp_embedding_fwd,  # noqa: E402,F401
+                        nsp_linear_logp_bwd, nsp_linear_logp_fwd, nsp_norm_bwd, nsp_norm_fwd, nsp_rotary_bwd,
+                        nsp_rotary_fwd, nsp_token_logp_bwd, nsp_token_logp_fwd)
 except ImportError as e:
     raise ImportError(f"{e}: build it with `python -m paper_2609_22755_amd.build` (there is no non-HIP fallback)") from e
