@@ -73,8 +73,8 @@ __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void
   P x;
   const int v0 = tp * P::NP, q0 = tq * NQ;
   const LinearArgs &a = f.a;
-  x.run(smem, typename P::LoadP(a.w, a.w_stride, v0, a.vocab, 0, x.wave, x.lane),
-        typename P::LoadQ(a.x, a.x_stride, f.t0 + q0, f.t0 + f.n, 0, x.wave, x.lane), a.dim);
+  x.run(smem, typename P::LoadP(a.w, a.w_stride, v0, a.vocab, 0, a.dim, x.wave, x.lane),
+        typename P::LoadQ(a.x, a.x_stride, f.t0 + q0, f.t0 + f.n, 0, a.dim, x.wave, x.lane), a.dim);
   const int l32 = x.lane & 31, h = x.lane >> 5;
   const float c = a.scale * kLog2e;
   float4 *stat = (float4 *)smem;                 // [WP][NQ]
@@ -303,8 +303,8 @@ __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void
   P x;
   const int v0 = tp * P::NP, q0 = tq * NQ;     // (of the piece)
   const LinearArgs &a = b.a;
-  x.run(smem, typename P::LoadP(a.w, a.w_stride, b.v0 + v0, b.v0 + b.n_v, 0, x.wave, x.lane),
-        typename P::LoadQ(b.x, a.dim, q0, n, 0, x.wave, x.lane), a.dim);
+  x.run(smem, typename P::LoadP(a.w, a.w_stride, b.v0 + v0, b.v0 + b.n_v, 0, a.dim, x.wave, x.lane),
+        typename P::LoadQ(b.x, a.dim, q0, n, 0, a.dim, x.wave, x.lane), a.dim);
   const int l32 = x.lane & 31, h = x.lane >> 5;
   const int vw = v0 + x.p0();
 #pragma unroll
@@ -372,8 +372,8 @@ __global__ __launch_bounds__(512, kWavesPerSimd<typename DxTile<NQ>::P>) void li
   const int len = (int)plan::round_up(plan::ceil_div(b.f.piece, b.f.split_x), tile::kStep);
   const int k0 = part * len, n_k = max(0, min(b.n_v - k0, len));
   const int p0 = tp * P::NP, q0 = tq * NQ, dim = b.a.dim;
-  x.run(smem, typename P::LoadP(b.a.w, b.a.w_stride, p0, dim, b.v0 + k0, x.wave, x.lane),
-        typename P::LoadQ(b.dl, b.f.piece, q0, n, k0, x.wave, x.lane), n_k);
+  x.run(smem, typename P::LoadP(b.a.w, b.a.w_stride, p0, dim, b.v0 + k0, n_k, x.wave, x.lane),
+        typename P::LoadQ(b.dl, b.f.piece, q0, n, k0, n_k, x.wave, x.lane), n_k);
   if constexpr (OUT == kSums) {
     float *sums = b.sum_x + (int64_t)part * b.f.rows * dim;
     put_product<P, OUT>(x, smem, p0, q0, n, dim, !b.first, [&](int r) { return (char *)(sums + (int64_t)r * dim); });
@@ -396,7 +396,7 @@ __global__ __launch_bounds__(512, 2) void linear_dw_kernel(BwdTiles b, int tiles
   const int len = (int)plan::round_up(plan::ceil_div(n, b.f.split_w), tile::kStep);
   const int k0 = part * len, n_k = max(0, min(n - k0, len));
   const int p0 = tp * P::NP, q0 = tq * P::NQ, dim = b.a.dim;
-  x.run(smem, P::LoadP(b.x, dim, p0, dim, k0, x.wave, x.lane), P::LoadQ(b.dl, b.f.piece, q0, b.n_v, k0, x.wave, x.lane), n_k);
+  x.run(smem, P::LoadP(b.x, dim, p0, dim, k0, n_k, x.wave, x.lane), P::LoadQ(b.dl, b.f.piece, q0, b.n_v, k0, n_k, x.wave, x.lane), n_k);
   if constexpr (OUT == kSums) {
     float *sums = b.sum_w + (int64_t)part * b.f.piece * dim;
     put_product<P, OUT>(x, smem, p0, q0, b.n_v, dim, false, [&](int r) { return (char *)(sums + (int64_t)r * dim); });
