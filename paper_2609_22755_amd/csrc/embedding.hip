@@ -7,11 +7,15 @@
 //
 // Backward: the tokens are sorted by their ids, stably (counting sort, digit by
 // digit), so that a row's tokens lie side by side in their order and every sum has
-// a fixed order, without an atomic.  A wave takes a chunk of the sorted list and a
-// strip of columns, adds rows as long as the id stays the same and stores each id's
-// sum: to the table, or, where the id goes on beyond the chunk, in float32 for a
-// second kernel that adds the chunks' sums in order.  Rows of ids that no token has
-// are zeroed beside that.
+// a fixed order, without an atomic on data.  A wave takes a chunk of the sorted list
+// and a strip of columns, adds rows as long as the id stays the same and stores each
+// id's sum: to the table, or, where the id goes on beyond the chunk, in float32 for
+// a second kernel that adds the chunks' sums in order.
+//
+// The sort keeps few compute units busy and no memory; the rows of ids that no token
+// has are zeroed beside its last launch: up to 16384 tokens, which one workgroup
+// sorts in LDS, all rows (at most as many again are written), of more those that
+// the first pass left without a flag.
 #include "row_common.hpp"
 #include "vocab_internal.hpp"
 
@@ -96,23 +100,61 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(EmbedArgs a, int str
 
 // -------------------------------------------------------------------- sort --
 
-constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64, kSortRounds = plan::kSortBlock / kSortThreads;
-constexpr int kMaxBins = 1 << 10;
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kRounds = plan::kSortBlock / kSortThreads, kWholeRounds = plan::kSortWhole / kSortThreads;
+constexpr int kMaxBins = 1 << plan::kSortBits;
 
 struct SortArgs {
   const int64_t *tokens;       // the first pass reads these
   const uint32_t *key_in, *token_in;
-  uint32_t *key_out, *token_out, *hist;
-  uint8_t *flags;
-  int32_t n_tokens, vocab, blocks, shift, bits;
+  uint32_t *key_out, *token_out, *hist;   // hist: [block][digit], after them the sums
+  uint8_t *flags;              // ids that some token has; null: any may have one
+  int32_t n_tokens, vocab, blocks, passes, shift, bits;
   bool first;                  // pass
+  bool added;                  // hist holds sums over the blocks before
+  char *dw;                    // rows to be zeroed by the workgroups past the blocks
+  int64_t row_bytes;
+  int32_t row_elems, elem_bytes;
 };
 
 __device__ __forceinline__ uint32_t key_of(int64_t token, int vocab) { return token >= 0 && token < vocab ? (uint32_t)token : (uint32_t)vocab; }
 
-__device__ __forceinline__ void clear_flags(uint8_t *flags, int vocab, int first, int step) {
-  u32x4 *f = (u32x4 *)flags;                     // (whole 256 bytes)
-  for (int i = first; i < (vocab + 15) / 16; i += step) f[i] = u32x4{};
+// Rows without a token, by one of the workgroups that a sort's last launch has for
+// them: 64 neighbours a workgroup, as many lanes a row as it has vectors, so that
+// the chip writes in the order of the addresses (131072 rows of 8 KB: 6.3 TB/s, with
+// resident workgroups that step over the table 5.1; a fill of the same 6.8).  Rows
+// that lie side by side and are all zeroed go as one, 256 KB a workgroup.
+constexpr int kZeroRows = 64;
+constexpr int64_t kZeroBytes = 256 << 10;
+
+__device__ __forceinline__ void zero_rows(const SortArgs &a, int64_t group) {
+  const int64_t bytes = (int64_t)a.row_elems * a.elem_bytes;
+  if (!a.flags && a.row_bytes == bytes) {
+    const int64_t all = a.vocab * bytes, lead = min(all, (int64_t)(-(intptr_t)a.dw & 15)), vecs = (all - lead) / 16;
+    const int64_t lo = group * (kZeroBytes / 16), hi = min(vecs, lo + kZeroBytes / 16);
+    for (int64_t i = lo + threadIdx.x; i < hi; i += kSortThreads) *(u32x4 *)(a.dw + lead + 16 * i) = u32x4{};
+    if (group == 0) {
+      const int64_t tail = lead + 16 * vecs;
+      for (int64_t c = 2 * (int64_t)threadIdx.x; c < lead; c += 2 * kSortThreads) *(uint16_t *)(a.dw + c) = 0;
+      for (int64_t c = tail + 2 * (int64_t)threadIdx.x; c < all; c += 2 * kSortThreads) *(uint16_t *)(a.dw + c) = 0;
+    }
+    return;
+  }
+  const int lane = threadIdx.x & 63;
+  const int64_t v0 = group * kZeroRows;
+  uint64_t rows = __ballot(v0 + lane < a.vocab && !(a.flags && a.flags[v0 + lane]));
+  int lanes = 64;
+  while (lanes < kSortThreads && 16 * lanes < bytes) lanes *= 2;
+  const int side = (int)threadIdx.x / lanes, sides = kSortThreads / lanes, at = (int)threadIdx.x % lanes;
+  for (int i = 0; rows; ++i, rows &= rows - 1) {
+    if (i % sides != side) continue;
+    char *w = a.dw + (v0 + __builtin_ctzll(rows)) * a.row_bytes;
+    if (bytes >= 16) {                           // the last vector reaches back
+      for (int64_t c = 16 * at; c < bytes; c += 16 * lanes) *(u32x4_any *)(w + min(c, bytes - 16)) = u32x4{};
+    } else {
+      for (int64_t c = 2 * at; c < bytes; c += 2 * lanes) *(uint16_t *)(w + c) = 0;
+    }
+  }
 }
 
 // How many of a block's keys have each digit.
@@ -120,10 +162,13 @@ __global__ __launch_bounds__(kSortThreads) void embedding_count_kernel(SortArgs 
   __shared__ int bins[kMaxBins];
   const int n_bins = 1 << a.bits;
   for (int i = threadIdx.x; i < n_bins; i += kSortThreads) bins[i] = 0;
-  if (a.first) clear_flags(a.flags, a.vocab, blockIdx.x * kSortThreads + threadIdx.x, gridDim.x * kSortThreads);
+  if (a.first) {
+    u32x4 *f = (u32x4 *)a.flags;                 // (whole 256 bytes)
+    for (int i = blockIdx.x * kSortThreads + threadIdx.x; i < (a.vocab + 15) / 16; i += gridDim.x * kSortThreads) f[i] = u32x4{};
+  }
   __syncthreads();
 #pragma unroll
-  for (int r = 0; r < kSortRounds; ++r) {
+  for (int r = 0; r < kRounds; ++r) {
     const int i = blockIdx.x * plan::kSortBlock + r * kSortThreads + threadIdx.x;
     if (i < a.n_tokens) {
       const uint32_t k = a.first ? key_of(a.tokens[i], a.vocab) : a.key_in[i];
@@ -131,11 +176,30 @@ __global__ __launch_bounds__(kSortThreads) void embedding_count_kernel(SortArgs 
     }
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < n_bins; i += kSortThreads) a.hist[(int64_t)i * a.blocks + blockIdx.x] = bins[i];
+  for (int i = threadIdx.x; i < n_bins; i += kSortThreads) a.hist[((int64_t)blockIdx.x << a.bits) + i] = bins[i];
 }
 
-// The sum of the values of the threads before this one; `total`: of all.
-__device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t *sh, uint32_t &total) {
+// Each digit's counts to sums over the blocks before; a thread a digit.
+__global__ __launch_bounds__(64) void embedding_add_kernel(SortArgs a) {
+  const int bin = (int)blockIdx.x * 64 + (int)threadIdx.x;
+  if (bin >= 1 << a.bits) return;
+  uint32_t sum = 0;
+  uint32_t *at = a.hist + bin;
+  for (int b0 = 0; b0 < a.blocks; b0 += 32) {
+    uint32_t c[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) c[i] = b0 + i < a.blocks ? at[(int64_t)(b0 + i) << a.bits] : 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      if (b0 + i < a.blocks) at[(int64_t)(b0 + i) << a.bits] = sum;
+      sum += c[i];
+    }
+  }
+  at[(int64_t)a.blocks << a.bits] = sum;
+}
+
+// The sum of the values of the threads before this one.
+__device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t *sh) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint32_t up = x;
 #pragma unroll
@@ -143,41 +207,12 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t x, uint32_t *sh, uint32_
     const uint32_t o = __shfl_up(up, d);
     up += lane >= d ? o : 0;
   }
-  __syncthreads();                               // (sh may still be read)
   if (lane == 63) sh[wave] = up;
   __syncthreads();
   uint32_t before = up - x;
-  total = 0;
-  for (int w = 0; w < (int)blockDim.x / 64; ++w) {
-    const uint32_t s = sh[w];
-    before += w < wave ? s : 0;
-    total += s;
-  }
+  for (int w = 0; w < kSortWaves; ++w) before += w < wave ? sh[w] : 0;
+  __syncthreads();                               // (sh may be written again)
   return before;
-}
-
-// Counts to places: one workgroup over digits, then blocks.
-__global__ __launch_bounds__(kSortThreads) void embedding_scan_kernel(SortArgs a) {
-  __shared__ uint32_t sh[kSortWaves];
-  const int64_t n = (int64_t)a.blocks << a.bits;
-  uint32_t base = 0;
-  for (int64_t i0 = 0; i0 < n; i0 += 8 * kSortThreads) {
-    const int64_t i = i0 + 8 * (int64_t)threadIdx.x;
-    uint32_t v[8], sum = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      v[e] = i + e < n ? a.hist[i + e] : 0;
-      sum += v[e];
-    }
-    uint32_t total;
-    uint32_t at = base + sum_before(sum, sh, total);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (i + e < n) a.hist[i + e] = at;
-      at += v[e];
-    }
-    base += total;
-  }
 }
 
 // Lanes whose digit is this lane's.
@@ -192,24 +227,30 @@ __device__ __forceinline__ uint64_t alike(uint32_t digit, int bits, bool there) 
 
 // A wave's keys (in order, round by round), their ranks among the wave's keys of
 // the same digit, and the wave's counts of each digit.
+template <int R>
 struct Ranks {
-  uint32_t key[kSortRounds], token[kSortRounds], rank[kSortRounds];
+  uint32_t key[R], token[R], rank[R];
 
-  template <class Key>
-  __device__ __forceinline__ void take(uint32_t *counts, int n, int first, int shift, int bits, Key key_at) {
+  template <class C, class Key>
+  __device__ __forceinline__ void take(C *counts, int n, int first, int shift, int bits, Key key_at) {
     const int lane = threadIdx.x & 63;
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
+    for (int r = 0; r < R; ++r) {
       const int i = first + 64 * r + lane;
-      const bool there = i < n;
       key[r] = 0;
       token[r] = 0;
-      if (there) key_at(i, key[r], token[r]);
+      if (i < n) key_at(i, key[r], token[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const bool there = first + 64 * r + lane < n;
+      rank[r] = 0;
+      if (first + 64 * r >= n) continue;         // (whole waves)
       const uint32_t d = (key[r] >> shift) & ((1u << bits) - 1);
       const uint64_t m = alike(d, bits, there);
       const uint32_t have = there ? counts[d] : 0;
       rank[r] = have + __popcll(m & ((uint64_t(1) << lane) - 1));
-      if (there && (m >> lane) == 1) counts[d] = have + __popcll(m);   // the last of them
+      if (there && (m >> lane) == 1) counts[d] = (C)(have + __popcll(m));   // the last of them
       __builtin_amdgcn_wave_barrier();
     }
   }
@@ -218,11 +259,16 @@ struct Ranks {
 // The keys of a block to their places by one digit.
 __global__ __launch_bounds__(kSortThreads) void embedding_move_kernel(SortArgs a) {
   __shared__ uint32_t counts[kSortWaves][kMaxBins];
+  __shared__ uint32_t sums[2][kMaxBins], sh[kSortWaves];
+  if ((int)blockIdx.x >= a.blocks) {
+    zero_rows(a, (int)blockIdx.x - a.blocks);
+    return;
+  }
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, n_bins = 1 << a.bits;
   for (int i = threadIdx.x; i < kSortWaves * n_bins; i += kSortThreads) counts[i >> a.bits][i & (n_bins - 1)] = 0;
   __syncthreads();
-  const int first = blockIdx.x * plan::kSortBlock + wave * (64 * kSortRounds);
-  Ranks x;
+  const int first = blockIdx.x * plan::kSortBlock + wave * (64 * kRounds);
+  Ranks<kRounds> x;
   x.take(counts[wave], a.n_tokens, first, a.shift, a.bits, [&](int i, uint32_t &k, uint32_t &t) {
     if (a.first) {
       k = key_of(a.tokens[i], a.vocab);
@@ -233,65 +279,89 @@ __global__ __launch_bounds__(kSortThreads) void embedding_move_kernel(SortArgs a
       t = a.token_in[i];
     }
   });
-  __syncthreads();
-  for (int b = threadIdx.x; b < n_bins; b += kSortThreads) {
-    uint32_t at = a.hist[(int64_t)b * a.blocks + blockIdx.x];
-    for (int w = 0; w < kSortWaves; ++w) {
-      const uint32_t c = counts[w][b];
-      counts[w][b] = at;
-      at += c;
+  // Of each digit: the keys of the blocks before this one, and of all (half the
+  // threads each a half of the blocks).
+  static_assert(kSortThreads == 2 * kMaxBins, "two threads a digit");
+  const int bin = threadIdx.x % kMaxBins, half = threadIdx.x / kMaxBins;
+  uint32_t before = 0, all = 0;
+  if (a.added) {
+    if (!half && bin < n_bins) {
+      before = a.hist[((int64_t)blockIdx.x << a.bits) + bin];
+      all = a.hist[((int64_t)a.blocks << a.bits) + bin];
+    }
+  } else if (bin < n_bins) {
+    const int lo = half ? a.blocks / 2 : 0, hi = half ? a.blocks : a.blocks / 2;
+    for (int b0 = lo; b0 < hi; b0 += 16) {
+      uint32_t c[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) c[i] = b0 + i < hi ? a.hist[((int64_t)(b0 + i) << a.bits) + bin] : 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        before += b0 + i < (int)blockIdx.x ? c[i] : 0;
+        all += c[i];
+      }
     }
   }
+  if (half) sums[0][bin] = before, sums[1][bin] = all;
+  __syncthreads();
+  if (!half) before += sums[0][bin], all += sums[1][bin];
+  uint32_t at = sum_before(half ? 0 : all, sh) + before;
+  if (!half && bin < n_bins)
+    for (int w = 0; w < kSortWaves; ++w) {
+      const uint32_t c = counts[w][bin];
+      counts[w][bin] = at;
+      at += c;
+    }
   __syncthreads();
 #pragma unroll
-  for (int r = 0; r < kSortRounds; ++r) {
+  for (int r = 0; r < kRounds; ++r) {
     if (first + 64 * r + lane >= a.n_tokens) continue;
-    const uint32_t at = counts[wave][(x.key[r] >> a.shift) & (n_bins - 1)] + x.rank[r];
-    a.key_out[at] = x.key[r];
-    a.token_out[at] = x.token[r];
+    const uint32_t to = counts[wave][(x.key[r] >> a.shift) & (n_bins - 1)] + x.rank[r];
+    a.key_out[to] = x.key[r];
+    a.token_out[to] = x.token[r];
   }
 }
 
-// All passes of one block, in LDS.
-__global__ __launch_bounds__(kSortThreads) void embedding_sort_kernel(SortArgs a, int passes) {
-  __shared__ uint32_t counts[kSortWaves][kMaxBins];
-  __shared__ uint32_t keys[plan::kSortBlock], places[plan::kSortBlock], sh[kSortWaves];
+// All passes by the first workgroup, in LDS.
+template <int R>
+__global__ __launch_bounds__(kSortThreads) void embedding_sort_kernel(SortArgs a) {
+  __shared__ uint32_t keys[R * kSortThreads], places[R * kSortThreads], sh[kSortWaves];
+  __shared__ uint16_t counts[kSortWaves][kMaxBins];
+  if (blockIdx.x > 0) {
+    zero_rows(a, (int)blockIdx.x - 1);
+    return;
+  }
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, n_bins = 1 << a.bits;
-  clear_flags(a.flags, a.vocab, threadIdx.x, kSortThreads);
-  __syncthreads();
-  const int first = wave * (64 * kSortRounds);
-  for (int p = 0; p < passes; ++p) {
+  // as many rounds a wave as the tokens need
+  const int rounds = (a.n_tokens + kSortThreads - 1) / kSortThreads, first = wave * (64 * rounds);
+  const int n = min(a.n_tokens, first + 64 * rounds);
+  for (int p = 0; p < a.passes; ++p) {
     const int shift = p * a.bits;
     for (int i = threadIdx.x; i < kSortWaves * n_bins; i += kSortThreads) counts[i >> a.bits][i & (n_bins - 1)] = 0;
     __syncthreads();
-    Ranks x;
-    x.take(counts[wave], a.n_tokens, first, shift, a.bits, [&](int i, uint32_t &k, uint32_t &t) {
-      if (p == 0) {
-        k = key_of(a.tokens[i], a.vocab);
-        t = (uint32_t)i;
-        if (k < (uint32_t)a.vocab) a.flags[k] = 1;
-      } else {
-        k = keys[i];
-        t = places[i];
-      }
+    Ranks<R> x;
+    x.take(counts[wave], n, first, shift, a.bits, [&](int i, uint32_t &k, uint32_t &t) {
+      k = p == 0 ? key_of(a.tokens[i], a.vocab) : keys[i];
+      t = p == 0 ? (uint32_t)i : places[i];
     });
     __syncthreads();
-    uint32_t sum = 0, total;
-    if ((int)threadIdx.x < n_bins)
-      for (int w = 0; w < kSortWaves; ++w) sum += counts[w][threadIdx.x];
-    uint32_t at = sum_before(sum, sh, total);
-    if ((int)threadIdx.x < n_bins)
+    const int bin = threadIdx.x;
+    uint32_t sum = 0;
+    if (bin < n_bins)
+      for (int w = 0; w < kSortWaves; ++w) sum += counts[w][bin];
+    uint32_t at = sum_before(sum, sh);
+    if (bin < n_bins)
       for (int w = 0; w < kSortWaves; ++w) {
-        const uint32_t c = counts[w][threadIdx.x];
-        counts[w][threadIdx.x] = at;
+        const uint32_t c = counts[w][bin];
+        counts[w][bin] = (uint16_t)at;           // (below 16384: the last, past all, is not read)
         at += c;
       }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
-      if (first + 64 * r + lane >= a.n_tokens) continue;
+    for (int r = 0; r < R; ++r) {
+      if (first + 64 * r + lane >= n) continue;
       const uint32_t to = counts[wave][(x.key[r] >> shift) & (n_bins - 1)] + x.rank[r];
-      if (p == passes - 1) {
+      if (p == a.passes - 1) {
         a.key_out[to] = x.key[r];
         a.token_out[to] = x.token[r];
       } else {
@@ -303,24 +373,58 @@ __global__ __launch_bounds__(kSortThreads) void embedding_sort_kernel(SortArgs a
   }
 }
 
+// Rows alone, where there are no tokens.
+__global__ __launch_bounds__(kSortThreads) void embedding_zero_kernel(SortArgs a) { zero_rows(a, (int)blockIdx.x); }
+
 // ---------------------------------------------------------------- backward --
 
 struct SumArgs {
   EmbedArgs a;
   const uint32_t *key, *token;  // sorted
-  const uint8_t *flags;
   float *part;                  // [chunk][head, tail][dim]
-  int strips, sum_groups;       // strips of columns; workgroups that sum (the others zero)
+  int strips;                   // of columns
 };
 
 constexpr int kAhead = 8;       // rows of a wave in flight
 
-// A chunk's sums of a strip.
+// Float32 sums of a lane's columns, kept between the kernels.
+template <int N>
+__device__ __forceinline__ void keep(float *to, int cnt, const float (&x)[N]) {
+  typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+  if (cnt >= N) {
+#pragma unroll
+    for (int e = 0; e < N; e += 4) *(f32x4_any *)(to + e) = f32x4_any{x[e], x[e + 1], x[e + 2], x[e + 3]};
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (e < cnt) to[e] = x[e];
+  }
+}
+template <int N>
+__device__ __forceinline__ void kept(const float *from, int cnt, float (&x)[N]) {
+  typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+  if (cnt >= N) {
+#pragma unroll
+    for (int e = 0; e < N; e += 4) {
+      const f32x4_any v = *(const f32x4_any *)(from + e);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[e + i] = v[i];
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = e < cnt ? from[e] : 0.f;
+  }
+}
+
+// A chunk's sums of a strip, by a wave.
 template <class W, class Y>
-__device__ __forceinline__ void sum_chunk(const SumArgs &s, int chunk, int strip) {
+__global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs s) {
   constexpr int N = kVec<Y>;
   const EmbedArgs &a = s.a;
   const int lane = threadIdx.x & 63;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int chunk = (int)(unit / s.strips), strip = (int)(unit - (int64_t)chunk * s.strips);
+  if (chunk >= a.f.chunks) return;
   const int c0 = (strip * 64 + lane) * N;
   const int col = a.dim >= N ? min(c0, a.dim - N) : 0, cnt = a.dim >= N ? N : a.dim;
   const bool there = c0 < a.dim;
@@ -333,10 +437,7 @@ __device__ __forceinline__ void sum_chunk(const SumArgs &s, int chunk, int strip
     if (id < (uint32_t)a.vocab && there) {
       if (open || goes_on) {
         // (of a chunk that lies within one id's rows only the head is used)
-        float *to = s.part + ((int64_t)chunk * 2 + (open ? 0 : 1)) * a.dim + col;
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-          if (e < cnt) to[e] = acc[e];
+        keep(s.part + ((int64_t)chunk * 2 + (open ? 0 : 1)) * a.dim + col, cnt, acc);
       } else {
         float o[N];
 #pragma unroll
@@ -383,39 +484,15 @@ __device__ __forceinline__ void sum_chunk(const SumArgs &s, int chunk, int strip
   end(hi < a.n_tokens && s.key[hi] == id);
 }
 
+// The rows of an id that goes over several chunks: a workgroup a chunk that one
+// begins in, a wave a strip.
+constexpr int kJoinWaves = 8, kJoinAhead = 8;
 template <class W, class Y>
-__global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs s) {
-  const EmbedArgs &a = s.a;
-  const int lane = threadIdx.x & 63;
-  if ((int)blockIdx.x < s.sum_groups) {
-    const int64_t unit = (int64_t)blockIdx.x * 4 + (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int chunk = (int)(unit / s.strips), strip = (int)(unit - (int64_t)chunk * s.strips);
-    if (chunk < a.f.chunks) sum_chunk<W, Y>(s, chunk, strip);
-    return;
-  }
-  // rows without tokens
-  constexpr int N = kVec<W>;
-  const int64_t step = (int64_t)(gridDim.x - s.sum_groups) * 4;
-  for (int64_t v = (int64_t)(blockIdx.x - s.sum_groups) * 4 + (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6); v < a.vocab; v += step) {
-    if (s.flags && s.flags[v]) continue;
-    W *w = (W *)a.w.data + v * a.w.ts;
-    if (a.dim >= N) {
-      for (int c = lane * N; c < a.dim; c += 64 * N) store16(w + min(c, a.dim - N), u32x4{});
-    } else if (lane < a.dim) {
-      w[lane] = (W)0.f;
-    }
-  }
-}
-
-// The rows of an id that goes over several chunks: a workgroup a strip and chunk
-// that one begins in; its waves take the chunks in turn.
-template <class W, class Y>
-__global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs s) {
+__global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(SumArgs s) {
   constexpr int N = kVec<Y>;
-  __shared__ float sh[4][64][N + 1];
   const EmbedArgs &a = s.a;
   const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int chunk = (int)(blockIdx.x / s.strips), strip = (int)(blockIdx.x - (int64_t)chunk * s.strips);
+  const int chunk = (int)blockIdx.x;
   const int lo = chunk * a.f.chunk, hi = lo + a.f.chunk;    // (never the last chunk)
   const uint32_t id = s.key[hi - 1];
   if (id >= (uint32_t)a.vocab || s.key[hi] != id) return;
@@ -429,34 +506,29 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(SumArgs s) {
     more += run;
     all = run == 64;
   }
-  const int c0 = (strip * 64 + lane) * N;
-  const int col = a.dim >= N ? min(c0, a.dim - N) : 0, cnt = a.dim >= N ? N : a.dim;
-  const bool there = c0 < a.dim;
-  float acc[N] = {};
-  if (there) {
-    // part 0 is the tail of this chunk, part i the head of the i-th after it
-    const float *from = s.part + col;
-    const auto at = [&](int i) { return from + ((int64_t)(chunk + i) * 2 + (i == 0 ? 1 : 0)) * a.dim; };
-    for (int i0 = wave; i0 <= more; i0 += 16) {
-      float v[4][N];
+  for (int strip = wave; strip < s.strips; strip += kJoinWaves) {
+    const int c0 = (strip * 64 + lane) * N;
+    if (c0 >= a.dim) continue;
+    const int col = a.dim >= N ? min(c0, a.dim - N) : 0, cnt = a.dim >= N ? N : a.dim;
+    // the tail of this chunk, then the heads of those after it
+    const float *head = s.part + (int64_t)chunk * 2 * a.dim + col;
+    float acc[N];
+    kept(head + a.dim, cnt, acc);
+    for (int i0 = 1; i0 <= more; i0 += kJoinAhead) {
+      float v[kJoinAhead][N];
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < kJoinAhead; ++j) {
+        if (i0 + j <= more) kept(head + (int64_t)(i0 + j) * 2 * a.dim, cnt, v[j]);
+      }
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[j][e] = i0 + 4 * j <= more && e < cnt ? at(i0 + 4 * j)[e] : 0.f;
+      for (int j = 0; j < kJoinAhead; ++j)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int e = 0; e < N; ++e) acc[e] += v[j][e];
+        for (int e = 0; e < N; ++e) acc[e] += i0 + j <= more ? v[j][e] : 0.f;
     }
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[e] *= a.scale;
+    store_n<W>((W *)a.w.data + (int64_t)id * a.w.ts + col, cnt, acc);
   }
-#pragma unroll
-  for (int e = 0; e < N; ++e) sh[wave][lane][e] = acc[e];
-  __syncthreads();
-  if (wave != 0 || !there) return;
-  float o[N];
-#pragma unroll
-  for (int e = 0; e < N; ++e) o[e] = ((sh[0][lane][e] + sh[1][lane][e]) + (sh[2][lane][e] + sh[3][lane][e])) * a.scale;
-  store_n<W>((W *)a.w.data + (int64_t)id * a.w.ts + col, cnt, o);
 }
 
 template <class W, class Y>
@@ -471,32 +543,37 @@ hipError_t fwd(const EmbedArgs &a, hipStream_t s) {
 template <class W, class Y>
 hipError_t bwd(const EmbedArgs &a, hipStream_t s) {
   const plan::EmbedBwd &f = a.f;
-  const int64_t rows = plan::ceil_div(a.vocab, 4);
-  const int zero_groups = (int)(rows < 65536 ? rows : 65536);
-  SumArgs r{};
-  r.a = a;
-  if (a.n_tokens == 0) {
-    embedding_sum_kernel<W, Y><<<zero_groups, 256, 0, s>>>(r);
-    return hipGetLastError();
-  }
   SortArgs k{};
   k.tokens = a.tokens;
   k.n_tokens = a.n_tokens;
   k.vocab = a.vocab;
   k.blocks = f.blocks;
+  k.passes = f.passes;
   k.bits = f.bits;
-  k.hist = (uint32_t *)(a.ws + f.hist_off);
-  k.flags = (uint8_t *)(a.ws + f.flag_off);
+  k.dw = a.w.data;
+  k.row_bytes = a.w.ts * (int64_t)sizeof(W);
+  k.row_elems = a.dim;
+  k.elem_bytes = (int)sizeof(W);
+  const bool flags = f.blocks > 0, side_by_side = !flags && k.row_bytes == (int64_t)a.dim * (int)sizeof(W);
+  const int zero = (int)(side_by_side ? plan::ceil_div(a.vocab * k.row_bytes, kZeroBytes) : plan::ceil_div(a.vocab, kZeroRows));
+  if (a.n_tokens == 0) {
+    embedding_zero_kernel<<<zero, kSortThreads, 0, s>>>(k);
+    return hipGetLastError();
+  }
   uint32_t *const key[2] = {(uint32_t *)(a.ws + f.key_off[0]), (uint32_t *)(a.ws + f.key_off[1])};
   uint32_t *const token[2] = {(uint32_t *)(a.ws + f.token_off[0]), (uint32_t *)(a.ws + f.token_off[1])};
   int in = 0;                                    // where the sorted list ends up
   hipError_t e = hipSuccess;
-  if (f.blocks == 1) {
+  if (f.blocks == 0) {
     k.key_out = key[0];
     k.token_out = token[0];
-    embedding_sort_kernel<<<1, kSortThreads, 0, s>>>(k, f.passes);
+    if (a.n_tokens <= kRounds * kSortThreads) embedding_sort_kernel<kRounds><<<1 + zero, kSortThreads, 0, s>>>(k);
+    else if (a.n_tokens <= 2 * kRounds * kSortThreads) embedding_sort_kernel<2 * kRounds><<<1 + zero, kSortThreads, 0, s>>>(k);
+    else embedding_sort_kernel<kWholeRounds><<<1 + zero, kSortThreads, 0, s>>>(k);
     e = hipGetLastError();
   } else {
+    k.hist = (uint32_t *)(a.ws + f.hist_off);
+    k.flags = (uint8_t *)(a.ws + f.flag_off);
     for (int p = 0; p < f.passes && e == hipSuccess; ++p) {
       k.first = p == 0;
       k.shift = p * f.bits;
@@ -507,23 +584,31 @@ hipError_t bwd(const EmbedArgs &a, hipStream_t s) {
       k.token_out = token[in];
       embedding_count_kernel<<<f.blocks, kSortThreads, 0, s>>>(k);
       if ((e = hipGetLastError()) != hipSuccess) break;
-      embedding_scan_kernel<<<1, kSortThreads, 0, s>>>(k);
+      // every workgroup adds the others' counts itself, unless that would be most of its work
+      k.added = f.blocks > 128;
+      if (k.added) embedding_add_kernel<<<(1 << f.bits) / 64 + 1, 64, 0, s>>>(k);
       if ((e = hipGetLastError()) != hipSuccess) break;
-      embedding_move_kernel<<<f.blocks, kSortThreads, 0, s>>>(k);
+      // (after one pass alone the flags are not all set before its end)
+      const bool zeroes = p == f.passes - 1 && p > 0;
+      embedding_move_kernel<<<f.blocks + (zeroes ? zero : 0), kSortThreads, 0, s>>>(k);
+      e = hipGetLastError();
+    }
+    if (e == hipSuccess && f.passes == 1) {
+      embedding_zero_kernel<<<zero, kSortThreads, 0, s>>>(k);
       e = hipGetLastError();
     }
   }
   if (e != hipSuccess) return e;
+  SumArgs r{};
+  r.a = a;
   r.key = key[in];
   r.token = token[in];
-  r.flags = k.flags;
   r.part = (float *)(a.ws + f.part_off);
   r.strips = (int)plan::ceil_div(a.dim, 64 * kVec<Y>);
-  r.sum_groups = (int)plan::ceil_div((int64_t)f.chunks * r.strips, 4);
-  embedding_sum_kernel<W, Y><<<r.sum_groups + zero_groups, 256, 0, s>>>(r);
+  embedding_sum_kernel<W, Y><<<(int)plan::ceil_div((int64_t)f.chunks * r.strips, 4), 256, 0, s>>>(r);
   e = hipGetLastError();
   if (e != hipSuccess || f.chunks == 1) return e;
-  embedding_join_kernel<W, Y><<<(int)((f.chunks - 1) * (int64_t)r.strips), 256, 0, s>>>(r);
+  embedding_join_kernel<W, Y><<<f.chunks - 1, 64 * kJoinWaves, 0, s>>>(r);
   return hipGetLastError();
 }
 

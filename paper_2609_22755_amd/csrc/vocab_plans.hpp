@@ -98,36 +98,40 @@ constexpr LinearBwd linear_bwd(int64_t n_tokens, int dim, int vocab) {
 
 constexpr int64_t kEmbedMaxTokens = 1 << 26;
 constexpr int kEmbedMaxVocab = 1 << 30, kEmbedMaxDim = 1 << 20;
-constexpr int kSortBlock = 4096;                // tokens that a workgroup sorts at a time
+constexpr int kSortBlock = 4096;                // tokens that a workgroup of a pass takes
+constexpr int kSortWhole = 16384;               // tokens that one workgroup sorts by itself
+constexpr int kSortBits = 9;                    // most of a digit
 
 struct EmbedBwd {
   int chunk, chunks;           // sorted tokens of a chunk
   int passes, bits;            // of the sort: digits of so many bits (a token id, or vocab for none)
-  int blocks;                  // workgroups of a pass; 1: all of it in one
+  int blocks;                  // workgroups of a pass; 0: one workgroup sorts
   size_t key_off[2], token_off[2], hist_off, flag_off, part_off, bytes;
 };
 // A chunk's sorted tokens are summed by one wave a strip of columns; what a
 // token's rows come to in a chunk they do not end in is kept in float32.  Longer
-// chunks keep less (two rows each), shorter ones leave more waves.
+// chunks keep less (two rows each), shorter ones leave more waves; one chunk needs
+// no second kernel.
 constexpr EmbedBwd embed_bwd(int64_t n_tokens, int dim, int vocab) {
   EmbedBwd f{};
   if (n_tokens <= 0) return f;
-  f.chunk = 8;
+  f.chunk = n_tokens <= 32 ? 32 : 8;
   while (f.chunk < 128 && n_tokens / (2 * f.chunk) >= 1024) f.chunk *= 2;
   f.chunks = (int)ceil_div(n_tokens, f.chunk);
   int width = 1;
   while (width < 31 && (int64_t(1) << width) <= vocab) ++width;
-  f.passes = (width + 9) / 10;
+  f.passes = (width + kSortBits - 1) / kSortBits;
   f.bits = (width + f.passes - 1) / f.passes;
-  f.blocks = (int)ceil_div(n_tokens, kSortBlock);
+  f.blocks = n_tokens <= kSortWhole ? 0 : (int)ceil_div(n_tokens, kSortBlock);
   size_t at = 0;
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < (f.blocks ? 2 : 1); ++i) {
     f.key_off[i] = at, at += pad256((size_t)n_tokens * 4);
     f.token_off[i] = at, at += pad256((size_t)n_tokens * 4);
   }
   f.hist_off = at;
-  if (f.blocks > 1) at += pad256(((size_t)f.blocks << f.bits) * 4);
-  f.flag_off = at, at += pad256((size_t)vocab);
+  if (f.blocks) at += pad256(((size_t)(f.blocks + 1) << f.bits) * 4);
+  f.flag_off = at;
+  if (f.blocks) at += pad256((size_t)vocab);
   f.part_off = at;
   if (f.chunks > 1) at += pad256((size_t)f.chunks * 2 * dim * 4);
   f.bytes = at;

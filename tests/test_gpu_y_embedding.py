@@ -68,14 +68,15 @@ def test_rows(T, dim, V, wt, dt):
 
 @pytest.mark.parametrize("wt,dt", TYPES)
 @pytest.mark.parametrize("T,dim,V", [(1, 1, 1), (1, 8, 3), (3, 3, 2), (7, 9, 10), (8, 16, 1), (9, 16, 1), (24, 512, 1000), (100, 1111, 50), (2049, 80, 300),
-                                     (4096, 33, 70000), (4097, 33, 70000), (9000, 24, 1023), (9000, 24, 1024), (20000, 8, 3), (300000, 5, 40)])
+                                     (4096, 33, 70000), (4097, 33, 70000), (9000, 24, 1023), (9000, 24, 1024), (20000, 8, 3), (300000, 5, 40),
+                                     (16384, 16, 600), (16385, 16, 600), (17000, 12, 511), (17000, 12, 512), (30000, 9, 270000), (600001, 3, 50)])
 def test_gradient(T, dim, V, wt, dt):
     rng = np.random.default_rng(T * dim + V + 1)
     ids, dy = _ids(rng, T, V), draw(rng, (T, dim), dt)
     _check_bwd(ids, dy, V, _bwd(ids, dy, V, wt, 0.7), 0.7)
 
 
-@pytest.mark.parametrize("T", [64, 5000, 9000])
+@pytest.mark.parametrize("T", [32, 64, 5000, 17000])
 def test_long_runs_and_their_borders(T):
     """Ids whose tokens begin and end at the borders of chunks, and one of them all."""
     rng = np.random.default_rng(T)
@@ -139,7 +140,7 @@ def test_no_tokens():
     assert not dw.any()
 
 
-@pytest.mark.parametrize("T", [24, 9000])
+@pytest.mark.parametrize("T", [24, 9000, 20000])
 def test_repeats_streams_and_graphs(T):
     rng = np.random.default_rng(11)
     V = 700
