@@ -12,11 +12,12 @@
 // without its weighted one; a workgroup takes a row, or a part of one where there
 // are few, and ends it with one alternative a thread.
 //
-// Backward: a workgroup takes 16 KB of a row.  Its vectors are on their way while
-// every wave weighs the alternatives for itself (no barrier before the sums);
-// they are stored as if there were no alternatives, and after a barrier the
-// threads whose alternative lies in this part store its element anew, each token
-// once with all the weight that it has.
+// Backward: a workgroup takes 16 to 64 KB of a row, 16 KB at a time: more of them
+// weigh the alternatives more often, and stream better.  The first vectors
+// are on their way while every wave weighs the alternatives for itself (no
+// barrier before the sums); all are stored as if there were no alternatives, and
+// after a barrier the threads whose alternative lies in this part store its element
+// anew, each token once with all the weight that it has.
 #include "logit_sums.hpp"
 #include "vocab_internal.hpp"
 
@@ -194,73 +195,85 @@ __global__ __launch_bounds__(kThreads) void distill_join_kernel(DistillArgs a) {
 
 // ---------------------------------------------------------------- backward --
 
-constexpr int kBwdVecs = 4;   // vectors of a lane
+constexpr int kBwdVecs = 4;    // vectors of a lane in flight
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void distill_bwd_kernel(DistillArgs a, int chunks) {
-  constexpr int V = kVec<T>;
-  constexpr int kChunk = kThreads * V * kBwdVecs;
-  __shared__ int at[kDistillMaxTop];
-  __shared__ float q[kDistillMaxTop];
-  const int64_t units = (int64_t)a.n_tokens * chunks;
+// TURNS: times that a workgroup takes as many.
+template <class T, int TURNS>
+__global__ __launch_bounds__(kThreads) void distill_bwd_kernel(DistillArgs a, int parts) {
+  constexpr int V = kVec<T>, kTurn = kThreads * V * kBwdVecs, kPart = kTurn * TURNS;
+  __shared__ int4 at[kDistillMaxTop / 4];
+  __shared__ float4 q[kDistillMaxTop / 4];
+  static_assert(kDistillMaxTop == kThreads, "an alternative a thread");
+  const int64_t units = (int64_t)a.n_tokens * parts;
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int row = (int)(unit / chunks), chunk = (int)(unit - (int64_t)row * chunks);
+    const int row = (int)(unit / parts), part = (int)(unit - (int64_t)row * parts);
     const T *z = (const T *)a.logits + (int64_t)row * a.row_stride;
     T *dz = (T *)a.dlogits + (int64_t)row * a.d_row_stride;
     const float g = a.g_loss[row], lse = a.lse_in[row];
     const bool still = lse == kNegInf || g == 0.f;
-    const int from = chunk * kChunk, first = from + (int)threadIdx.x * V;
+    const int64_t from = (int64_t)part * kPart;
+    const int lo = (int)from, hi = (int)min((int64_t)a.vocab, from + kPart);
     u32x4 raw[kBwdVecs];
-    float edge[V] = {};
-    int ragged = -1;                            // the vector that the row ends in
+    const auto fetch = [&](int base) {             // (a row without a gradient is not read)
 #pragma unroll
-    for (int r = 0; r < kBwdVecs; ++r) {
-      const int e0 = first + r * kThreads * V;
-      if (!still && e0 + V <= a.vocab) raw[r] = load16(z + e0);
-      else if (!still && e0 < a.vocab) ragged = r;
-    }
-    if (ragged >= 0) load_some(z + first + ragged * kThreads * V, a.vocab - first - ragged * kThreads * V, kNegInf, edge);
+      for (int r = 0; r < kBwdVecs; ++r) {
+        const int e0 = base + (r * kThreads + (int)threadIdx.x) * V;
+        if (!still && e0 + V <= hi) raw[r] = load16(z + e0);
+      }
+    };
+    fetch(lo);
     const Weighed w(a, row);
     const bool zero = still || !w.any;
     const float nan = lse < -kNegInf ? 0.f : kNan, gs = a.scale * g, k0 = gs * w.sum + nan;
     const auto slope = [&](float v) {
       const float d = (v * a.scale - lse) * kLog2e;
-      return zero ? 0.f : exp2_fast(fminf(d, 0.f)) * k0;
+      return exp2_fast(fminf(d, 0.f)) * k0;
     };
     Alternative mine;
     float zk = 0.f;
+    if ((int)threadIdx.x < a.top) mine = Alternative(a, row, threadIdx.x);
+    ((int *)at)[threadIdx.x] = mine.at;
+    ((float *)q)[threadIdx.x] = mine.weight(w.c);
     if ((int)threadIdx.x < a.top) {
-      mine = Alternative(a, row, threadIdx.x);
-      at[threadIdx.x] = mine.at;
-      q[threadIdx.x] = mine.weight(w.c);
-      if (mine.at < from || mine.at >= from + kChunk || zero) mine.at = -1;
+      if (mine.at < lo || mine.at >= hi || zero) mine.at = -1;
       if (mine.at >= 0) zk = to_f32(z[mine.at]);   // (before it may be overwritten)
     }
     __syncthreads();
-#pragma unroll
-    for (int r = 0; r < kBwdVecs; ++r) {
-      const int e0 = first + r * kThreads * V;
-      if (e0 >= a.vocab) continue;
-      float v[V], o[V];
-      if (r == ragged || zero) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = edge[e];
-      } else {
-        unpack<T>(raw[r], v);
-      }
-#pragma unroll
-      for (int e = 0; e < V; ++e) o[e] = slope(v[e]);
-      store_vec(dz + e0, a.vocab - e0, o);
-    }
     float weight = 0.f;
     if (mine.at >= 0) {
-      for (int k = 0; k < a.top; ++k) {
-        if (at[k] != mine.at) continue;
-        if (k < (int)threadIdx.x) {              // the first of them stores
-          mine.at = -1;
-          break;
+      bool first = true;
+      for (int k = 0; k < a.top; k += 4) {
+        const int4 i = at[k / 4];
+        const float4 x = q[k / 4];
+        weight += i.x == mine.at ? x.x : 0.f;
+        weight += i.y == mine.at ? x.y : 0.f;
+        weight += i.z == mine.at ? x.z : 0.f;
+        weight += i.w == mine.at ? x.w : 0.f;
+        const int before = (int)threadIdx.x - k;
+        first &= !((i.x == mine.at && before > 0) || (i.y == mine.at && before > 1) || (i.z == mine.at && before > 2) ||
+                   (i.w == mine.at && before > 3));
+      }
+      if (!first) mine.at = -1;                    // the first of them stores
+    }
+    for (int base = lo; base < hi; base += kTurn) {
+      u32x4 now[kBwdVecs];
+#pragma unroll
+      for (int r = 0; r < kBwdVecs; ++r) now[r] = raw[r];
+      if (base + kTurn < hi) fetch(base + kTurn);
+#pragma unroll
+      for (int r = 0; r < kBwdVecs; ++r) {
+        const int e0 = base + (r * kThreads + (int)threadIdx.x) * V;
+        if (e0 + V <= hi) {
+          float v[V];
+          unpack<T>(now[r], v);
+#pragma unroll
+          for (int e = 0; e < V; ++e) v[e] = slope(v[e]);
+          u32x4 o = pack<T>(v);
+          if (zero) o = u32x4{};
+          store16(dz + e0, o);
+        } else if (e0 < hi) {                      // the row's end
+          for (int e = e0; e < hi; ++e) dz[e] = zero ? (T)0.f : (T)slope(to_f32(z[e]));
         }
-        weight += q[k];
       }
     }
     __syncthreads();
@@ -280,13 +293,20 @@ hipError_t fwd(DistillArgs a, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <class T, int TURNS>
+hipError_t bwd_turns(const DistillArgs &a, hipStream_t s) {
+  const int parts = (int)plan::ceil_div(a.vocab, kThreads * kVec<T> * kBwdVecs * TURNS);
+  const int64_t units = (int64_t)a.n_tokens * parts;
+  distill_bwd_kernel<T, TURNS><<<(int)(units < kMaxGrid ? units : kMaxGrid), kThreads, 0, s>>>(a, parts);
+  return hipGetLastError();
+}
+
 template <class T>
 hipError_t bwd(const DistillArgs &a, hipStream_t s) {
-  constexpr int per = kThreads * kVec<T> * kBwdVecs;
-  const int chunks = (int)(((int64_t)a.vocab + per - 1) / per);
-  const int64_t units = (int64_t)a.n_tokens * chunks;
-  distill_bwd_kernel<T><<<(int)(units < kMaxGrid ? units : kMaxGrid), kThreads, 0, s>>>(a, chunks);
-  return hipGetLastError();
+  // (us at one, two and four turns. 8192 x 131072 bf16, 8 alternatives: 679, 691, 742;
+  // 20: 700, 680, 736; 64: 760, 692, 738; 256: 1413, 878, 809.  777 x 50021 float32, 20:
+  // 55, 57, 65; 64: 59, 62, 68; 256: 108, 80, 84)
+  return a.top * kVec<T> <= 128 ? bwd_turns<T, 1>(a, s) : a.top <= 128 ? bwd_turns<T, 2>(a, s) : bwd_turns<T, 4>(a, s);
 }
 
 }  // namespace
