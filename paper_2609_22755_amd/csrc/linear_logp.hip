@@ -135,36 +135,60 @@ __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void
   }
 }
 
-// The tiles of 64 tokens a workgroup, 16 strands of tiles.
-constexpr int kJoinStrands = 16;
-__global__ __launch_bounds__(1024) void linear_logp_join_kernel(FwdTiles f) {
-  __shared__ float4 sh[kJoinStrands][64];
-  const int lane = threadIdx.x & 63, strand = threadIdx.x >> 6;
-  const int tok = (int)blockIdx.x * 64 + lane;
+// The tiles of 16 tokens a workgroup: 64 strands of tiles, joined over the four of a
+// wave, then over the waves.
+constexpr int kJoinTokens = 16, kJoinStrands = 64;
+__global__ __launch_bounds__(kJoinTokens * kJoinStrands) void linear_logp_join_kernel(FwdTiles f) {
+  constexpr int kWaves = kJoinTokens * kJoinStrands / 64;
+  __shared__ float4 sh[kWaves][kJoinTokens];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mine = lane % kJoinTokens;
+  const int tok = (int)blockIdx.x * kJoinTokens + mine, strand = threadIdx.x / kJoinTokens;
   const float c = f.a.scale * kLog2e;
   float m = kLowest, s = 0.f, u = 0.f;
-  const auto add = [&](const float4 &o) {
-    const float to = fmaxf(m, o.x), d = fmaxf((m - to) * c, -1e4f), e = fmaxf((o.x - to) * c, -1e4f);
+  const auto add = [&](float om, float os, float ou) {
+    const float to = fmaxf(m, om), d = fmaxf((m - to) * c, -1e4f), e = fmaxf((om - to) * c, -1e4f);
     const float fd = fast_exp2(d), fe = fast_exp2(e);
-    u = fd * (u + d * s) + fe * (o.z + e * o.y);
-    s = fd * s + fe * o.y;
+    u = fd * (u + d * s) + fe * (ou + e * os);
+    s = fd * s + fe * os;
     m = to;
   };
+  const auto across = [&](int lanes) {             // (both sides add the same two, the lower lanes' first)
+    const float om = __shfl_xor(m, lanes), os = __shfl_xor(s, lanes), ou = __shfl_xor(u, lanes);
+    if (lane & lanes) {
+      const float tm = m, ts = s, tu = u;
+      m = om, s = os, u = ou;
+      add(tm, ts, tu);
+    } else {
+      add(om, os, ou);
+    }
+  };
   if (tok < f.n) {
-    int t = strand;
-    for (; t + 7 * kJoinStrands < f.tiles_p; t += 8 * kJoinStrands) {
+    const float4 *part = f.part + tok;
+    for (int t = strand; t < f.tiles_p; t += 8 * kJoinStrands) {
       float4 o[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) o[i] = f.part[(t + i * kJoinStrands) * f.panel + tok];
+      for (int i = 0; i < 8; ++i) o[i] = t + i * kJoinStrands < f.tiles_p ? part[(t + i * kJoinStrands) * f.panel] : make_float4(kLowest, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) add(o[i]);
+      for (int i = 0; i < 8; ++i) add(o[i].x, o[i].y, o[i].z);
     }
-    for (; t < f.tiles_p; t += kJoinStrands) add(f.part[t * f.panel + tok]);
   }
-  sh[strand][lane] = make_float4(m, s, u, 0.f);
+  across(16);
+  across(32);
+  if (lane < kJoinTokens) sh[wave][lane] = make_float4(m, s, u, 0.f);
   __syncthreads();
-  if (strand != 0 || tok >= f.n) return;
-  for (int w = 1; w < kJoinStrands; ++w) add(sh[w][lane]);
+  if (wave != 0) return;
+  {
+    const float4 o = sh[lane / kJoinTokens * (kWaves / 4)][mine];
+    m = o.x, s = o.y, u = o.z;
+  }
+#pragma unroll
+  for (int w = 1; w < kWaves / 4; ++w) {
+    const float4 o = sh[lane / kJoinTokens * (kWaves / 4) + w][mine];
+    add(o.x, o.y, o.z);
+  }
+  across(16);
+  across(32);
+  if (lane >= kJoinTokens || tok >= f.n) return;
   const int64_t t = f.t0 + tok;
   const bool none = s == 0.f;                    // logits of -inf alone
   const float log_s = log2f(s) * kLn2, top = m * f.a.scale;
@@ -500,7 +524,7 @@ hipError_t launch_linear_logp_fwd(const LinearArgs &a, hipStream_t s) {
     f.tiles_q = (int)plan::ceil_div(f.n, p.tile);
     hipError_t e = p.tile == 32 ? fwd_tiles<32>(f, s) : p.tile == 64 ? fwd_tiles<64>(f, s) : p.tile == 128 ? fwd_tiles<128>(f, s) : fwd_tiles<256>(f, s);
     if (e != hipSuccess) return e;
-    linear_logp_join_kernel<<<(f.n + 63) / 64, 1024, 0, s>>>(f);
+    linear_logp_join_kernel<<<(f.n + kJoinTokens - 1) / kJoinTokens, kJoinTokens * kJoinStrands, 0, s>>>(f);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
