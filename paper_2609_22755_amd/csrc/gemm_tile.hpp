@@ -22,6 +22,7 @@
 #pragma once
 
 #include <type_traits>
+#include <utility>
 
 #include "device_common.hpp"
 
@@ -36,6 +37,16 @@ constexpr int kRingP = 3, kRingQ = 2;
 constexpr unsigned kOutside = 0x80000000u;
 
 enum Lie { kAlong, kAcross };
+
+// f(0), ..., f(N - 1), as constants.
+template <int... I, class F>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F f) {
+  (f(std::integral_constant<int, I>()), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void static_for(F f) {
+  each_of(std::make_integer_sequence<int, N>(), f);
+}
 
 // One stage of an operand of N rows or columns.
 template <Lie LIE, int N>
@@ -176,19 +187,40 @@ struct Product {
       for (int p = 0; p < BP; ++p) acc[q][p] = f32x16{};
     const auto at_p = [&](int stage) { return smem + stage % kRingP * kBytesP; };
     const auto at_q = [&](int stage) { return smem + kAtQ + stage % kRingQ * kBytesQ; };
-    const auto read = [&](Operands &x, int stage, int kb) {
+    const auto read_q = [&](Operands &x, int stage, int kb) {
 #pragma unroll
       for (int q = 0; q < BQ; ++q) x.q[q] = rq.operand(smem, kb, q, stage % kRingQ * kBytesQ);
+    };
+    const auto read_p = [&](Operands &x, int stage, int kb) {
 #pragma unroll
       for (int p = 0; p < BP; ++p) x.p[p] = rp.operand(smem, kb, p, stage % kRingP * kBytesP);
-      __builtin_amdgcn_sched_barrier(0);
     };
-    const auto multiply = [&](const Operands &x) {
+    // The products of x, with the next block's operands (block kb of `stage`) read
+    // into `next` behind the first of them and `loads` direct loads, one behind each of
+    // the following: what they take to issue hides behind a product.
+    const auto block = [&](const Operands &x, Operands &next, int stage, int kb, auto loads, auto load) {
 #pragma unroll
       for (int p = 0; p < BP; ++p)
 #pragma unroll
-        for (int q = 0; q < BQ; ++q) acc[q][p] = mfma32x32x16(x.p[p], x.q[q], acc[q][p]);
-      __builtin_amdgcn_sched_barrier(0);
+        for (int q = 0; q < BQ; ++q) {
+          constexpr int kProducts = BP * BQ, kLoads = decltype(loads)::value;
+          const int i = p * BQ + q;
+          acc[q][p] = mfma32x32x16(x.p[p], x.q[q], acc[q][p]);
+          if (i == 0) {
+            read_q(next, stage, kb);
+            read_p(next, stage, kb);
+          }
+          if constexpr (kLoads > 0) {
+            if (i > 0 || kProducts == 1) {
+              // loads j with 1 + j * (kProducts - 1) / kLoads == i, or all of them
+              static_for<kLoads>([&](auto j) {
+                constexpr int J = decltype(j)::value;
+                if ((kProducts == 1 ? 0 : 1 + J * (kProducts - 1) / kLoads) == i) load(j);
+              });
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
     };
     lp.template load<0, IP>(at_p(0));
     lq.template load<0, IQ>(at_q(0));
@@ -197,25 +229,21 @@ struct Product {
     wait_loads_le<IP + IQ>();
     stage_barrier();
     Operands a, b;
-    read(a, 0, 0);
+    read_q(a, 0, 0);
+    read_p(a, 0, 0);
     const int stages = (n_k + kStep - 1) / kStep;
+    const auto none = [](auto) {};
     const auto stage = [&](auto cur) {
       constexpr int CUR = decltype(cur)::value;
-      lp.template load<0, IP / 2>(at_p(CUR + 2));
-      read(b, CUR, 1);
-      multiply(a);
-      lp.template load<IP / 2, IP>(at_p(CUR + 2));
-      read(a, CUR, 2);
-      multiply(b);
-      read(b, CUR, 3);
-      multiply(a);
+      block(a, b, CUR, 1, std::integral_constant<int, IP / 2>(), [&](auto j) { lp.template load<j, j + 1>(at_p(CUR + 2)); });
+      block(b, a, CUR, 2, std::integral_constant<int, IP - IP / 2>(),
+            [&](auto j) { lp.template load<IP / 2 + j, IP / 2 + j + 1>(at_p(CUR + 2)); });
+      block(a, b, CUR, 3, std::integral_constant<int, 0>(), none);
       // the next stage is in LDS (P's after it may be on its way), and the last
       // operands of this one in registers
       wait_loads_le<IP>();
       stage_barrier();
-      lq.template load<0, IQ>(at_q(CUR + 2));
-      read(a, CUR + 1, 0);
-      multiply(b);
+      block(b, a, CUR + 1, 0, std::integral_constant<int, IQ>(), [&](auto j) { lq.template load<j, j + 1>(at_q(CUR + 2)); });
     };
     for (int t = 0; t < stages;) {
 #define NSP_TILE_STAGE(CUR)                       \

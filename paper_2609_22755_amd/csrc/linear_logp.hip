@@ -103,17 +103,23 @@ __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void
 #pragma unroll
     for (int p = 0; p < P::BP; ++p)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) m = fmaxf(m, x.acc[q][p][i]);
+      for (int i = 0; i < 16; i += 2) m = fmaxf(fmaxf(m, x.acc[q][p][i]), x.acc[q][p][i + 1]);
     m = wave_max_halves(m);
     float s = 0.f, u = 0.f;
+    const auto sums = [&](auto least) {
+      s = u = 0.f;
 #pragma unroll
-    for (int p = 0; p < P::BP; ++p)
+      for (int p = 0; p < P::BP; ++p)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float d = (x.acc[q][p][i] - m) * c, e = fast_exp2(d);
-        s += e;
-        u = fmaf(e, fmaxf(d, -200.f), u);
-      }
+        for (int i = 0; i < 16; ++i) {
+          const float d = (x.acc[q][p][i] - m) * c, e = fast_exp2(d);
+          s += e;
+          u = fmaf(e, least(d), u);
+        }
+    };
+    sums([](float d) { return d; });
+    // 0 times infinity: logits of -inf count for nothing (a NaN stays one in s)
+    if (__any(u != u)) sums([](float d) { return fmaxf(d, -200.f); });
     s = wave_sum_halves(s);
     u = wave_sum_halves(u);
     if (h == 0) stat[x.wp * NQ + x.q0() + 32 * q + l32] = make_float4(m, s, u, 0.f);
@@ -334,19 +340,26 @@ __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void
 #pragma unroll
   for (int q = 0; q < P::BQ; ++q) {
     const int r0 = q0 + x.q0() + 32 * q, r = r0 + l32;
-    const bool there = r < n;
-    const float4 k = there ? b.coef[r] : make_float4(0.f, 0.f, 0.f, 0.f);
-    const int y = there ? b.target[r] - b.v0 - vw : -1;
+    // (rows from n on and columns from n_v on are read by nobody)
+    const float4 k = r < n ? b.coef[r] : make_float4(0.f, 0.f, 0.f, 0.f);
+    const int y = r < n ? b.target[r] - b.v0 - vw : -1;
+    const auto each = [&](auto slope) {
 #pragma unroll
-    for (int p = 0; p < P::BP; ++p)
+      for (int p = 0; p < P::BP; ++p)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float d = (x.acc[q][p][i] * a.scale - k.x) * kLog2e;
-        float g = fast_exp2(fminf(d, 0.f)) * (k.y + k.z * fmaxf(d, -200.f));
-        const int e = 32 * p + p_of(i, h);
-        if (e == y) g += k.w;
-        x.acc[q][p][i] = there && vw + e < b.n_v ? g : 0.f;
-      }
+        for (int i = 0; i < 16; ++i) {
+          const float d = (x.acc[q][p][i] * a.scale - k.x) * kLog2e;
+          x.acc[q][p][i] = fast_exp2(fminf(d, 0.f)) * slope(d);
+        }
+    };
+    if (__any(k.z != 0.f)) each([&](float d) { return k.y + k.z * fmaxf(d, -200.f); });
+    else each([&](float) { return k.y; });
+    if (__any(y >= 0 && y < 32 * P::BP)) {
+#pragma unroll
+      for (int p = 0; p < P::BP; ++p)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x.acc[q][p][i] += 32 * p + p_of(i, h) == y ? k.w : 0.f;
+    }
     char *out = b.dl + 2 * ((int64_t)r0 * b.f.piece + vw);
     put_rows<P::BP, false>(x.acc[q], smem + x.wave * (2048 * P::BP), 32, 32 * P::BP, x.lane,
                            [&](int row, int byte, f32x4 v) { *(f32x4 *)(out + (int64_t)row * 2 * b.f.piece + byte) = v; });
