@@ -262,21 +262,26 @@ struct Product {
   }
 };
 
-// Tile `id` of np x nq (p, q), for workgroups that go to the XCDs in turn: each
-// XCD takes one run of the order, in which `group` neighbours of p pass over all q
-// (its compute units then share group + some of q's operands in its L2).  False:
-// there is none.
-__device__ __forceinline__ bool place(int id, int np, int nq, int group, int &p, int &q) {
-  const int total = np * nq, x = id % kXcdQueues, i = id / kXcdQueues;
-  const int per = total / kXcdQueues, more = total % kXcdQueues;
-  if (i >= per + (x < more ? 1 : 0)) return false;
-  const int at = x * per + min(x, more) + i;
-  const int g = at / (group * nq), in = at - g * group * nq;
-  const int wide = min(group, np - g * group);
-  q = in / wide;
-  p = g * group + in - q * wide;
-  return true;
-}
+// Tile `id` of np x nq (p, q) in `parts` parts, for workgroups that go to the XCDs in
+// turn: each XCD takes one run of the order, part after part, in which `group`
+// neighbours of p pass over all q (its compute units then share group + some of q's
+// operands in its L2).  False: there is none.
+struct Place {
+  int p, q, part;
+  __device__ __forceinline__ bool find(int id, int np, int nq, int parts, int group) {
+    const int tiles = np * nq, total = tiles * parts, x = id % kXcdQueues, i = id / kXcdQueues;
+    const int per = total / kXcdQueues, more = total % kXcdQueues;
+    if (i >= per + (x < more ? 1 : 0)) return false;
+    int at = x * per + min(x, more) + i;
+    part = parts > 1 ? at / tiles : 0;
+    at -= part * tiles;
+    const int g = at / (group * nq), in = at - g * group * nq;
+    const int wide = min(group, np - g * group);
+    q = in / wide;
+    p = g * group + in - q * wide;
+    return true;
+  }
+};
 
 }  // namespace tile
 }  // namespace nsp

@@ -68,10 +68,10 @@ template <int NQ>
 __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void linear_logp_tiles_kernel(FwdTiles f) {
   typedef typename LogitTile<NQ>::P P;
   __shared__ __attribute__((aligned(1024))) char smem[P::kLds];
-  int tp, tq;
-  if (!tile::place(blockIdx.x, f.tiles_p, f.tiles_q, kGroup, tp, tq)) return;
+  tile::Place at;
+  if (!at.find(blockIdx.x, f.tiles_p, f.tiles_q, 1, kGroup)) return;
   P x;
-  const int v0 = tp * P::NP, q0 = tq * NQ;
+  const int v0 = at.p * P::NP, q0 = at.q * NQ;
   const LinearArgs &a = f.a;
   x.run(smem, typename P::LoadP(a.w, a.w_stride, v0, a.vocab, 0, a.dim, x.wave, x.lane),
         typename P::LoadQ(a.x, a.x_stride, f.t0 + q0, f.t0 + f.n, 0, a.dim, x.wave, x.lane), a.dim);
@@ -137,7 +137,7 @@ __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void
       r.y = er * r.y + eo * o.y;
       r.x = m;
     }
-    f.part[tp * f.panel + q0 + tok] = r;
+    f.part[at.p * f.panel + q0 + tok] = r;
   }
 }
 
@@ -228,71 +228,105 @@ struct BwdTiles {
   char *dl;                    // [rows][piece]
   float *sum_x, *sum_w;        // [split][rows][dim], [split][piece][dim]
   int v0, n_v;                 // the piece
-  bool first, last;
+  bool first, last;            // of the pieces
+  bool sums_x;                 // dx goes by float32 sums
+  int tiles_dim;               // tiles of columns
+  int grid_x, grid_w;          // workgroups of dx and dw, multiples of kXcdQueues
 };
+
+// A token's coefficients; whether it has a gradient.
+struct Coefficients {
+  bool some = false;
+  float lse = 0.f, k0 = 0.f, k1 = 0.f, at = 0.f;
+  int y = -1;
+  __device__ __forceinline__ Coefficients(const LinearArgs &a, int64_t t) {
+    if (t >= a.n_tokens) return;
+    const int64_t target = a.g_logp ? a.targets[t] : -1;
+    const bool given = target >= 0 && target < a.vocab;
+    const float gl = given ? a.g_logp[t] : 0.f, gs = a.g_lse ? a.g_lse[t] : 0.f, ge = a.g_entropy ? a.g_entropy[t] : 0.f;
+    lse = a.lse_in[t];
+    some = !(lse == kNegInf || (gl == 0.f && gs == 0.f && ge == 0.f));
+    k0 = a.scale * (gs - gl - (ge != 0.f ? ge * a.entropy_in[t] : 0.f)) + (lse < -kNegInf ? 0.f : kNan);
+    k1 = -a.scale * ge * kLn2;
+    at = a.scale * gl;
+    y = given ? (int)target : -1;
+  }
+  __device__ __forceinline__ void store(const BwdTiles &b, int64_t t, int row) const {
+    b.place[t] = some ? row : -1;
+    if (!some) return;
+    b.order[row] = (int)t;
+    b.coef[row] = make_float4(lse, k0, k1, at);
+    b.target[row] = y;
+  }
+};
+
+// Threads of a workgroup of 1024 before this one that have `some`; n: of all.
+__device__ __forceinline__ int count_before(bool some, int (&sums)[16], int &n) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t in = __ballot(some);
+  if (lane == 0) sums[wave] = __popcll(in);
+  __syncthreads();
+  int before = __popcll(in & ((uint64_t(1) << lane) - 1));
+  n = 0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) {
+    before += w < wave ? sums[w] : 0;
+    n += sums[w];
+  }
+  __syncthreads();                               // (sums may be written again)
+  return before;
+}
+
+// A token's hidden row to its place; dx of a token without one is zero.
+__device__ __forceinline__ void gather_row(const BwdTiles &b, int64_t t, int row) {
+  const LinearArgs &a = b.a;
+  const int lane = threadIdx.x & 63;
+  if (row >= 0) {
+    const u32x4 *from = (const u32x4 *)(a.x + 2 * t * a.x_stride);
+    u32x4 *to = (u32x4 *)(b.x + 2 * (int64_t)row * a.dim);
+    for (int i = lane; i < a.dim / 8; i += 64) to[i] = from[i];
+  } else if (a.dx) {
+    u32x4 *to = (u32x4 *)(a.dx + (a.g_f32 ? 4 : 2) * t * a.dx_stride);
+    for (int i = lane; i < a.dim / (a.g_f32 ? 4 : 8); i += 64) to[i] = u32x4{};
+  }
+}
 
 // Which tokens have a gradient, in order, and the coefficients of their rows.
 __global__ __launch_bounds__(1024) void linear_rows_kernel(BwdTiles b) {
   __shared__ int sums[16];
-  __shared__ int base;
-  const LinearArgs &a = b.a;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (threadIdx.x == 0) base = 0;
-  __syncthreads();
-  for (int64_t t0 = 0; t0 < a.n_tokens; t0 += 1024) {
+  int base = 0;
+  for (int64_t t0 = 0; t0 < b.a.n_tokens; t0 += 1024) {
     const int64_t t = t0 + threadIdx.x;
-    bool some = false;
-    float lse = 0.f, k0 = 0.f, k1 = 0.f, at = 0.f;
-    int y = -1;
-    if (t < a.n_tokens) {
-      const int64_t target = a.g_logp ? a.targets[t] : -1;
-      const bool given = target >= 0 && target < a.vocab;
-      const float gl = given ? a.g_logp[t] : 0.f, gs = a.g_lse ? a.g_lse[t] : 0.f, ge = a.g_entropy ? a.g_entropy[t] : 0.f;
-      lse = a.lse_in[t];
-      some = !(lse == kNegInf || (gl == 0.f && gs == 0.f && ge == 0.f));
-      k0 = a.scale * (gs - gl - (ge != 0.f ? ge * a.entropy_in[t] : 0.f)) + (lse < -kNegInf ? 0.f : kNan);
-      k1 = -a.scale * ge * kLn2;
-      at = a.scale * gl;
-      y = given ? (int)target : -1;
-    }
-    const uint64_t in = __ballot(some);
-    const int before = __popcll(in & ((uint64_t(1) << lane) - 1));
-    if (lane == 0) sums[wave] = __popcll(in);
-    __syncthreads();
-    int at_row = base + before;
-    for (int w = 0; w < wave; ++w) at_row += sums[w];
-    if (t < a.n_tokens) b.place[t] = some ? at_row : -1;
-    if (some) {
-      b.order[at_row] = (int)t;
-      b.coef[at_row] = make_float4(lse, k0, k1, at);
-      b.target[at_row] = y;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      int n = 0;
-      for (int w = 0; w < 16; ++w) n += sums[w];
-      base += n;
-    }
-    __syncthreads();
+    const Coefficients c(b.a, t);
+    int n;
+    const int before = count_before(c.some, sums, n);
+    if (t < b.a.n_tokens) c.store(b, t, base + before);
+    base += n;
   }
   if (threadIdx.x == 0) *b.count = base;
 }
 
-// A token's hidden row to its place; dx of the others is zero.
 __global__ __launch_bounds__(256) void linear_gather_kernel(BwdTiles b) {
-  const LinearArgs &a = b.a;
-  const int wave = (int)threadIdx.x >> 6, lane = threadIdx.x & 63;
-  for (int64_t t = (int64_t)blockIdx.x * 4 + wave; t < a.n_tokens; t += (int64_t)gridDim.x * 4) {
-    const int at = b.place[t];
-    if (at >= 0) {
-      const u32x4 *from = (const u32x4 *)(a.x + 2 * t * a.x_stride);
-      u32x4 *to = (u32x4 *)(b.x + 2 * (int64_t)at * a.dim);
-      for (int i = lane; i < a.dim / 8; i += 64) to[i] = from[i];
-    } else if (a.dx) {
-      u32x4 *to = (u32x4 *)(a.dx + (a.g_f32 ? 4 : 2) * t * a.dx_stride);
-      for (int i = lane; i < a.dim / (a.g_f32 ? 4 : 8); i += 64) to[i] = u32x4{};
-    }
+  const int wave = (int)threadIdx.x >> 6;
+  for (int64_t t = (int64_t)blockIdx.x * 4 + wave; t < b.a.n_tokens; t += (int64_t)gridDim.x * 4) gather_row(b, t, b.place[t]);
+}
+
+// Both, of up to kLinearFew tokens: every workgroup finds all places for itself.
+__global__ __launch_bounds__(1024) void linear_rows_gather_kernel(BwdTiles b) {
+  static_assert(plan::kLinearFew == 1024, "a token a thread");
+  __shared__ int sums[16], place[plan::kLinearFew];
+  const int64_t t = threadIdx.x;
+  const Coefficients c(b.a, t);
+  int n;
+  const int before = count_before(c.some, sums, n);
+  place[t] = c.some ? before : -1;
+  if (blockIdx.x == 0) {
+    if (t < b.a.n_tokens) c.store(b, t, before);
+    if (t == 0) *b.count = n;
   }
+  __syncthreads();
+  const int wave = (int)threadIdx.x >> 6;
+  for (int r = (int)blockIdx.x * 16 + wave; r < b.a.n_tokens; r += (int)gridDim.x * 16) gather_row(b, r, place[r]);
 }
 
 // 32 q's (one a lane pair) of 32 * NB p's, of a wave's sums, as rows of p: through
@@ -328,10 +362,10 @@ __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void
   static_assert(P::kLds >= 512 * 32 * P::BP, "room for the rows that are stored");
   __shared__ __attribute__((aligned(1024))) char smem[P::kLds];
   const int n = *b.count;
-  int tp, tq;
-  if (!tile::place(blockIdx.x, tiles_p, (n + NQ - 1) / NQ, kGroup, tp, tq)) return;
+  tile::Place at;
+  if (!at.find(blockIdx.x, tiles_p, (n + NQ - 1) / NQ, 1, kGroup)) return;
   P x;
-  const int v0 = tp * P::NP, q0 = tq * NQ;     // (of the piece)
+  const int v0 = at.p * P::NP, q0 = at.q * NQ;   // (of the piece)
   const LinearArgs &a = b.a;
   x.run(smem, typename P::LoadP(a.w, a.w_stride, b.v0 + v0, b.v0 + b.n_v, 0, a.dim, x.wave, x.lane),
         typename P::LoadQ(b.x, a.dim, q0, n, 0, a.dim, x.wave, x.lane), a.dim);
@@ -396,51 +430,62 @@ template <>
 struct DxTile<256> { typedef Product<kAcross, kAlong, 256, 256, 2, 4> P; };
 template <>
 struct DxTile<64> { typedef Product<kAcross, kAlong, 256, 64, 4, 2> P; };
+// dw: p: columns, q: the piece's vocabulary rows, k: gathered rows.
+typedef Product<kAcross, kAcross, 256, 256, 2, 4> DwTile;
 
-template <int NQ, Out OUT>
-__global__ __launch_bounds__(512, kWavesPerSimd<typename DxTile<NQ>::P>) void linear_dx_kernel(BwdTiles b, int tiles_p) {
+template <int NQ>
+__device__ __forceinline__ void dx_tile(const BwdTiles &b, int id, char *smem) {
   typedef typename DxTile<NQ>::P P;
-  __shared__ __attribute__((aligned(1024))) char smem[P::kLds];
-  const int n = *b.count;
-  int tp, tq;
-  if (!tile::place(blockIdx.x, tiles_p, (n + NQ - 1) / NQ, kGroup, tp, tq)) return;
+  const int n = *b.count, dim = b.a.dim;
+  tile::Place at;
+  if (!at.find(id, b.tiles_dim, (n + NQ - 1) / NQ, b.f.split_x, kGroup)) return;
   P x;
-  const int part = blockIdx.y;
   const int len = (int)plan::round_up(plan::ceil_div(b.f.piece, b.f.split_x), tile::kStep);
-  const int k0 = part * len, n_k = max(0, min(b.n_v - k0, len));
-  const int p0 = tp * P::NP, q0 = tq * NQ, dim = b.a.dim;
+  const int k0 = at.part * len, n_k = max(0, min(b.n_v - k0, len));
+  const int p0 = at.p * P::NP, q0 = at.q * NQ;
   x.run(smem, typename P::LoadP(b.a.w, b.a.w_stride, p0, dim, b.v0 + k0, n_k, x.wave, x.lane),
         typename P::LoadQ(b.dl, b.f.piece, q0, n, k0, n_k, x.wave, x.lane), n_k);
-  if constexpr (OUT == kSums) {
-    float *sums = b.sum_x + (int64_t)part * b.f.rows * dim;
-    put_product<P, OUT>(x, smem, p0, q0, n, dim, !b.first, [&](int r) { return (char *)(sums + (int64_t)r * dim); });
+  const auto row = [&](int es) { return [=, &b](int r) { return b.a.dx + (int64_t)b.order[r] * b.a.dx_stride * es; }; };
+  if (b.sums_x) {
+    float *sums = b.sum_x + (int64_t)at.part * b.f.rows * dim;
+    put_product<P, kSums>(x, smem, p0, q0, n, dim, !b.first, [&](int r) { return (char *)(sums + (int64_t)r * dim); });
+  } else if (b.a.g_f32) {
+    put_product<P, kF32>(x, smem, p0, q0, n, dim, false, row(4));
   } else {
-    put_product<P, OUT>(x, smem, p0, q0, n, dim, false,
-                        [&](int r) { return b.a.dx + (int64_t)b.order[r] * b.a.dx_stride * (OUT == kF32 ? 4 : 2); });
+    put_product<P, kBf16>(x, smem, p0, q0, n, dim, false, row(2));
   }
 }
 
-// dw of a piece: p: columns, q: the piece's vocabulary rows, k: gathered rows.
-typedef Product<kAcross, kAcross, 256, 256, 2, 4> DwTile;
-template <Out OUT>
-__global__ __launch_bounds__(512, 2) void linear_dw_kernel(BwdTiles b, int tiles_p) {
+__device__ __forceinline__ void dw_tile(const BwdTiles &b, int id, char *smem) {
   typedef DwTile P;
-  __shared__ __attribute__((aligned(1024))) char smem[P::kLds];
-  int tp, tq;
-  if (!tile::place(blockIdx.x, tiles_p, (int)plan::ceil_div(b.n_v, P::NQ), kGroup, tp, tq)) return;
+  const int dim = b.a.dim;
+  tile::Place at;
+  if (!at.find(id, b.tiles_dim, (int)plan::ceil_div(b.n_v, P::NQ), b.f.split_w, kGroup)) return;
   P x;
-  const int n = *b.count, part = blockIdx.y;
+  const int n = *b.count;
   const int len = (int)plan::round_up(plan::ceil_div(n, b.f.split_w), tile::kStep);
-  const int k0 = part * len, n_k = max(0, min(n - k0, len));
-  const int p0 = tp * P::NP, q0 = tq * P::NQ, dim = b.a.dim;
+  const int k0 = at.part * len, n_k = max(0, min(n - k0, len));
+  const int p0 = at.p * P::NP, q0 = at.q * P::NQ;
   x.run(smem, P::LoadP(b.x, dim, p0, dim, k0, n_k, x.wave, x.lane), P::LoadQ(b.dl, b.f.piece, q0, b.n_v, k0, n_k, x.wave, x.lane), n_k);
-  if constexpr (OUT == kSums) {
-    float *sums = b.sum_w + (int64_t)part * b.f.piece * dim;
-    put_product<P, OUT>(x, smem, p0, q0, b.n_v, dim, false, [&](int r) { return (char *)(sums + (int64_t)r * dim); });
+  const auto row = [&](int es) { return [=, &b](int r) { return b.a.dw + (int64_t)(b.v0 + r) * b.a.dw_stride * es; }; };
+  if (b.f.split_w > 1) {
+    float *sums = b.sum_w + (int64_t)at.part * b.f.piece * dim;
+    put_product<P, kSums>(x, smem, p0, q0, b.n_v, dim, false, [&](int r) { return (char *)(sums + (int64_t)r * dim); });
+  } else if (b.a.g_f32) {
+    put_product<P, kF32>(x, smem, p0, q0, b.n_v, dim, false, row(4));
   } else {
-    put_product<P, OUT>(x, smem, p0, q0, b.n_v, dim, false,
-                        [&](int r) { return b.a.dw + (int64_t)(b.v0 + r) * b.a.dw_stride * (OUT == kF32 ? 4 : 2); });
+    put_product<P, kBf16>(x, smem, p0, q0, b.n_v, dim, false, row(2));
   }
+}
+
+// dx's tiles, then dw's, of a piece.
+template <int NQ>
+__global__ __launch_bounds__(512, 2) void linear_grads_kernel(BwdTiles b) {
+  constexpr int kX = DxTile<NQ>::P::kLds;
+  __shared__ __attribute__((aligned(1024))) char smem[kX > DwTile::kLds ? kX : DwTile::kLds];
+  const int id = (int)blockIdx.x;
+  if (id < b.grid_x) dx_tile<NQ>(b, id, smem);
+  else dw_tile(b, id - b.grid_x, smem);
 }
 
 // The parts' sums, in order, as rows of the gradient.
@@ -449,24 +494,22 @@ __global__ __launch_bounds__(256) void linear_sums_kernel(BwdTiles b) {
   const int rows = DX ? *b.count : b.n_v, dim = b.a.dim, parts = DX ? b.f.split_x : b.f.split_w;
   const int64_t per = (DX ? b.f.rows : (int64_t)b.f.piece) * dim;
   const float *sums = DX ? b.sum_x : b.sum_w;
-  const int vecs = dim / 8;
+  const int vecs = dim / 4;
   const int64_t n = (int64_t)rows * vecs;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int r = (int)(i / vecs), c = (int)(i - (int64_t)r * vecs) * 8;
+    const int r = (int)(i / vecs), c = (int)(i - (int64_t)r * vecs) * 4;
     const float *from = sums + (int64_t)r * dim + c;
-    f32x4 lo = *(const f32x4 *)from, hi = *(const f32x4 *)(from + 4);
-    for (int p = 1; p < parts; ++p) {
-      lo += *(const f32x4 *)(from + p * per);
-      hi += *(const f32x4 *)(from + p * per + 4);
+    f32x4 sum = *(const f32x4 *)from;
+    for (int p0 = 1; p0 < parts; p0 += 8) {
+      f32x4 v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = p0 + j < parts ? *(const f32x4 *)(from + (p0 + j) * per) : f32x4{};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum += v[j];
     }
     char *row = DX ? b.a.dx + (int64_t)b.order[r] * b.a.dx_stride * (F32 ? 4 : 2) : b.a.dw + (int64_t)(b.v0 + r) * b.a.dw_stride * (F32 ? 4 : 2);
-    if constexpr (F32) {
-      *(f32x4 *)(row + 4 * c) = lo;
-      *(f32x4 *)(row + 4 * c + 16) = hi;
-    } else {
-      const u32x4 v = {pack_bf16(lo[0], lo[1]), pack_bf16(lo[2], lo[3]), pack_bf16(hi[0], hi[1]), pack_bf16(hi[2], hi[3])};
-      *(u32x4 *)(row + 2 * c) = v;
-    }
+    if constexpr (F32) *(f32x4 *)(row + 4 * c) = sum;
+    else *(uint2 *)(row + 2 * c) = make_uint2(pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3]));
   }
 }
 
@@ -493,27 +536,28 @@ hipError_t dl_tiles(const BwdTiles &b, hipStream_t s) {
 }
 
 template <int NQ>
-hipError_t dx_tiles(const BwdTiles &b, bool sums, hipStream_t s) {
-  const int tiles_p = (int)plan::ceil_div(b.a.dim, plan::kTileP);
-  const dim3 grid(grid_of(tiles_p * plan::ceil_div(b.f.rows, NQ)), b.f.split_x);
-  if (sums) linear_dx_kernel<NQ, kSums><<<grid, 512, 0, s>>>(b, tiles_p);
-  else if (b.a.g_f32) linear_dx_kernel<NQ, kF32><<<grid, 512, 0, s>>>(b, tiles_p);
-  else linear_dx_kernel<NQ, kBf16><<<grid, 512, 0, s>>>(b, tiles_p);
+hipError_t launch_grads(const BwdTiles &b, hipStream_t s) {
+  const int grid = b.grid_x + b.grid_w;
+  if (grid > 0) linear_grads_kernel<NQ><<<grid, 512, 0, s>>>(b);
   return hipGetLastError();
 }
 
-hipError_t dw_tiles(const BwdTiles &b, hipStream_t s) {
-  const int tiles_p = (int)plan::ceil_div(b.a.dim, plan::kTileP);
-  const dim3 grid(grid_of(tiles_p * plan::ceil_div(b.n_v, DwTile::NQ)), b.f.split_w);
-  if (b.f.split_w > 1) linear_dw_kernel<kSums><<<grid, 512, 0, s>>>(b, tiles_p);
-  else if (b.a.g_f32) linear_dw_kernel<kF32><<<grid, 512, 0, s>>>(b, tiles_p);
-  else linear_dw_kernel<kBf16><<<grid, 512, 0, s>>>(b, tiles_p);
-  return hipGetLastError();
+// In one launch, where dx alone would leave compute units idle.  (100 x 704 x 12000: 21
+// and 12 us apart, XX together; where both fill them the two together are 1% slower.)
+template <int NQ>
+hipError_t grads(BwdTiles b, hipStream_t s) {
+  b.grid_x = b.a.dx ? grid_of(b.tiles_dim * plan::ceil_div(b.f.rows, NQ) * b.f.split_x) : 0;
+  b.grid_w = b.a.dw ? grid_of(b.tiles_dim * plan::ceil_div(b.n_v, DwTile::NQ) * b.f.split_w) : 0;
+  if (b.grid_x <= plan::kUnits || b.grid_w == 0) return launch_grads<NQ>(b, s);
+  BwdTiles w = b;
+  w.grid_x = b.grid_w = 0;
+  const hipError_t e = launch_grads<NQ>(w, s);
+  return e == hipSuccess ? launch_grads<NQ>(b, s) : e;
 }
 
 template <bool DX>
 hipError_t join_sums(const BwdTiles &b, hipStream_t s) {
-  const int64_t vecs = (DX ? b.f.rows : (int64_t)b.n_v) * (b.a.dim / 8);
+  const int64_t vecs = (DX ? b.f.rows : (int64_t)b.n_v) * (b.a.dim / 4);
   const int64_t want = plan::ceil_div(vecs, 256);
   const int grid = (int)(want < 8192 ? want : 8192);
   if (b.a.g_f32) linear_sums_kernel<true, DX><<<grid, 256, 0, s>>>(b);
@@ -563,24 +607,30 @@ hipError_t launch_linear_logp_bwd(const LinearArgs &a, hipStream_t s) {
   b.dl = a.ws + b.f.dl_off;
   b.sum_x = (float *)(a.ws + b.f.sum_x_off);
   b.sum_w = (float *)(a.ws + b.f.sum_w_off);
-  linear_rows_kernel<<<1, 1024, 0, s>>>(b);
-  hipError_t e = hipGetLastError();
+  hipError_t e;
+  if (a.n_tokens <= plan::kLinearFew) {
+    const int64_t groups = plan::ceil_div(a.n_tokens, 16);
+    linear_rows_gather_kernel<<<(int)groups, 1024, 0, s>>>(b);
+    e = hipGetLastError();
+  } else {
+    linear_rows_kernel<<<1, 1024, 0, s>>>(b);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    const int64_t groups = plan::ceil_div(a.n_tokens, 4);
+    linear_gather_kernel<<<(int)(groups < 65536 ? groups : 65536), 256, 0, s>>>(b);
+    e = hipGetLastError();
+  }
   if (e != hipSuccess) return e;
-  const int64_t groups = plan::ceil_div(a.n_tokens, 4);
-  linear_gather_kernel<<<(int)(groups < 65536 ? groups : 65536), 256, 0, s>>>(b);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const bool sums = b.f.pieces > 1 || b.f.split_x > 1;
+  b.sums_x = b.f.pieces > 1 || b.f.split_x > 1;
+  b.tiles_dim = (int)plan::ceil_div(a.dim, plan::kTileP);
   for (int p = 0; p < b.f.pieces; ++p) {
     b.v0 = p * b.f.piece;
     b.n_v = a.vocab - b.v0 < b.f.piece ? a.vocab - b.v0 : b.f.piece;
     b.first = p == 0;
     b.last = p == b.f.pieces - 1;
     e = b.f.tile == 32 ? dl_tiles<32>(b, s) : b.f.tile == 64 ? dl_tiles<64>(b, s) : b.f.tile == 128 ? dl_tiles<128>(b, s) : dl_tiles<256>(b, s);
-    if (e == hipSuccess && a.dw) e = dw_tiles(b, s);
+    if (e == hipSuccess) e = b.f.tile_x == 64 ? grads<64>(b, s) : grads<256>(b, s);
     if (e == hipSuccess && a.dw && b.f.split_w > 1) e = join_sums<false>(b, s);
-    if (e == hipSuccess && a.dx) e = b.f.tile <= 64 ? dx_tiles<64>(b, sums, s) : dx_tiles<256>(b, sums, s);
-    if (e == hipSuccess && a.dx && b.last && sums) e = join_sums<true>(b, s);
+    if (e == hipSuccess && a.dx && b.last && b.sums_x) e = join_sums<true>(b, s);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

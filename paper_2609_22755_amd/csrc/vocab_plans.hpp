@@ -19,8 +19,16 @@ constexpr int kLinearMaxDim = 1 << 16, kLinearMaxVocab = 1 << 24;
 constexpr int64_t kLinearMaxStride = 1 << 20;   // offsets within a tile stay below 2^31 bytes
 constexpr int kTileP = 256;                     // vocabulary rows, or columns of a gradient, of a tile
 
-// Tokens of a tile of logits.
-constexpr int linear_tile(int64_t n_tokens) { return n_tokens <= 32 ? 32 : n_tokens <= 64 ? 64 : n_tokens <= 128 ? 128 : 256; }
+// Compute units that a product's tiles should keep busy.
+constexpr int kUnits = 256;
+
+// Tokens of a tile of logits.  Past 128 tokens, 128 or 256: the tiles of 128 take some
+// 0.56 of the time, and leave fewer compute units idle in their last turn.
+constexpr int linear_tile(int64_t n_tokens, int vocab) {
+  if (n_tokens <= 128) return n_tokens <= 32 ? 32 : n_tokens <= 64 ? 64 : 128;
+  const int64_t p = ceil_div(vocab, kTileP), half = ceil_div(p * ceil_div(n_tokens, 128), kUnits), whole = ceil_div(p * ceil_div(n_tokens, 256), kUnits);
+  return 56 * half < 100 * whole ? 128 : 256;
+}
 
 // Tokens of the forward that are worked on together: their statistics per tile
 // of the vocabulary (16 bytes) stay below some hundred MB.
@@ -34,7 +42,7 @@ struct LinearFwd {
 };
 constexpr LinearFwd linear_fwd(int64_t n_tokens, int vocab) {
   LinearFwd f{};
-  f.tile = linear_tile(n_tokens);
+  f.tile = linear_tile(n_tokens, vocab);
   f.panel = n_tokens < kLinearPanel ? round_up(n_tokens, f.tile) : kLinearPanel;
   f.tiles_p = ceil_div(vocab, kTileP);
   f.part_off = 0;
@@ -43,18 +51,20 @@ constexpr LinearFwd linear_fwd(int64_t n_tokens, int vocab) {
   return f;
 }
 
-// Compute units that a product's tiles should keep busy.
-constexpr int kUnits = 256;
-// Parts of a product's sums over k, where its tiles are too few: of 512 k at least.
+// Parts of a product's sums over k, where its tiles are too few: of 256 k at least.
 constexpr int linear_split(int64_t tiles, int64_t n_k) {
   int64_t s = tiles > 0 ? kUnits / tiles : 1;
-  const int64_t most = n_k / 512;
+  const int64_t most = n_k / 256;
   s = s < most ? s : most;
   return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
 }
+// Tokens that one workgroup finds the rows of, which then every workgroup of the
+// gathering does for itself.
+constexpr int kLinearFew = 1024;
 
 struct LinearBwd {
-  int tile;                    // tokens of a tile
+  int tile;                    // tokens of a tile of logits
+  int tile_x;                  // tokens of a tile of dx
   int64_t rows;                // tokens, in whole tiles
   int piece;                   // vocabulary rows of a piece, in whole tiles
   int pieces;
@@ -67,7 +77,7 @@ struct LinearBwd {
 // 6 T dim piece operations: 2% at pieces of 32768).
 constexpr LinearBwd linear_bwd(int64_t n_tokens, int dim, int vocab) {
   LinearBwd f{};
-  f.tile = linear_tile(n_tokens);
+  f.tile = linear_tile(n_tokens, vocab);
   f.rows = round_up(n_tokens, f.tile);
   const int64_t all = round_up(vocab, kTileP);
   int64_t piece = (int64_t(1) << 28) / (f.rows > 0 ? f.rows : 1) / kTileP * kTileP;
@@ -76,7 +86,8 @@ constexpr LinearBwd linear_bwd(int64_t n_tokens, int dim, int vocab) {
   f.piece = (int)round_up(ceil_div(all, f.pieces), kTileP);
   f.pieces = (int)ceil_div(all, f.piece);
   const int64_t cols = ceil_div(dim, kTileP);
-  f.split_x = linear_split(cols * (f.rows / f.tile), f.piece);
+  f.tile_x = n_tokens <= 64 ? 64 : 256;
+  f.split_x = linear_split(cols * ceil_div(n_tokens, f.tile_x), f.piece);
   f.split_w = linear_split(cols * (f.piece / kTileP), n_tokens);
   size_t at = 0;
   f.count_off = at, at += 256;
