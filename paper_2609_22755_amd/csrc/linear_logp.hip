@@ -224,7 +224,7 @@ struct BwdTiles {
   int *place;                  // [tokens]: a token's row, -1: it has no gradient
   float4 *coef;                // [rows]: lse, k0, k1, the target's
   int *target;                 // [rows], -1: none
-  char *x;                     // gathered rows
+  char *x;                     // gathered rows [rows][f.dim]
   char *dl;                    // [rows][piece]
   float *sum_x, *sum_w;        // [split][rows][dim], [split][piece][dim]
   int v0, n_v;                 // the piece
@@ -283,7 +283,7 @@ __device__ __forceinline__ void gather_row(const BwdTiles &b, int64_t t, int row
   const int lane = threadIdx.x & 63;
   if (row >= 0) {
     const u32x4 *from = (const u32x4 *)(a.x + 2 * t * a.x_stride);
-    u32x4 *to = (u32x4 *)(b.x + 2 * (int64_t)row * a.dim);
+    u32x4 *to = (u32x4 *)(b.x + 2 * (int64_t)row * b.f.dim);
     for (int i = lane; i < a.dim / 8; i += 64) to[i] = from[i];
   } else if (a.dx) {
     u32x4 *to = (u32x4 *)(a.dx + (a.g_f32 ? 4 : 2) * t * a.dx_stride);
@@ -368,7 +368,7 @@ __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void
   const int v0 = at.p * P::NP, q0 = at.q * NQ;   // (of the piece)
   const LinearArgs &a = b.a;
   x.run(smem, typename P::LoadP(a.w, a.w_stride, b.v0 + v0, b.v0 + b.n_v, 0, a.dim, x.wave, x.lane),
-        typename P::LoadQ(b.x, a.dim, q0, n, 0, a.dim, x.wave, x.lane), a.dim);
+        typename P::LoadQ(b.x, b.f.dim, q0, n, 0, a.dim, x.wave, x.lane), a.dim);
   const int l32 = x.lane & 31, h = x.lane >> 5;
   const int vw = v0 + x.p0();
 #pragma unroll
@@ -466,7 +466,7 @@ __device__ __forceinline__ void dw_tile(const BwdTiles &b, int id, char *smem) {
   const int len = (int)plan::round_up(plan::ceil_div(n, b.f.split_w), tile::kStep);
   const int k0 = at.part * len, n_k = max(0, min(n - k0, len));
   const int p0 = at.p * P::NP, q0 = at.q * P::NQ;
-  x.run(smem, P::LoadP(b.x, dim, p0, dim, k0, n_k, x.wave, x.lane), P::LoadQ(b.dl, b.f.piece, q0, b.n_v, k0, n_k, x.wave, x.lane), n_k);
+  x.run(smem, P::LoadP(b.x, b.f.dim, p0, dim, k0, n_k, x.wave, x.lane), P::LoadQ(b.dl, b.f.piece, q0, b.n_v, k0, n_k, x.wave, x.lane), n_k);
   const auto row = [&](int es) { return [=, &b](int r) { return b.a.dw + (int64_t)(b.v0 + r) * b.a.dw_stride * es; }; };
   if (b.f.split_w > 1) {
     float *sums = b.sum_w + (int64_t)at.part * b.f.piece * dim;

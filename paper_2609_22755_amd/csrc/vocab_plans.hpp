@@ -68,6 +68,7 @@ struct LinearBwd {
   int64_t rows;                // tokens, in whole tiles
   int piece;                   // vocabulary rows of a piece, in whole tiles
   int pieces;
+  int dim;                     // elements between gathered rows: whole 128-byte lines
   int split_x, split_w;        // parts of dx's and dw's sums
   size_t count_off, order_off, place_off, coef_off, target_off, x_off, dl_off, sum_x_off, sum_w_off, bytes;
 };
@@ -79,6 +80,7 @@ constexpr LinearBwd linear_bwd(int64_t n_tokens, int dim, int vocab) {
   LinearBwd f{};
   f.tile = linear_tile(n_tokens, vocab);
   f.rows = round_up(n_tokens, f.tile);
+  f.dim = (int)round_up(dim, 64);
   const int64_t all = round_up(vocab, kTileP);
   int64_t piece = (int64_t(1) << 28) / (f.rows > 0 ? f.rows : 1) / kTileP * kTileP;
   piece = piece < 4096 ? 4096 : piece;
@@ -95,7 +97,7 @@ constexpr LinearBwd linear_bwd(int64_t n_tokens, int dim, int vocab) {
   f.place_off = at, at += pad256((size_t)f.rows * 4);
   f.coef_off = at, at += pad256((size_t)f.rows * 16);
   f.target_off = at, at += pad256((size_t)f.rows * 4);
-  f.x_off = at, at += pad256((size_t)f.rows * dim * 2);
+  f.x_off = at, at += pad256((size_t)f.rows * f.dim * 2);
   f.dl_off = at, at += pad256((size_t)f.rows * f.piece * 2);
   f.sum_x_off = at;
   if (f.pieces > 1 || f.split_x > 1) at += pad256((size_t)f.split_x * f.rows * dim * 4);
