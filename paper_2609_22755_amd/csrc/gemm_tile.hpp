@@ -209,7 +209,9 @@ struct Product {
           if (i == 0) {
             read_q(next, stage, kb);
             read_p(next, stage, kb);
+            __builtin_amdgcn_s_setprio(1);       // (over the other wave's reads: 1%)
           }
+          if (i == BP * BQ - 1) __builtin_amdgcn_s_setprio(0);
           if constexpr (kLoads > 0) {
             if (i > 0 || kProducts == 1) {
               // loads j with 1 + j * (kProducts - 1) / kLoads == i, or all of them

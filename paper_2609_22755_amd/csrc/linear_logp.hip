@@ -31,7 +31,7 @@ using tile::Product;
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kNan = __builtin_nanf("");
 constexpr float kLowest = -3.402823466e38f;
-constexpr int kGroup = 8;      // neighbouring tiles of p that share q's in an L2
+constexpr int kGroup = 4;      // neighbouring tiles of p that share q's in an L2
 
 // A tile of logits: 256 vocabulary rows, NQ tokens.
 template <int NQ>
