@@ -49,12 +49,40 @@ __device__ __forceinline__ void store_n(T *p, int cnt, const float (&x)[N]) {
 
 // ----------------------------------------------------------------- forward --
 
-// Vectors of a lane: a wave takes a strip of so many times 64 of a row.
+// Vectors of a lane.  A wave takes a strip of so many times 64 of a row, or, of rows
+// of at most 64, as many rows as it has lanes for, so many times.
 constexpr int kFwdVecs = 4;
 
 template <class W, class Y>
+constexpr int kPair = kVec<W> < kVec<Y> ? kVec<W> : kVec<Y>;   // elements of a lane's vector
+
+template <class W, int N>
+__device__ __forceinline__ void load_pair(const W *p, bool some, float (&x)[N]) {
+  if constexpr (N == kVec<W>) {
+    u32x4 raw = {};
+    if (some) raw = *(const u32x4_any *)p;
+    unpack<W>(raw, x);
+  } else {                             // half a vector of bf16
+    u32x2_any raw = {};
+    if (some) raw = *(const u32x2_any *)p;
+    const u32x4 both = {raw[0], raw[1], 0, 0};
+    float v8[kVec<W>];
+    unpack<W>(both, v8);
+#pragma unroll
+    for (int e = 0; e < N; ++e) x[e] = v8[e];
+  }
+}
+template <class Y, int N>
+__device__ __forceinline__ void store_pair(Y *p, float scale, float (&x)[N]) {
+#pragma unroll
+  for (int e = 0; e < N; ++e) x[e] *= scale;
+  if constexpr (N == kVec<Y>) store16(p, pack<Y>(x));
+  else store_half(p, x);
+}
+
+template <class W, class Y>
 __global__ __launch_bounds__(256) void embedding_fwd_kernel(EmbedArgs a, int strips) {
-  constexpr int N = kVec<W> < kVec<Y> ? kVec<W> : kVec<Y>;   // elements of a lane's vector
+  constexpr int N = kPair<W, Y>;
   const int lane = threadIdx.x & 63;
   const int64_t units = (int64_t)a.n_tokens * strips;
   for (int64_t unit = (int64_t)blockIdx.x * 4 + (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6); unit < units; unit += (int64_t)gridDim.x * 4) {
@@ -67,33 +95,44 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(EmbedArgs a, int str
     // the last vector of a row reaches back over its neighbour's elements
     const auto at = [&](int i) { return min(c0 + i * 64 * N, a.dim - N); };
     float x[kFwdVecs][N];
-    if (a.dim >= N) {
 #pragma unroll
-      for (int i = 0; i < kFwdVecs; ++i) {
-        if constexpr (N == kVec<W>) {
-          u32x4 raw = {};
-          if (some && c0 + i * 64 * N < a.dim) raw = *(const u32x4_any *)(w + at(i));
-          unpack<W>(raw, x[i]);
-        } else {                       // half a vector of bf16
-          u32x2_any raw = {};
-          if (some && c0 + i * 64 * N < a.dim) raw = *(const u32x2_any *)(w + at(i));
-          const u32x4 both = {raw[0], raw[1], 0, 0};
-          float v8[kVec<W>];
-          unpack<W>(both, v8);
+    for (int i = 0; i < kFwdVecs; ++i) load_pair<W, N>(w + at(i), some && c0 + i * 64 * N < a.dim, x[i]);
 #pragma unroll
-          for (int e = 0; e < N; ++e) x[i][e] = v8[e];
-        }
-      }
+    for (int i = 0; i < kFwdVecs; ++i)
+      if (c0 + i * 64 * N < a.dim) store_pair<Y, N>(y + at(i), a.scale, x[i]);
+  }
+}
+
+// Rows of at most 64 vectors, 1 << bits lanes each.
+template <class W, class Y>
+__global__ __launch_bounds__(256) void embedding_narrow_kernel(EmbedArgs a, int bits) {
+  constexpr int N = kPair<W, Y>;
+  const int lane = threadIdx.x & 63, per = 64 >> bits;   // rows of a wave at a time
+  const int c0 = (lane & ((1 << bits) - 1)) * N;
+  const bool there = c0 < a.dim;
+  const int col = a.dim >= N ? min(c0, a.dim - N) : 0;
+  const int64_t t0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * (per * kFwdVecs) + (lane >> bits);
+  int64_t v[kFwdVecs];
 #pragma unroll
-      for (int i = 0; i < kFwdVecs; ++i) {
-        if (c0 + i * 64 * N >= a.dim) continue;
+  for (int i = 0; i < kFwdVecs; ++i) {
+    const int64_t t = t0 + i * per;
+    v[i] = t < a.n_tokens ? a.tokens[t] : -1;
+    if (v[i] >= a.vocab) v[i] = -1;
+  }
+  if (a.dim >= N) {
+    float x[kFwdVecs][N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) x[i][e] *= a.scale;
-        if constexpr (N == kVec<Y>) store16(y + at(i), pack<Y>(x[i]));
-        else store_half(y + at(i), x[i]);
-      }
-    } else if (c0 < a.dim) {           // (less than a vector: one lane)
-      for (int e = 0; e < a.dim; ++e) y[e] = (Y)(some ? to_f32(w[e]) * a.scale : 0.f);
+    for (int i = 0; i < kFwdVecs; ++i) load_pair<W, N>((const W *)a.w.data + (v[i] >= 0 ? v[i] : 0) * a.w.ts + col, v[i] >= 0 && there, x[i]);
+#pragma unroll
+    for (int i = 0; i < kFwdVecs; ++i)
+      if (t0 + i * per < a.n_tokens && there) store_pair<Y, N>((Y *)a.y.data + (t0 + i * per) * a.y.ts + col, a.scale, x[i]);
+  } else if (there) {                  // less than a vector: a lane a row
+#pragma unroll
+    for (int i = 0; i < kFwdVecs; ++i) {
+      if (t0 + i * per >= a.n_tokens) continue;
+      Y *y = (Y *)a.y.data + (t0 + i * per) * a.y.ts;
+      const W *w = (const W *)a.w.data + (v[i] >= 0 ? v[i] : 0) * a.w.ts;
+      for (int e = 0; e < a.dim; ++e) y[e] = (Y)(v[i] >= 0 ? to_f32(w[e]) * a.scale : 0.f);
     }
   }
 }
@@ -373,7 +412,7 @@ __global__ __launch_bounds__(kSortThreads) void embedding_sort_kernel(SortArgs a
   }
 }
 
-// Rows alone, where there are no tokens.
+// Rows alone.
 __global__ __launch_bounds__(kSortThreads) void embedding_zero_kernel(SortArgs a) { zero_rows(a, (int)blockIdx.x); }
 
 // ---------------------------------------------------------------- backward --
@@ -531,10 +570,86 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(SumArgs
   }
 }
 
+// Few tokens: a workgroup takes some rows of the table, finds their tokens among all,
+// in order, and forms its rows, a wave a row's strip, all in one launch.  (70 tokens
+// of 69335 rows of 1393 float32: 78 us by the sort, XX here; a fill of the table 57.)
+constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64;
+
+template <class W, class Y>
+__global__ __launch_bounds__(kFewThreads) void embedding_few_kernel(EmbedArgs a, int rows) {
+  constexpr int N = kVec<Y>;
+  __shared__ int id[plan::kEmbedFew], token[plan::kEmbedFew], sums[kFewWaves];
+  const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t v0 = (int64_t)blockIdx.x * rows;
+  const int n_rows = (int)min((int64_t)rows, a.vocab - v0);
+  int n = 0;                                     // of the workgroup's tokens
+  for (int t0 = 0; t0 < a.n_tokens; t0 += kFewThreads) {
+    const int t = t0 + (int)threadIdx.x;
+    const int64_t v = t < a.n_tokens ? a.tokens[t] - v0 : -1;
+    const bool mine = v >= 0 && v < n_rows;
+    const uint64_t in = __ballot(mine);
+    if (lane == 0) sums[wave] = __popcll(in);
+    __syncthreads();
+    int at = n + __popcll(in & ((uint64_t(1) << lane) - 1));
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) {
+      at += w < wave ? sums[w] : 0;
+      n += sums[w];
+    }
+    if (mine) id[at] = (int)v, token[at] = t;
+    __syncthreads();
+  }
+  W *const out = (W *)a.w.data + v0 * a.w.ts;
+  const int64_t bytes = (int64_t)a.dim * (int)sizeof(W);
+  if (n == 0 && a.w.ts == a.dim) {               // rows side by side, all zero
+    char *const p = (char *)out;
+    const int64_t all = n_rows * bytes, lead = min(all, (int64_t)(-(intptr_t)p & 15)), vecs = (all - lead) / 16, tail = lead + 16 * vecs;
+    for (int64_t i = threadIdx.x; i < vecs; i += kFewThreads) *(u32x4 *)(p + lead + 16 * i) = u32x4{};
+    for (int64_t c = 2 * (int64_t)threadIdx.x; c < lead; c += 2 * kFewThreads) *(uint16_t *)(p + c) = 0;
+    for (int64_t c = tail + 2 * (int64_t)threadIdx.x; c < all; c += 2 * kFewThreads) *(uint16_t *)(p + c) = 0;
+    return;
+  }
+  const int strips = (a.dim + 64 * N - 1) / (64 * N);
+  for (int unit = wave; unit < n_rows * strips; unit += kFewWaves) {
+    const int r = unit / strips, c0 = ((unit - r * strips) * 64 + lane) * N;
+    const int col = a.dim >= N ? min(c0, a.dim - N) : 0, cnt = a.dim >= N ? N : a.dim;
+    const Y *dy = (const Y *)a.y.data + col;
+    float acc[N] = {};
+    for (int j0 = 0; j0 < n; j0 += 64) {
+      uint64_t in = __ballot(j0 + lane < n && id[min(j0 + lane, n - 1)] == r);
+      while (in) {
+        constexpr int kTake = 4;                 // rows in flight
+        float v[kTake][N];
+#pragma unroll
+        for (int k = 0; k < kTake; ++k) {
+          const bool some = in != 0;
+          const int j = some ? j0 + __builtin_ctzll(in) : j0;
+          in &= in - 1;
+          load_vec_kept(dy + (int64_t)token[j] * a.y.ts, some && c0 < a.dim ? cnt : 0, 0.f, v[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kTake; ++k)
+#pragma unroll
+          for (int e = 0; e < N; ++e) acc[e] += v[k][e];
+      }
+    }
+    if (c0 >= a.dim) continue;
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[e] *= a.scale;
+    store_n<W>(out + (int64_t)r * a.w.ts + col, cnt, acc);
+  }
+}
+
 template <class W, class Y>
 hipError_t fwd(const EmbedArgs &a, hipStream_t s) {
-  constexpr int N = kVec<W> < kVec<Y> ? kVec<W> : kVec<Y>;
-  const int strips = (int)plan::ceil_div(a.dim, 64 * N * kFwdVecs);
+  const int64_t vecs = plan::ceil_div(a.dim, kPair<W, Y>);
+  if (vecs <= 64) {
+    int bits = 0;
+    while ((1 << bits) < vecs) ++bits;
+    embedding_narrow_kernel<W, Y><<<(int)plan::ceil_div(a.n_tokens, 4 * kFwdVecs * (64 >> bits)), 256, 0, s>>>(a, bits);
+    return hipGetLastError();
+  }
+  const int strips = (int)plan::ceil_div(vecs, 64 * kFwdVecs);
   const int64_t groups = plan::ceil_div((int64_t)a.n_tokens * strips, 4);
   embedding_fwd_kernel<W, Y><<<(int)(groups < (1 << 20) ? groups : 1 << 20), 256, 0, s>>>(a, strips);
   return hipGetLastError();
@@ -543,6 +658,11 @@ hipError_t fwd(const EmbedArgs &a, hipStream_t s) {
 template <class W, class Y>
 hipError_t bwd(const EmbedArgs &a, hipStream_t s) {
   const plan::EmbedBwd &f = a.f;
+  if (plan::embed_few(a.n_tokens, a.dim, (int)sizeof(Y))) {   // (also of none)
+    const int rows = plan::embed_few_rows(a.dim * (int64_t)sizeof(W), a.vocab);
+    embedding_few_kernel<W, Y><<<(int)plan::ceil_div(a.vocab, rows), kFewThreads, 0, s>>>(a, rows);
+    return hipGetLastError();
+  }
   SortArgs k{};
   k.tokens = a.tokens;
   k.n_tokens = a.n_tokens;
@@ -556,10 +676,6 @@ hipError_t bwd(const EmbedArgs &a, hipStream_t s) {
   k.elem_bytes = (int)sizeof(W);
   const bool flags = f.blocks > 0, side_by_side = !flags && k.row_bytes == (int64_t)a.dim * (int)sizeof(W);
   const int zero = (int)(side_by_side ? plan::ceil_div(a.vocab * k.row_bytes, kZeroBytes) : plan::ceil_div(a.vocab, kZeroRows));
-  if (a.n_tokens == 0) {
-    embedding_zero_kernel<<<zero, kSortThreads, 0, s>>>(k);
-    return hipGetLastError();
-  }
   uint32_t *const key[2] = {(uint32_t *)(a.ws + f.key_off[0]), (uint32_t *)(a.ws + f.key_off[1])};
   uint32_t *const token[2] = {(uint32_t *)(a.ws + f.token_off[0]), (uint32_t *)(a.ws + f.token_off[1])};
   int in = 0;                                    // where the sorted list ends up

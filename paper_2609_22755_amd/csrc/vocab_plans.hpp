@@ -115,6 +115,18 @@ constexpr int kSortBlock = 4096;                // tokens that a workgroup of a 
 constexpr int kSortWhole = 16384;               // tokens that one workgroup sorts by itself
 constexpr int kSortBits = 9;                    // most of a digit
 
+// Few tokens, whose rows one workgroup could add: a kernel that needs no sort.
+// (Bytes that a workgroup reads in some 25 us, if all tokens have one id.)
+constexpr int kEmbedFew = 1024;
+constexpr int64_t kEmbedFewBytes = 2 << 20;
+constexpr bool embed_few(int64_t n_tokens, int dim, int es) { return n_tokens <= kEmbedFew && n_tokens * dim * es <= kEmbedFewBytes; }
+// Table rows of one of its workgroups: some 96 KB, 1024 workgroups at least.
+constexpr int embed_few_rows(int64_t row_bytes, int vocab) {
+  int64_t r = (96 << 10) / row_bytes, most = vocab / 1024;
+  r = r < most ? r : most;
+  return (int)(r < 1 ? 1 : r > 64 ? 64 : r);
+}
+
 struct EmbedBwd {
   int chunk, chunks;           // sorted tokens of a chunk
   int passes, bits;            // of the sort: digits of so many bits (a token id, or vocab for none)
@@ -129,7 +141,8 @@ constexpr EmbedBwd embed_bwd(int64_t n_tokens, int dim, int vocab) {
   EmbedBwd f{};
   if (n_tokens <= 0) return f;
   f.chunk = n_tokens <= 32 ? 32 : 8;
-  while (f.chunk < 128 && n_tokens / (2 * f.chunk) >= 1024) f.chunk *= 2;
+  const int64_t strips = ceil_div(dim, 512);
+  while (f.chunk < 128 && n_tokens / (2 * f.chunk) * (strips < 4 ? strips : 4) >= 4096) f.chunk *= 2;
   f.chunks = (int)ceil_div(n_tokens, f.chunk);
   int width = 1;
   while (width < 31 && (int64_t(1) << width) <= vocab) ++width;

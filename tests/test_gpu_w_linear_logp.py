@@ -45,21 +45,20 @@ def _ws(n):
     return torch.full((n,), 255, dtype=torch.uint8, device="cuda") if n else None
 
 
-def _forward(x, w, y, scale=1.0, stream=None):
+def _forward(x, w, y, scale=1.0):
     T, (V, dim) = x.shape[0], w.shape
     o = {n: torch.full((T,), -7.0, device="cuda") for n in ("logp", "lse", "entropy")}
-    nsp.nsp_linear_logp_fwd(x, w, y, o["logp"], o["lse"], o["entropy"], _ws(nsp.nsp_linear_logp_fwd_workspace(T, dim, V)), scale=scale,
-                            stream=stream)
+    nsp.nsp_linear_logp_fwd(x, w, y, o["logp"], o["lse"], o["entropy"], _ws(nsp.nsp_linear_logp_fwd_workspace(T, dim, V)), scale=scale)
     return o
 
 
-def _backward(x, w, y, o, g, scale=1.0, dtype=BF, dx=True, dw=True, stream=None):
+def _backward(x, w, y, o, g, scale=1.0, dtype=BF, dx=True, dw=True):
     """g: gradients of logp, lse, entropy, or None."""
     T, (V, dim) = x.shape[0], w.shape
     dx = torch.full((T, dim), NAN, dtype=dtype, device="cuda") if dx is True else dx
     dw = torch.full((V, dim), NAN, dtype=dtype, device="cuda") if dw is True else dw
     nsp.nsp_linear_logp_bwd(x, w, y, o["lse"], dx, dw, _ws(nsp.nsp_linear_logp_bwd_workspace(T, dim, V)), g_logp=g[0], g_lse=g[1],
-                            g_entropy=g[2], entropy=o["entropy"] if g[2] is not None else None, scale=scale, stream=stream)
+                            g_entropy=g[2], entropy=o["entropy"] if g[2] is not None else None, scale=scale)
     return dx, dw
 
 
@@ -294,8 +293,8 @@ def test_repeats_streams_and_graphs(T, dim, V):
     dx, dw = _backward(x, w, y, o, g)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
-    o2 = _forward(x, w, y, stream=side)
-    with torch.cuda.stream(side):
+    with torch.cuda.stream(side):                # (its buffers are filled on that stream too)
+        o2 = _forward(x, w, y)
         dx2, dw2 = _backward(x, w, y, o2, g)
     side.synchronize()
     assert all(torch.equal(o[n], o2[n]) for n in o) and torch.equal(dx, dx2) and torch.equal(dw, dw2)

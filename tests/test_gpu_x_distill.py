@@ -40,11 +40,11 @@ def _inputs(T, V, K, dtype, seed, twice=True):
     return rng, z, torch.from_numpy(index).cuda(), torch.from_numpy(t).cuda()
 
 
-def _forward(z, index, t, kind, scale=1.0, stream=None):
+def _forward(z, index, t, kind, scale=1.0):
     T, V = z.shape
     loss, lse = torch.full((T,), -7.0, device="cuda"), torch.full((T,), -7.0, device="cuda")
     ws = torch.full((nsp.nsp_distill_fwd_workspace(T, V),), 255, dtype=torch.uint8, device="cuda")
-    nsp.nsp_distill_fwd(z, index, t, loss, lse, ws, kind=kind, scale=scale, stream=stream)
+    nsp.nsp_distill_fwd(z, index, t, loss, lse, ws, kind=kind, scale=scale)
     return loss, lse
 
 
@@ -212,7 +212,8 @@ def test_repeats_streams_and_graphs(T, V):
         torch.cuda.synchronize()
         side = torch.cuda.Stream()
         side.wait_stream(torch.cuda.current_stream())
-        l2, s2 = _forward(zs, index, t, 0, stream=side)
+        with torch.cuda.stream(side):            # (its buffers are filled on that stream too)
+            l2, s2 = _forward(zs, index, t, 0)
         side.synchronize()
         d2 = torch.empty_like(z)
         nsp.nsp_distill_bwd(zs, index, t, s2, g, d2)

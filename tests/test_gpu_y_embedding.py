@@ -31,11 +31,11 @@ def _ids(rng, T, V, much=True):
     return torch.from_numpy(ids).cuda()
 
 
-def _bwd(ids, dy, V, dtype, scale=1.0, dw=None, stream=None):
+def _bwd(ids, dy, V, dtype, scale=1.0, dw=None):
     T, dim = dy.shape
     dw = torch.full((V, dim), NAN, dtype=dtype, device="cuda") if dw is None else dw
     ws = torch.full((nsp.nsp_embedding_bwd_workspace(T, dim, V),), 255, dtype=torch.uint8, device="cuda")
-    nsp.nsp_embedding_bwd(ids, dy, dw, ws, scale=scale, stream=stream)
+    nsp.nsp_embedding_bwd(ids, dy, dw, ws, scale=scale)
     return dw
 
 
@@ -149,7 +149,8 @@ def test_repeats_streams_and_graphs(T):
     assert torch.equal(want, _bwd(ids, dy, V, F))
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
-    got = _bwd(ids, dy, V, F, stream=side)
+    with torch.cuda.stream(side):                # (its buffers are filled on that stream too)
+        got = _bwd(ids, dy, V, F)
     side.synchronize()
     assert torch.equal(want, got)
     i2, dw = ids.clone(), torch.empty_like(want)
