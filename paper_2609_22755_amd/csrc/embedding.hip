@@ -455,16 +455,27 @@ __device__ __forceinline__ void kept(const float *from, int cnt, float (&x)[N]) 
   }
 }
 
-// A chunk's sums of a strip, by a wave.
-template <class W, class Y>
-__global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs s) {
+// A chunk's sums of a strip, by a wave; NARROW: of rows of at most 32 vectors, by
+// 1 << bits lanes.  EARLY: the next rows are on their way while these are added: for
+// few waves (5003 x 1111 float32 44 us instead of 50); many of them get in each
+// other's way in memory (262144 x 4096 850 us instead of 680).
+template <class W, class Y, bool NARROW, bool EARLY>
+__global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs s, int bits) {
   constexpr int N = kVec<Y>;
   const EmbedArgs &a = s.a;
   const int lane = threadIdx.x & 63;
   const int64_t unit = (int64_t)blockIdx.x * 4 + (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int chunk = (int)(unit / s.strips), strip = (int)(unit - (int64_t)chunk * s.strips);
-  if (chunk >= a.f.chunks) return;
-  const int c0 = (strip * 64 + lane) * N;
+  int chunk, c0;
+  if constexpr (NARROW) {
+    const int64_t at = (unit << (6 - bits)) + (lane >> bits);
+    if (at >= a.f.chunks) return;
+    chunk = (int)at;
+    c0 = (lane & ((1 << bits) - 1)) * N;
+  } else {
+    chunk = (int)(unit / s.strips);
+    if (chunk >= a.f.chunks) return;
+    c0 = ((int)(unit - (int64_t)chunk * s.strips) * 64 + lane) * N;
+  }
   const int col = a.dim >= N ? min(c0, a.dim - N) : 0, cnt = a.dim >= N ? N : a.dim;
   const bool there = c0 < a.dim;
   const int lo = chunk * a.f.chunk, hi = min(lo + a.f.chunk, a.n_tokens);
@@ -488,51 +499,54 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs s) {
 #pragma unroll
     for (int e = 0; e < N; ++e) acc[e] = 0.f;
   };
-  for (int p = lo; p < hi; p += kAhead) {
-    u32x4 raw[kAhead];
-    float few[N];
-    uint32_t ids[kAhead];
-    if (a.dim >= N) {
+  u32x4 raw[kAhead];
+  uint32_t ids[kAhead];
+  const auto fetch = [&](int p) {
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) {
-        const int at = min(p + i, hi - 1);
-        ids[i] = s.key[at];
-        raw[i] = u32x4{};
-        if (there && p + i < hi && ids[i] < (uint32_t)a.vocab) raw[i] = load16(dy + (int64_t)s.token[at] * a.y.ts);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) ids[i] = s.key[min(p + i, hi - 1)];
+    for (int i = 0; i < kAhead; ++i) {
+      const int at = min(p + i, hi - 1);
+      ids[i] = s.key[at];
+      raw[i] = u32x4{};
+      if (a.dim >= N && there && p + i < hi && ids[i] < (uint32_t)a.vocab) raw[i] = load16(dy + (int64_t)s.token[at] * a.y.ts);
     }
+  };
+  fetch(lo);
+  for (int p = lo; p < hi; p += kAhead) {
+    u32x4 now[kAhead];
+    uint32_t now_id[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) now[i] = raw[i], now_id[i] = ids[i];
+    if (EARLY && p + kAhead < hi) fetch(p + kAhead);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
       if (p + i >= hi) break;
-      if (ids[i] != id) {
+      if (now_id[i] != id) {
         end(false);
-        id = ids[i];
+        id = now_id[i];
       }
-      if (a.dim >= N) {
-        unpack<Y>(raw[i], few);
-      } else {
-        load_some(dy + (int64_t)s.token[p + i] * a.y.ts, there && id < (uint32_t)a.vocab ? cnt : 0, 0.f, few);
-      }
+      float v[N];
+      if (a.dim >= N) unpack<Y>(now[i], v);
+      else load_some(dy + (int64_t)s.token[p + i] * a.y.ts, there && id < (uint32_t)a.vocab ? cnt : 0, 0.f, v);
 #pragma unroll
-      for (int e = 0; e < N; ++e) acc[e] += few[e];
+      for (int e = 0; e < N; ++e) acc[e] += v[e];
     }
+    if (!EARLY && p + kAhead < hi) fetch(p + kAhead);
   }
   end(hi < a.n_tokens && s.key[hi] == id);
 }
 
-// The rows of an id that goes over several chunks: a workgroup a chunk that one
-// begins in, a wave a strip.
+// The rows of an id that goes over several chunks: a wave a strip and chunk that one
+// begins in.
 constexpr int kJoinWaves = 8, kJoinAhead = 8;
 template <class W, class Y>
 __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(SumArgs s) {
   constexpr int N = kVec<Y>;
   const EmbedArgs &a = s.a;
-  const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int chunk = (int)blockIdx.x;
-  const int lo = chunk * a.f.chunk, hi = lo + a.f.chunk;    // (never the last chunk)
+  const int lane = threadIdx.x & 63;
+  const int64_t unit = (int64_t)blockIdx.x * kJoinWaves + (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int chunk = (int)(unit / s.strips), strip = (int)(unit - (int64_t)chunk * s.strips);
+  if (chunk >= a.f.chunks - 1) return;
+  const int lo = chunk * a.f.chunk, hi = lo + a.f.chunk;
   const uint32_t id = s.key[hi - 1];
   if (id >= (uint32_t)a.vocab || s.key[hi] != id) return;
   if (s.key[lo] == id && lo > 0 && s.key[lo - 1] == id) return;   // it began before
@@ -545,29 +559,25 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(SumArgs
     more += run;
     all = run == 64;
   }
-  for (int strip = wave; strip < s.strips; strip += kJoinWaves) {
-    const int c0 = (strip * 64 + lane) * N;
-    if (c0 >= a.dim) continue;
-    const int col = a.dim >= N ? min(c0, a.dim - N) : 0, cnt = a.dim >= N ? N : a.dim;
-    // the tail of this chunk, then the heads of those after it
-    const float *head = s.part + (int64_t)chunk * 2 * a.dim + col;
-    float acc[N];
-    kept(head + a.dim, cnt, acc);
-    for (int i0 = 1; i0 <= more; i0 += kJoinAhead) {
-      float v[kJoinAhead][N];
+  const int c0 = (strip * 64 + lane) * N;
+  if (c0 >= a.dim) return;
+  const int col = a.dim >= N ? min(c0, a.dim - N) : 0, cnt = a.dim >= N ? N : a.dim;
+  // the tail of this chunk, then the heads of those after it
+  const float *head = s.part + (int64_t)chunk * 2 * a.dim + col;
+  float acc[N];
+  kept(head + a.dim, cnt, acc);
+  for (int i0 = 1; i0 <= more; i0 += kJoinAhead) {
+    float v[kJoinAhead][N];
 #pragma unroll
-      for (int j = 0; j < kJoinAhead; ++j) {
-        if (i0 + j <= more) kept(head + (int64_t)(i0 + j) * 2 * a.dim, cnt, v[j]);
-      }
+    for (int j = 0; j < kJoinAhead; ++j) kept(head + (int64_t)min(i0 + j, more) * 2 * a.dim, cnt, v[j]);
 #pragma unroll
-      for (int j = 0; j < kJoinAhead; ++j)
+    for (int j = 0; j < kJoinAhead; ++j)
 #pragma unroll
-        for (int e = 0; e < N; ++e) acc[e] += i0 + j <= more ? v[j][e] : 0.f;
-    }
-#pragma unroll
-    for (int e = 0; e < N; ++e) acc[e] *= a.scale;
-    store_n<W>((W *)a.w.data + (int64_t)id * a.w.ts + col, cnt, acc);
+      for (int e = 0; e < N; ++e) acc[e] += i0 + j <= more ? v[j][e] : 0.f;
   }
+#pragma unroll
+  for (int e = 0; e < N; ++e) acc[e] *= a.scale;
+  store_n<W>((W *)a.w.data + (int64_t)id * a.w.ts + col, cnt, acc);
 }
 
 // Few tokens: a workgroup takes some rows of the table, finds their tokens among all,
@@ -618,19 +628,33 @@ __global__ __launch_bounds__(kFewThreads) void embedding_few_kernel(EmbedArgs a,
     for (int j0 = 0; j0 < n; j0 += 64) {
       uint64_t in = __ballot(j0 + lane < n && id[min(j0 + lane, n - 1)] == r);
       while (in) {
-        constexpr int kTake = 4;                 // rows in flight
-        float v[kTake][N];
+        int at[kAhead], some = 0;                // as many in flight; the last again where there are fewer
 #pragma unroll
-        for (int k = 0; k < kTake; ++k) {
-          const bool some = in != 0;
-          const int j = some ? j0 + __builtin_ctzll(in) : j0;
+        for (int k = 0; k < kAhead; ++k) {
+          at[k] = in ? token[j0 + __builtin_ctzll(in)] : at[k > 0 ? k - 1 : 0];
+          some += in != 0;
           in &= in - 1;
-          load_vec_kept(dy + (int64_t)token[j] * a.y.ts, some && c0 < a.dim ? cnt : 0, 0.f, v[k]);
         }
+        if (a.dim >= N) {
+          u32x4 raw[kAhead];
 #pragma unroll
-        for (int k = 0; k < kTake; ++k)
+          for (int k = 0; k < kAhead; ++k) raw[k] = *(const u32x4_any *)(dy + (int64_t)at[k] * a.y.ts);
 #pragma unroll
-          for (int e = 0; e < N; ++e) acc[e] += v[k][e];
+          for (int k = 0; k < kAhead; ++k) {
+            if (k >= some) break;
+            float v[N];
+            unpack<Y>(raw[k], v);
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc[e] += v[e];
+          }
+        } else {
+          for (int k = 0; k < some; ++k) {
+            float v[N];
+            load_some(dy + (int64_t)at[k] * a.y.ts, cnt, 0.f, v);
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc[e] += v[e];
+          }
+        }
       }
     }
     if (c0 >= a.dim) continue;
@@ -721,10 +745,15 @@ hipError_t bwd(const EmbedArgs &a, hipStream_t s) {
   r.token = token[in];
   r.part = (float *)(a.ws + f.part_off);
   r.strips = (int)plan::ceil_div(a.dim, 64 * kVec<Y>);
-  embedding_sum_kernel<W, Y><<<(int)plan::ceil_div((int64_t)f.chunks * r.strips, 4), 256, 0, s>>>(r);
+  int bits = 0;
+  while ((1 << bits) < plan::ceil_div(a.dim, kVec<Y>)) ++bits;
+  const int64_t waves = (int64_t)f.chunks * r.strips;
+  if (bits < 6) embedding_sum_kernel<W, Y, true, true><<<(int)plan::ceil_div(f.chunks, 4 * (64 >> bits)), 256, 0, s>>>(r, bits);
+  else if (waves <= 8192) embedding_sum_kernel<W, Y, false, true><<<(int)plan::ceil_div(waves, 4), 256, 0, s>>>(r, bits);
+  else embedding_sum_kernel<W, Y, false, false><<<(int)plan::ceil_div(waves, 4), 256, 0, s>>>(r, bits);
   e = hipGetLastError();
   if (e != hipSuccess || f.chunks == 1) return e;
-  embedding_join_kernel<W, Y><<<f.chunks - 1, 64 * kJoinWaves, 0, s>>>(r);
+  embedding_join_kernel<W, Y><<<(int)plan::ceil_div((f.chunks - 1) * (int64_t)r.strips, kJoinWaves), 64 * kJoinWaves, 0, s>>>(r);
   return hipGetLastError();
 }
 

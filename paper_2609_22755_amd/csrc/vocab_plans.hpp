@@ -116,13 +116,15 @@ constexpr int kSortWhole = 16384;               // tokens that one workgroup sor
 constexpr int kSortBits = 9;                    // most of a digit
 
 // Few tokens, whose rows one workgroup could add: a kernel that needs no sort.
-// (Bytes that a workgroup reads in some 25 us, if all tokens have one id.)
-constexpr int kEmbedFew = 1024;
-constexpr int64_t kEmbedFewBytes = 2 << 20;
+// (At most what one reads in some 10 us, if all tokens have one id.  With and without
+// a sort: 24 x 512 of 3000 rows 15.4 and 7.9 us, 400 x 512 14.6 and 8.1, 200 x 2048 of
+// 32000 30.8 and 22.6, 400 x 2048 31.0 and 33.6, 1000 x 512 of 3000 15.4 and 17.3.)
+constexpr int kEmbedFew = 512;
+constexpr int64_t kEmbedFewBytes = 1 << 20;
 constexpr bool embed_few(int64_t n_tokens, int dim, int es) { return n_tokens <= kEmbedFew && n_tokens * dim * es <= kEmbedFewBytes; }
-// Table rows of one of its workgroups: some 96 KB, 1024 workgroups at least.
+// Table rows of one of its workgroups: some 32 KB, 1024 workgroups at least.
 constexpr int embed_few_rows(int64_t row_bytes, int vocab) {
-  int64_t r = (96 << 10) / row_bytes, most = vocab / 1024;
+  int64_t r = (32 << 10) / row_bytes, most = vocab / 1024;
   r = r < most ? r : most;
   return (int)(r < 1 ? 1 : r > 64 ? 64 : r);
 }
@@ -135,14 +137,15 @@ struct EmbedBwd {
 };
 // A chunk's sorted tokens are summed by one wave a strip of columns; what a
 // token's rows come to in a chunk they do not end in is kept in float32.  Longer
-// chunks keep less (two rows each), shorter ones leave more waves; one chunk needs
-// no second kernel.
+// chunks keep less (two rows each) and leave the joining wave of a frequent id fewer
+// (of an id with a twelfth of the tokens, which is what the most frequent ones have:
+// 100, of narrow rows 500); shorter ones leave more waves, and one chunk needs no
+// second kernel.
 constexpr EmbedBwd embed_bwd(int64_t n_tokens, int dim, int vocab) {
   EmbedBwd f{};
   if (n_tokens <= 0) return f;
   f.chunk = n_tokens <= 32 ? 32 : 8;
-  const int64_t strips = ceil_div(dim, 512);
-  while (f.chunk < 128 && n_tokens / (2 * f.chunk) * (strips < 4 ? strips : 4) >= 4096) f.chunk *= 2;
+  while (f.chunk < 128 && n_tokens > (dim < 512 ? 6250 : 1250) * (int64_t)f.chunk) f.chunk *= 2;
   f.chunks = (int)ceil_div(n_tokens, f.chunk);
   int width = 1;
   while (width < 31 && (int64_t(1) << width) <= vocab) ++width;
