@@ -154,6 +154,7 @@ struct SortArgs {
   char *dw;                    // rows to be zeroed by the workgroups past the blocks
   int64_t row_bytes;
   int32_t row_elems, elem_bytes;
+  int32_t groups;              // of zero_rows
 };
 
 __device__ __forceinline__ uint32_t key_of(int64_t token, int vocab) { return token >= 0 && token < vocab ? (uint32_t)token : (uint32_t)vocab; }
@@ -165,8 +166,9 @@ __device__ __forceinline__ uint32_t key_of(int64_t token, int vocab) { return to
 // that lie side by side and are all zeroed go as one, 256 KB a workgroup.
 constexpr int kZeroRows = 64;
 constexpr int64_t kZeroBytes = 256 << 10;
+constexpr int kZeroGrid = 1 << 20;               // (a launch holds less than 2^32 threads)
 
-__device__ __forceinline__ void zero_rows(const SortArgs &a, int64_t group) {
+__device__ __forceinline__ void zero_group(const SortArgs &a, int64_t group) {
   const int64_t bytes = (int64_t)a.row_elems * a.elem_bytes;
   if (!a.flags && a.row_bytes == bytes) {
     const int64_t all = a.vocab * bytes, lead = min(all, (int64_t)(-(intptr_t)a.dw & 15)), vecs = (all - lead) / 16;
@@ -194,6 +196,11 @@ __device__ __forceinline__ void zero_rows(const SortArgs &a, int64_t group) {
       for (int64_t c = 2 * at; c < bytes; c += 2 * lanes) *(uint16_t *)(w + c) = 0;
     }
   }
+}
+
+// By workgroup `first` of `n`.
+__device__ __forceinline__ void zero_rows(const SortArgs &a, int first, int n) {
+  for (int g = first; g < a.groups; g += n) zero_group(a, g);
 }
 
 // How many of a block's keys have each digit.
@@ -300,7 +307,7 @@ __global__ __launch_bounds__(kSortThreads) void embedding_move_kernel(SortArgs a
   __shared__ uint32_t counts[kSortWaves][kMaxBins];
   __shared__ uint32_t sums[2][kMaxBins], sh[kSortWaves];
   if ((int)blockIdx.x >= a.blocks) {
-    zero_rows(a, (int)blockIdx.x - a.blocks);
+    zero_rows(a, (int)blockIdx.x - a.blocks, (int)gridDim.x - a.blocks);
     return;
   }
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, n_bins = 1 << a.bits;
@@ -367,7 +374,7 @@ __global__ __launch_bounds__(kSortThreads) void embedding_sort_kernel(SortArgs a
   __shared__ uint32_t keys[R * kSortThreads], places[R * kSortThreads], sh[kSortWaves];
   __shared__ uint16_t counts[kSortWaves][kMaxBins];
   if (blockIdx.x > 0) {
-    zero_rows(a, (int)blockIdx.x - 1);
+    zero_rows(a, (int)blockIdx.x - 1, (int)gridDim.x - 1);
     return;
   }
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, n_bins = 1 << a.bits;
@@ -413,7 +420,7 @@ __global__ __launch_bounds__(kSortThreads) void embedding_sort_kernel(SortArgs a
 }
 
 // Rows alone.
-__global__ __launch_bounds__(kSortThreads) void embedding_zero_kernel(SortArgs a) { zero_rows(a, (int)blockIdx.x); }
+__global__ __launch_bounds__(kSortThreads) void embedding_zero_kernel(SortArgs a) { zero_rows(a, (int)blockIdx.x, (int)gridDim.x); }
 
 // ---------------------------------------------------------------- backward --
 
@@ -595,8 +602,8 @@ __global__ __launch_bounds__(kFewThreads) void embedding_few_kernel(EmbedArgs a,
   int n = 0;                                     // of the workgroup's tokens
   for (int t0 = 0; t0 < a.n_tokens; t0 += kFewThreads) {
     const int t = t0 + (int)threadIdx.x;
-    const int64_t v = t < a.n_tokens ? a.tokens[t] - v0 : -1;
-    const bool mine = v >= 0 && v < n_rows;
+    const uint64_t v = t < a.n_tokens ? (uint64_t)a.tokens[t] - (uint64_t)v0 : ~uint64_t(0);
+    const bool mine = v < (uint64_t)n_rows;
     const uint64_t in = __ballot(mine);
     if (lane == 0) sums[wave] = __popcll(in);
     __syncthreads();
@@ -699,7 +706,8 @@ hipError_t bwd(const EmbedArgs &a, hipStream_t s) {
   k.row_elems = a.dim;
   k.elem_bytes = (int)sizeof(W);
   const bool flags = f.blocks > 0, side_by_side = !flags && k.row_bytes == (int64_t)a.dim * (int)sizeof(W);
-  const int zero = (int)(side_by_side ? plan::ceil_div(a.vocab * k.row_bytes, kZeroBytes) : plan::ceil_div(a.vocab, kZeroRows));
+  k.groups = (int)(side_by_side ? plan::ceil_div(a.vocab * k.row_bytes, kZeroBytes) : plan::ceil_div(a.vocab, kZeroRows));
+  const int zero = k.groups < kZeroGrid ? k.groups : kZeroGrid;
   uint32_t *const key[2] = {(uint32_t *)(a.ws + f.key_off[0]), (uint32_t *)(a.ws + f.key_off[1])};
   uint32_t *const token[2] = {(uint32_t *)(a.ws + f.token_off[0]), (uint32_t *)(a.ws + f.token_off[1])};
   int in = 0;                                    // where the sorted list ends up

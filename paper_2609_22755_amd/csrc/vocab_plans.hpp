@@ -30,9 +30,15 @@ constexpr int linear_tile(int64_t n_tokens, int vocab) {
   return 56 * half < 100 * whole ? 128 : 256;
 }
 
-// Tokens of the forward that are worked on together: their statistics per tile
-// of the vocabulary (16 bytes) stay below some hundred MB.
+// Tokens of the forward that are worked on together, at most: 16 bytes are kept of each
+// and tile of the vocabulary (256 MB at 131072 rows).  Fewer of large vocabularies: 1 GB,
+// but 4096 tokens at least.
 constexpr int64_t kLinearPanel = 32768;
+constexpr int64_t linear_panel(int64_t tiles_p) {
+  int64_t n = kLinearPanel;
+  while (n > 4096 && n * tiles_p > (int64_t(1) << 26)) n /= 2;
+  return n;
+}
 
 struct LinearFwd {
   int tile;
@@ -43,8 +49,9 @@ struct LinearFwd {
 constexpr LinearFwd linear_fwd(int64_t n_tokens, int vocab) {
   LinearFwd f{};
   f.tile = linear_tile(n_tokens, vocab);
-  f.panel = n_tokens < kLinearPanel ? round_up(n_tokens, f.tile) : kLinearPanel;
   f.tiles_p = ceil_div(vocab, kTileP);
+  f.panel = linear_panel(f.tiles_p);
+  if (n_tokens < f.panel) f.panel = round_up(n_tokens, f.tile);
   f.part_off = 0;
   f.target_off = pad256((size_t)f.tiles_p * f.panel * 16);
   f.bytes = f.target_off + pad256((size_t)f.panel * 4);
@@ -122,11 +129,14 @@ constexpr int kSortBits = 9;                    // most of a digit
 constexpr int kEmbedFew = 512;
 constexpr int64_t kEmbedFewBytes = 1 << 20;
 constexpr bool embed_few(int64_t n_tokens, int dim, int es) { return n_tokens <= kEmbedFew && n_tokens * dim * es <= kEmbedFewBytes; }
-// Table rows of one of its workgroups: some 32 KB, 1024 workgroups at least.
+// Table rows of one of its workgroups: some 32 KB, 1024 workgroups at least, and
+// 2^22 at most (a launch holds less than 2^32 threads).
 constexpr int embed_few_rows(int64_t row_bytes, int vocab) {
   int64_t r = (32 << 10) / row_bytes, most = vocab / 1024;
+  const int64_t least = ceil_div(vocab, 1 << 22);
   r = r < most ? r : most;
-  return (int)(r < 1 ? 1 : r > 64 ? 64 : r);
+  r = r > 64 ? 64 : r;
+  return (int)(r < least ? least : r < 1 ? 1 : r);
 }
 
 struct EmbedBwd {

@@ -61,9 +61,9 @@ static int64_t pick(int64_t n) { return (int64_t)(g_rng() % (uint64_t)n); }
 static void linear_plans(int64_t T, int dim, int V) {
   const plan::LinearFwd f = plan::linear_fwd(T, V);
   CHECK(f.tile == 32 || f.tile == 64 || f.tile == 128 || f.tile == 256);
-  CHECK(f.panel >= T || f.panel == plan::kLinearPanel);
+  CHECK(f.panel >= T || f.panel == plan::linear_panel(f.tiles_p));
   CHECK(f.panel % f.tile == 0 && f.tiles_p * plan::kTileP >= V);
-  CHECK(f.tiles_p * (f.panel / f.tile) < INT32_MAX - 8);
+  CHECK((f.tiles_p * (f.panel / f.tile) + 8) * 512 < int64_t(1) << 32);   // threads of a launch
   CHECK(f.target_off >= (size_t)(f.tiles_p * f.panel * 16) && f.bytes >= f.target_off + (size_t)f.panel * 4);
   const plan::LinearBwd b = plan::linear_bwd(T, dim, V);
   CHECK(b.rows >= T && b.rows % b.tile == 0 && b.rows < T + b.tile);
@@ -75,7 +75,7 @@ static void linear_plans(int64_t T, int dim, int V) {
   CHECK(b.split_x == 1 || b.piece / b.split_x >= 256);
   CHECK(b.split_w == 1 || T / b.split_w >= 256);
   const int64_t cols = plan::ceil_div(dim, plan::kTileP);
-  CHECK(b.piece / plan::kTileP * (b.rows / b.tile) < INT32_MAX - 8);
+  CHECK((b.piece / plan::kTileP * (b.rows / b.tile) + 8) * 512 < int64_t(1) << 32);
   CHECK(cols * plan::ceil_div(b.rows, b.tile_x) * b.split_x + cols * (b.piece / plan::kTileP) * b.split_w < INT32_MAX - 16);
   // one after another, none over the next
   const size_t off[] = {b.count_off, b.order_off, b.place_off, b.coef_off, b.target_off, b.x_off, b.dl_off, b.sum_x_off, b.sum_w_off, b.bytes};
@@ -101,7 +101,7 @@ static void embed_plans(int64_t T, int dim, int V) {
   CHECK(f.bytes >= f.part_off + (f.chunks > 1 ? (size_t)f.chunks * 2 * dim * 4 : 0));
   if (plan::embed_few(T, dim, 4)) CHECK(T <= plan::kEmbedFew);
   const int rows = plan::embed_few_rows((int64_t)dim * 4, V);
-  CHECK(rows >= 1 && rows <= 64);
+  CHECK(rows >= 1 && rows <= 256 && plan::ceil_div(V, rows) * 512 < int64_t(1) << 32);
 }
 
 static nsp_rows rows_at(uintptr_t at, int64_t stride) { return nsp_rows{reinterpret_cast<void *>(at), stride, 0}; }
