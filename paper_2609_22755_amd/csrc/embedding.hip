@@ -5,7 +5,8 @@
 // Bound by HBM: the forward reads a row and writes one a token, the backward reads
 // one a token and writes every row of the table.
 //
-// Backward: the tokens are sorted by their ids, stably (counting sort, digit by
+// Backward, of few tokens: zeros everywhere, then a kernel whose workgroups find the
+// tokens of an id among all.  Of more: the tokens are sorted by their ids, stably (counting sort, digit by
 // digit), so that a row's tokens lie side by side in their order and every sum has
 // a fixed order, without an atomic on data.  A wave takes a chunk of the sorted list
 // and a strip of columns, adds rows as long as the id stays the same and stores each
@@ -163,22 +164,37 @@ __device__ __forceinline__ uint32_t key_of(int64_t token, int vocab) { return to
 // them: 64 neighbours a workgroup, as many lanes a row as it has vectors, so that
 // the chip writes in the order of the addresses (131072 rows of 8 KB: 6.3 TB/s, with
 // resident workgroups that step over the table 5.1; a fill of the same 6.8).  Rows
-// that lie side by side and are all zeroed go as one, 256 KB a workgroup.
+// that lie side by side and are all zeroed go as one, 256 KB a workgroup: beside the
+// sort's LDS few workgroups are resident (50021 x 1111 float32 56 us in all, by 16 KB 76).
 constexpr int kZeroRows = 64;
 constexpr int64_t kZeroBytes = 256 << 10;
 constexpr int kZeroGrid = 1 << 20;               // (a launch holds less than 2^32 threads)
 
+// Zeros by THREADS threads, whole lines of 128 bytes.
+template <int THREADS>
+__device__ __forceinline__ void zero_bytes(char *p, int64_t bytes) {
+  const int64_t lead = min(bytes, (int64_t)(-(intptr_t)p & 127)), vecs = (bytes - lead) / 16, tail = lead + 16 * vecs;
+  for (int64_t i = threadIdx.x; i < vecs; i += THREADS) *(u32x4 *)(p + lead + 16 * i) = u32x4{};
+  const int c = 2 * (int)threadIdx.x;
+  if (c < lead) *(uint16_t *)(p + c) = 0;
+  if (tail + c < bytes) *(uint16_t *)(p + tail + c) = 0;
+}
+// A row by `lanes` of them.
+__device__ __forceinline__ void zero_row(char *w, int64_t bytes, int at, int lanes) {
+  if (bytes >= 16) {                             // the last vector reaches back
+    for (int64_t c = 16 * at; c < bytes; c += 16 * lanes) *(u32x4_any *)(w + min(c, bytes - 16)) = u32x4{};
+  } else {
+    for (int64_t c = 2 * at; c < bytes; c += 2 * lanes) *(uint16_t *)(w + c) = 0;
+  }
+}
+
 __device__ __forceinline__ void zero_group(const SortArgs &a, int64_t group) {
   const int64_t bytes = (int64_t)a.row_elems * a.elem_bytes;
   if (!a.flags && a.row_bytes == bytes) {
-    const int64_t all = a.vocab * bytes, lead = min(all, (int64_t)(-(intptr_t)a.dw & 15)), vecs = (all - lead) / 16;
-    const int64_t lo = group * (kZeroBytes / 16), hi = min(vecs, lo + kZeroBytes / 16);
-    for (int64_t i = lo + threadIdx.x; i < hi; i += kSortThreads) *(u32x4 *)(a.dw + lead + 16 * i) = u32x4{};
-    if (group == 0) {
-      const int64_t tail = lead + 16 * vecs;
-      for (int64_t c = 2 * (int64_t)threadIdx.x; c < lead; c += 2 * kSortThreads) *(uint16_t *)(a.dw + c) = 0;
-      for (int64_t c = tail + 2 * (int64_t)threadIdx.x; c < all; c += 2 * kSortThreads) *(uint16_t *)(a.dw + c) = 0;
-    }
+    // (cut at lines)
+    const int64_t all = a.vocab * bytes, skew = (intptr_t)a.dw & 127;
+    const int64_t lo = max(group * kZeroBytes - skew, (int64_t)0), hi = min(all, (group + 1) * kZeroBytes - skew);
+    if (lo < hi) zero_bytes<kSortThreads>(a.dw + lo, hi - lo);
     return;
   }
   const int lane = threadIdx.x & 63;
@@ -189,12 +205,7 @@ __device__ __forceinline__ void zero_group(const SortArgs &a, int64_t group) {
   const int side = (int)threadIdx.x / lanes, sides = kSortThreads / lanes, at = (int)threadIdx.x % lanes;
   for (int i = 0; rows; ++i, rows &= rows - 1) {
     if (i % sides != side) continue;
-    char *w = a.dw + (v0 + __builtin_ctzll(rows)) * a.row_bytes;
-    if (bytes >= 16) {                           // the last vector reaches back
-      for (int64_t c = 16 * at; c < bytes; c += 16 * lanes) *(u32x4_any *)(w + min(c, bytes - 16)) = u32x4{};
-    } else {
-      for (int64_t c = 2 * at; c < bytes; c += 2 * lanes) *(uint16_t *)(w + c) = 0;
-    }
+    zero_row(a.dw + (v0 + __builtin_ctzll(rows)) * a.row_bytes, bytes, at, lanes);
   }
 }
 
@@ -587,88 +598,114 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(SumArgs
   store_n<W>((W *)a.w.data + (int64_t)id * a.w.ts + col, cnt, acc);
 }
 
-// Few tokens: a workgroup takes some rows of the table, finds their tokens among all,
-// in order, and forms its rows, a wave a row's strip, all in one launch.  (70 tokens
-// of 69335 rows of 1393 float32: 78 us by the sort, XX here; a fill of the table 57.)
-constexpr int kFewThreads = 512, kFewWaves = kFewThreads / 64;
+// Zeros in `rows` rows of `bytes` bytes, a vector a thread: a workgroup that stores
+// once and ends keeps the chip writing in the order of the addresses (1 GB: 6.9 TB/s by
+// 4 KB a workgroup, 5.5 to 6.1 by 8 to 256 KB).  lanes: of a row, up to 256.
+constexpr int kFillThreads = 256, kFillBytes = 16 * kFillThreads;
+constexpr int64_t kFillGrid = 1 << 23;           // (a launch holds less than 2^32 threads)
 
-template <class W, class Y>
-__global__ __launch_bounds__(kFewThreads) void embedding_few_kernel(EmbedArgs a, int rows) {
-  constexpr int N = kVec<Y>;
-  __shared__ int id[plan::kEmbedFew], token[plan::kEmbedFew], sums[kFewWaves];
-  const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t v0 = (int64_t)blockIdx.x * rows;
-  const int n_rows = (int)min((int64_t)rows, a.vocab - v0);
-  int n = 0;                                     // of the workgroup's tokens
-  for (int t0 = 0; t0 < a.n_tokens; t0 += kFewThreads) {
-    const int t = t0 + (int)threadIdx.x;
-    const uint64_t v = t < a.n_tokens ? (uint64_t)a.tokens[t] - (uint64_t)v0 : ~uint64_t(0);
-    const bool mine = v < (uint64_t)n_rows;
-    const uint64_t in = __ballot(mine);
-    if (lane == 0) sums[wave] = __popcll(in);
-    __syncthreads();
-    int at = n + __popcll(in & ((uint64_t(1) << lane) - 1));
-#pragma unroll
-    for (int w = 0; w < kFewWaves; ++w) {
-      at += w < wave ? sums[w] : 0;
-      n += sums[w];
+__global__ __launch_bounds__(kFillThreads) void embedding_fill_kernel(char *dw, int64_t rows, int64_t bytes, int64_t row_bytes, int64_t strips, int lanes) {
+  if (rows == 1) {                               // side by side: cut at lines
+    const int64_t skew = (intptr_t)dw & 127;
+    for (int64_t unit = blockIdx.x; unit < strips; unit += gridDim.x) {
+      const int64_t at = unit * kFillBytes - skew + 16 * (int)threadIdx.x;
+      if (at >= 0 && at + 16 <= bytes) *(u32x4 *)(dw + at) = u32x4{};
+      else
+        for (int64_t c = max(at, (int64_t)0); c < min(at + 16, bytes); c += 2) *(uint16_t *)(dw + c) = 0;
     }
-    if (mine) id[at] = (int)v, token[at] = t;
-    __syncthreads();
-  }
-  W *const out = (W *)a.w.data + v0 * a.w.ts;
-  const int64_t bytes = (int64_t)a.dim * (int)sizeof(W);
-  if (n == 0 && a.w.ts == a.dim) {               // rows side by side, all zero
-    char *const p = (char *)out;
-    const int64_t all = n_rows * bytes, lead = min(all, (int64_t)(-(intptr_t)p & 15)), vecs = (all - lead) / 16, tail = lead + 16 * vecs;
-    for (int64_t i = threadIdx.x; i < vecs; i += kFewThreads) *(u32x4 *)(p + lead + 16 * i) = u32x4{};
-    for (int64_t c = 2 * (int64_t)threadIdx.x; c < lead; c += 2 * kFewThreads) *(uint16_t *)(p + c) = 0;
-    for (int64_t c = tail + 2 * (int64_t)threadIdx.x; c < all; c += 2 * kFewThreads) *(uint16_t *)(p + c) = 0;
     return;
   }
-  const int strips = (a.dim + 64 * N - 1) / (64 * N);
-  for (int unit = wave; unit < n_rows * strips; unit += kFewWaves) {
-    const int r = unit / strips, c0 = ((unit - r * strips) * 64 + lane) * N;
-    const int col = a.dim >= N ? min(c0, a.dim - N) : 0, cnt = a.dim >= N ? N : a.dim;
-    const Y *dy = (const Y *)a.y.data + col;
-    float acc[N] = {};
-    for (int j0 = 0; j0 < n; j0 += 64) {
-      uint64_t in = __ballot(j0 + lane < n && id[min(j0 + lane, n - 1)] == r);
-      while (in) {
-        int at[kAhead], some = 0;                // as many in flight; the last again where there are fewer
+  const int per = kFillThreads / lanes;
+  const int64_t groups = (rows + per - 1) / per;
+  for (int64_t unit = blockIdx.x; unit < groups * strips; unit += gridDim.x) {
+    const int64_t group = unit / strips, v = group * per + threadIdx.x / lanes, c = (unit - group * strips) * kFillBytes + 16 * ((int)threadIdx.x % lanes);
+    if (v >= rows || c >= bytes) continue;
+    char *const w = dw + v * row_bytes;
+    if (bytes >= 16) *(u32x4_any *)(w + min(c, bytes - 16)) = u32x4{};   // (the last vector reaches back)
+    else
+      for (int i = 0; i < bytes; i += 2) *(uint16_t *)(w + i) = 0;
+  }
+}
+
+// Few tokens, after the zeros: a workgroup a token and strip of columns, its waves a
+// run of the tokens each.  They find those of the workgroup's id, and if none comes
+// before its own add their rows, the runs' sums in order.
+constexpr int kFewWaves = 4;
+
+template <class W, class Y>
+__global__ __launch_bounds__(64 * kFewWaves) void embedding_few_kernel(EmbedArgs a, int strips) {
+  constexpr int N = kVec<Y>, kIds = plan::kEmbedFew / 64 / kFewWaves;
+  __shared__ float sums[kFewWaves - 1][N][64];
+  __shared__ int earlier[kFewWaves];
+  const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int t = (int)blockIdx.x / strips, c0 = (((int)blockIdx.x - t * strips) * 64 + lane) * N;
+  const int groups = (a.n_tokens + 64 * kFewWaves - 1) / (64 * kFewWaves), first = 64 * groups * wave;   // of 64 a run
+  int64_t id[kIds];
+#pragma unroll
+  for (int i = 0; i < kIds; ++i) id[i] = i < groups && first + 64 * i + lane < a.n_tokens ? a.tokens[first + 64 * i + lane] : -1;
+  const int64_t v = a.tokens[t];
+  if (v < 0 || v >= a.vocab) return;
+  uint64_t same[kIds];
+  bool before = false;
+#pragma unroll
+  for (int i = 0; i < kIds; ++i) {
+    same[i] = __ballot(id[i] == v);
+    const int left = t - first - 64 * i;         // tokens of the group before this one
+    before |= left > 0 && (same[i] & (left < 64 ? (uint64_t(1) << left) - 1 : ~uint64_t(0)));
+  }
+  if (lane == 0) earlier[wave] = before;
+  __syncthreads();
+  for (int w = 0; w < kFewWaves; ++w)
+    if (earlier[w]) return;
+  const int col = a.dim >= N ? min(c0, a.dim - N) : 0, cnt = a.dim >= N ? N : a.dim;
+  const Y *dy = (const Y *)a.y.data + col;
+  float acc[N] = {};
+#pragma unroll
+  for (int i = 0; i < kIds; ++i) {
+    uint64_t in = same[i];
+    while (in) {
+      int at[kAhead], some = 0;                  // as many in flight; the last again where there are fewer
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        at[k] = in ? first + 64 * i + __builtin_ctzll(in) : at[k > 0 ? k - 1 : 0];
+        some += in != 0;
+        in &= in - 1;
+      }
+      if (a.dim >= N) {
+        u32x4 raw[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) raw[k] = *(const u32x4_any *)(dy + (int64_t)at[k] * a.y.ts);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-          at[k] = in ? token[j0 + __builtin_ctzll(in)] : at[k > 0 ? k - 1 : 0];
-          some += in != 0;
-          in &= in - 1;
+          if (k >= some) break;
+          float x[N];
+          unpack<Y>(raw[k], x);
+#pragma unroll
+          for (int e = 0; e < N; ++e) acc[e] += x[e];
         }
-        if (a.dim >= N) {
-          u32x4 raw[kAhead];
+      } else {
+        for (int k = 0; k < some; ++k) {
+          float x[N];
+          load_some(dy + (int64_t)at[k] * a.y.ts, cnt, 0.f, x);
 #pragma unroll
-          for (int k = 0; k < kAhead; ++k) raw[k] = *(const u32x4_any *)(dy + (int64_t)at[k] * a.y.ts);
-#pragma unroll
-          for (int k = 0; k < kAhead; ++k) {
-            if (k >= some) break;
-            float v[N];
-            unpack<Y>(raw[k], v);
-#pragma unroll
-            for (int e = 0; e < N; ++e) acc[e] += v[e];
-          }
-        } else {
-          for (int k = 0; k < some; ++k) {
-            float v[N];
-            load_some(dy + (int64_t)at[k] * a.y.ts, cnt, 0.f, v);
-#pragma unroll
-            for (int e = 0; e < N; ++e) acc[e] += v[e];
-          }
+          for (int e = 0; e < N; ++e) acc[e] += x[e];
         }
       }
     }
-    if (c0 >= a.dim) continue;
-#pragma unroll
-    for (int e = 0; e < N; ++e) acc[e] *= a.scale;
-    store_n<W>(out + (int64_t)r * a.w.ts + col, cnt, acc);
   }
+  if (wave > 0) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) sums[wave - 1][e][lane] = acc[e];
+  }
+  __syncthreads();
+  if (wave > 0 || c0 >= a.dim) return;
+#pragma unroll
+  for (int w = 0; w < kFewWaves - 1; ++w)
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[e] += sums[w][e][lane];
+#pragma unroll
+  for (int e = 0; e < N; ++e) acc[e] *= a.scale;
+  store_n<W>((W *)a.w.data + v * a.w.ts + col, cnt, acc);
 }
 
 template <class W, class Y>
@@ -690,8 +727,18 @@ template <class W, class Y>
 hipError_t bwd(const EmbedArgs &a, hipStream_t s) {
   const plan::EmbedBwd &f = a.f;
   if (plan::embed_few(a.n_tokens, a.dim, (int)sizeof(Y))) {   // (also of none)
-    const int rows = plan::embed_few_rows(a.dim * (int64_t)sizeof(W), a.vocab);
-    embedding_few_kernel<W, Y><<<(int)plan::ceil_div(a.vocab, rows), kFewThreads, 0, s>>>(a, rows);
+    const int64_t bytes = a.dim * (int64_t)sizeof(W), row_bytes = a.w.ts * (int64_t)sizeof(W);
+    const bool whole = a.vocab == 1 || row_bytes == bytes;
+    const int64_t rows = whole ? 1 : a.vocab, each = whole ? a.vocab * bytes : bytes;
+    const int64_t strips = plan::ceil_div(each + (whole ? 127 : 0), kFillBytes);
+    int lanes = 1;
+    while (lanes < kFillThreads && 16 * lanes < bytes) lanes *= 2;
+    const int64_t grid = plan::ceil_div(rows, kFillThreads / lanes) * strips;
+    embedding_fill_kernel<<<(int)(grid < kFillGrid ? grid : kFillGrid), kFillThreads, 0, s>>>(a.w.data, rows, each, row_bytes, strips, lanes);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.n_tokens == 0) return e;
+    const int sum_strips = (int)plan::ceil_div(a.dim, 64 * kVec<Y>);
+    embedding_few_kernel<W, Y><<<a.n_tokens * sum_strips, 64 * kFewWaves, 0, s>>>(a, sum_strips);
     return hipGetLastError();
   }
   SortArgs k{};
@@ -706,7 +753,7 @@ hipError_t bwd(const EmbedArgs &a, hipStream_t s) {
   k.row_elems = a.dim;
   k.elem_bytes = (int)sizeof(W);
   const bool flags = f.blocks > 0, side_by_side = !flags && k.row_bytes == (int64_t)a.dim * (int)sizeof(W);
-  k.groups = (int)(side_by_side ? plan::ceil_div(a.vocab * k.row_bytes, kZeroBytes) : plan::ceil_div(a.vocab, kZeroRows));
+  k.groups = (int)(side_by_side ? plan::ceil_div(a.vocab * k.row_bytes + 127, kZeroBytes) : plan::ceil_div(a.vocab, kZeroRows));
   const int zero = k.groups < kZeroGrid ? k.groups : kZeroGrid;
   uint32_t *const key[2] = {(uint32_t *)(a.ws + f.key_off[0]), (uint32_t *)(a.ws + f.key_off[1])};
   uint32_t *const token[2] = {(uint32_t *)(a.ws + f.token_off[0]), (uint32_t *)(a.ws + f.token_off[1])};

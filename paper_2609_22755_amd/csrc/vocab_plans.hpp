@@ -122,21 +122,15 @@ constexpr int kSortBlock = 4096;                // tokens that a workgroup of a 
 constexpr int kSortWhole = 16384;               // tokens that one workgroup sorts by itself
 constexpr int kSortBits = 9;                    // most of a digit
 
-// Few tokens, whose rows one workgroup could add: a kernel that needs no sort.
-// (At most what one reads in some 10 us, if all tokens have one id.  With and without
-// a sort: 24 x 512 of 3000 rows 15.4 and 7.9 us, 400 x 512 14.6 and 8.1, 200 x 2048 of
-// 32000 30.8 and 22.6, 400 x 2048 31.0 and 33.6, 1000 x 512 of 3000 15.4 and 17.3.)
-constexpr int kEmbedFew = 512;
-constexpr int64_t kEmbedFewBytes = 1 << 20;
-constexpr bool embed_few(int64_t n_tokens, int dim, int es) { return n_tokens <= kEmbedFew && n_tokens * dim * es <= kEmbedFewBytes; }
-// Table rows of one of its workgroups: some 32 KB, 1024 workgroups at least, and
-// 2^22 at most (a launch holds less than 2^32 threads).
-constexpr int embed_few_rows(int64_t row_bytes, int vocab) {
-  int64_t r = (32 << 10) / row_bytes, most = vocab / 1024;
-  const int64_t least = ceil_div(vocab, 1 << 22);
-  r = r < most ? r : most;
-  r = r > 64 ? 64 : r;
-  return (int)(r < least ? least : r < 1 ? 1 : r);
+// Few tokens, of at most so many bytes of dy: a kernel of zeros and one that finds each
+// id's tokens itself.  (us, with and without a sort, tables in HBM.  Gained: 24 x 4096 of
+// 131072 rows 199 and 160, a fill alone 156; 70 x 1393 float32 of 69335 74 and 63; 400 x 512
+// of 3000 15.4 and 8.3; 1000 x 512 of 3000 16.7 and 9.7; 2000 x 512 18.0 and 13.4; 1000 x
+// 1024 float32 of 32000 33.2 and 29.5.  Lost, the sort hides beside the zeros of a large
+// table: 1000 x 2048 bf16 of 32000 32.8 and 34.8, 1500 x 1024 33.1 and 38.5)
+constexpr int kEmbedFew = 2048;
+constexpr bool embed_few(int64_t n_tokens, int dim, int es) {
+  return n_tokens <= kEmbedFew && n_tokens * dim * es <= (n_tokens <= 1024 ? 4 << 20 : 2 << 20);
 }
 
 struct EmbedBwd {

@@ -250,3 +250,26 @@ def test_table_with_far_rows(T):
     ws = _ws(nsp.nsp_embedding_bwd_workspace(T, dim, V))
     nsp.nsp_embedding_bwd(ids, dy, wf, ws)
     assert torch.equal(wf.double(), _count(ids, dy, V))
+
+
+@pytest.mark.parametrize("wt,dt", [(BF, BF), (F, F), (BF, F), (F, BF)])
+@pytest.mark.parametrize("T,dim", [(511, 40), (1024, 33), (1025, 33), (2047, 7), (2048, 72), (2049, 72), (1024, 1032), (1040, 1032), (2000, 300)])
+def test_embedding_gradient_with_and_without_a_sort(T, dim, wt, dt):
+    """Sizes around those from which tokens are sorted: sums of whole numbers, exact in float32 (and, below 256, in bf16)."""
+    V = 77
+    ids, dy = _ids(T, V + 2) - 1, _whole(T, dim).to(dt)         # ids out of the vocabulary on both sides
+    ids[T // 3:T // 2] = 5
+    there = (ids >= 0) & (ids < V)
+    want = _count(torch.where(there, ids, V), dy, V + 1)[:V]
+    dw = torch.full((V, dim), float("nan"), dtype=wt, device="cuda")
+    nsp.nsp_embedding_bwd(ids, dy, dw, _ws(nsp.nsp_embedding_bwd_workspace(T, dim, V)))
+    assert torch.equal(dw, want.to(wt))
+    # one id of all; none at all; rows apart, what lies between them left as it was
+    for one in (3, -1):
+        ids.fill_(one)
+        wide = torch.full((V, dim + 3), 7.0, dtype=wt, device="cuda")
+        nsp.nsp_embedding_bwd(ids, dy, wide[:, :dim], _ws(nsp.nsp_embedding_bwd_workspace(T, dim, V)))
+        want = torch.zeros(V, dim, dtype=torch.float64, device="cuda")
+        if one >= 0:
+            want[one] = dy.double().sum(0)
+        assert torch.equal(wide[:, :dim], want.to(wt)) and bool((wide[:, dim:] == 7).all())
