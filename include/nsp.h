@@ -684,11 +684,11 @@ nsp_status nsp_token_logp_bwd(nsp_dtype dtype, int64_t n_tokens, int32_t vocab, 
 
 /* Bytes of device workspace of nsp_linear_logp_fwd and _bwd (0 for invalid
  * sizes and no tokens).  Forward: 16 bytes a token and 256 vocabulary rows, of
- * 32768 tokens at most.  Backward: the hidden rows gathered (2 n_tokens dim bytes),
- * the gradient of the logits of one piece of the vocabulary (about 512 MB, more
- * from 65536 tokens on: 8192 bytes a token), and float32 sums (4 n_tokens dim bytes
- * with more than one piece, up to 64 times that, 256 MB about, where few
- * tiles have to be split). */
+ * 32768 tokens at most (fewer from 2^19 vocabulary rows on: 1 GB, or 4096 tokens).
+ * Backward: the hidden rows gathered (2 n_tokens dim bytes), the gradient of the
+ * logits of one piece of the vocabulary (512 MB at most, but 8192 bytes a token from
+ * 65536 tokens on), and float32 sums: 4 n_tokens dim bytes with more than one piece,
+ * and up to 256 tiles of 256 KB each of dx and of dw where few tiles are split. */
 size_t nsp_linear_logp_fwd_workspace(int64_t n_tokens, int32_t dim, int32_t vocab);
 size_t nsp_linear_logp_bwd_workspace(int64_t n_tokens, int32_t dim, int32_t vocab);
 
@@ -702,7 +702,7 @@ size_t nsp_linear_logp_bwd_workspace(int64_t n_tokens, int32_t dim, int32_t voca
  * else has lse = -inf, entropy 0 and, unless its target is ignored, logp = -inf.
  * A row with a NaN or +inf among its logits, or whose lse passes float32, has lse
  * and entropy NaN, and logp unless its target is ignored.  A row's results depend
- * on that row of x (and n_tokens) alone.
+ * on that row of x (and n_tokens and vocab) alone.
  *   x           bf16 [n_tokens] rows of dim elements; w: bf16 [vocab] rows
  *               (16-byte aligned, strides multiples of 8, up to 2^20)
  *   n_tokens    up to 2^22; dim: a multiple of 8 up to 65536; vocab: up to 2^24
@@ -724,7 +724,7 @@ nsp_status nsp_linear_logp_fwd(int64_t n_tokens, int32_t dim, int32_t vocab, con
  *     da_v = scale (g_logp (1[v = target] - p_v) + g_lse p_v
  *                   - g_entropy p_v (z_v - lse + entropy))
  *     dx[t] = sum_v da[t][v] w[v],   dw[v] = sum_t da[t][v] x[t]
- * da is rounded to bf16 (half a step of it, 2^-9, an element) for the matrix
+ * da is rounded to bf16 (half a step of it, 2^-8, an element) for the matrix
  * cores; sums are float32, rounded once to grad_dtype.  A token whose gradients are
  * all 0 (an ignored target takes g_logp as 0), or whose lse is -inf, takes no part,
  * whatever its row of x holds, and has dx = 0.  An lse of NaN or +inf makes the
@@ -811,8 +811,9 @@ nsp_status nsp_embedding_fwd(nsp_dtype w_dtype, nsp_dtype dtype, int64_t n_token
                              hipStream_t stream);
 
 /* Bytes of device workspace nsp_embedding_bwd needs (0 for invalid sizes and
- * no tokens): the tokens sorted by their ids (16 bytes each), a byte a table row,
- * and float32 sums (8 dim bytes for every 8 to 128 tokens). */
+ * no tokens): the tokens sorted by their ids (8 bytes each; from 16385 tokens on
+ * 16, the sort's counts and a byte a table row), and float32 sums (8 dim bytes for
+ * every 8 to 128 tokens). */
 size_t nsp_embedding_bwd_workspace(int64_t n_tokens, int32_t dim, int32_t vocab);
 
 /*

@@ -4,7 +4,7 @@ best tokens; forward and backward against the same step in float64 with automati
 differentiation, the same captured and replayed, two at once on two streams.
 
 Tolerance of the step, relative 2-norm: the embedding is exact; hidden rows are rounded
-to bf16 between the operators (2^-9 of each, independent), the student's logits of
+to bf16 between the operators (2^-8 of each at most), the student's logits of
 the distillation and every gradient that passes between the operators as well: at
 most 6 roundings of at most 2^-8 each, 2.4%.  Results of the forward: 1% of the
 largest."""
