@@ -688,7 +688,8 @@ nsp_status nsp_token_logp_bwd(nsp_dtype dtype, int64_t n_tokens, int32_t vocab, 
  * Backward: the hidden rows gathered (2 n_tokens dim bytes), the gradient of the
  * logits of one piece of the vocabulary (512 MB at most, but 8192 bytes a token from
  * 65536 tokens on), and float32 sums: 4 n_tokens dim bytes with more than one piece,
- * and up to 256 tiles of 256 KB each of dx and of dw where few tiles are split. */
+ * and up to 256 tiles of 256 KB each of dx and of dw where few tiles are split.
+ * Calls whose logits make few tiles: up to 256 such tiles of them too. */
 size_t nsp_linear_logp_fwd_workspace(int64_t n_tokens, int32_t dim, int32_t vocab);
 size_t nsp_linear_logp_bwd_workspace(int64_t n_tokens, int32_t dim, int32_t vocab);
 

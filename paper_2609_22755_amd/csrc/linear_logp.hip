@@ -56,6 +56,95 @@ constexpr int kWavesPerSimd = P::kLds > 80 * 1024 ? 2 : 4;
 // The p of element i of a block, from the block's first.
 __device__ __forceinline__ int p_of(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
 
+// 32 q's (one a lane pair) of 32 * NB p's, of a wave's sums, as rows of p: through
+// LDS (32 * 32 * NB elements of the wave's own), 16 bytes a lane.  put(row, byte,
+// 16 bytes) for rows below `rows`, elements below `cols`.
+template <int NB, bool F32, class Put>
+__device__ __forceinline__ void put_rows(const f32x16 *acc, char *lds, int rows, int cols, int lane_, Put put) {
+  const int lane = hidden(lane_);
+  constexpr int CH = NB * (F32 ? 8 : 4), PER = F32 ? 4 : 8;
+  const int l32 = lane & 31, h = lane >> 5;
+#pragma unroll
+  for (int mb = 0; mb < NB; ++mb)
+#pragma unroll
+    for (int gq = 0; gq < 4; ++gq) {
+      const f32x4 v = {acc[mb][4 * gq], acc[mb][4 * gq + 1], acc[mb][4 * gq + 2], acc[mb][4 * gq + 3]};
+      const int c = F32 ? 8 * mb + 2 * gq + h : 4 * mb + gq;
+      char *p = lds + 16 * (l32 * CH + (c ^ (l32 & (CH - 1))));
+      if constexpr (F32) *(f32x4 *)p = v;
+      else *(bf16x4 *)(p + 8 * h) = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
+    }
+#pragma unroll
+  for (int j = 0; j < CH / 2; ++j) {
+    const int row = (64 * j + lane) / CH, c = (64 * j + lane) % CH;
+    const f32x4 v = *(const f32x4 *)(lds + 16 * (row * CH + (c ^ (row & (CH - 1)))));
+    if (row < rows && c * PER < cols) put(row, 16 * c, v);
+  }
+}
+
+// ------------------------------------------------- logits of few tiles --
+
+// Sums of a part of dim, in float32: [part][rows][cols], for calls whose tiles are fewer than
+// the compute units.  Such a call is bound by what a unit has on its way from memory; the
+// parts bring more units to bear (8 x 4400 of 9040 rows: 36 tiles 48 us, 7 parts each 24).
+struct LogitParts {
+  const char *w, *x;
+  int64_t w_stride, x_stride;
+  const int *count;            // rows, null: n
+  int n, vocab, dim;
+  int split, tiles_p;
+  int64_t rows, cols;          // whole tiles
+  float *sums;
+
+  // Columns c .. c + 3 of a row, the parts in order.
+  __device__ __forceinline__ f32x4 at(int64_t row, int64_t c) const {
+    const float *from = sums + row * cols + c;
+    f32x4 z = *(const f32x4 *)from;
+    for (int p0 = 1; p0 < split; p0 += 5) {
+      f32x4 v[5];
+#pragma unroll
+      for (int j = 0; j < 5; ++j) v[j] = p0 + j < split ? *(const f32x4 *)(from + (p0 + j) * rows * cols) : f32x4{};
+#pragma unroll
+      for (int j = 0; j < 5; ++j) z += v[j];
+    }
+    return z;
+  }
+};
+
+template <int NQ>
+__global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void linear_parts_kernel(LogitParts f) {
+  typedef typename LogitTile<NQ>::P P;
+  static_assert(P::kLds >= P::NW * 4096 * P::BP, "room for the rows that are stored");
+  __shared__ __attribute__((aligned(1024))) char smem[P::kLds];
+  const int n = f.count ? *f.count : f.n;
+  tile::Place at;
+  if (!at.find(blockIdx.x, f.tiles_p, (n + NQ - 1) / NQ, f.split, kGroup)) return;
+  P x;
+  const int v0 = at.p * P::NP, q0 = at.q * NQ;
+  const int len = (int)plan::round_up(plan::ceil_div(f.dim, f.split), tile::kStep);
+  const int k0 = at.part * len, n_k = max(0, min(f.dim - k0, len));
+  x.run(smem, typename P::LoadP(f.w, f.w_stride, v0, f.vocab, k0, n_k, x.wave, x.lane),
+        typename P::LoadQ(f.x, f.x_stride, q0, n, k0, n_k, x.wave, x.lane), n_k);
+#pragma unroll
+  for (int q = 0; q < P::BQ; ++q) {
+    float *out = f.sums + (at.part * f.rows + q0 + x.q0() + 32 * q) * f.cols + v0 + x.p0();
+    put_rows<P::BP, true>(x.acc[q], smem + x.wave * (4096 * P::BP), 32, 32 * P::BP, x.lane,
+                          [&](int row, int byte, f32x4 v) { *(f32x4 *)((char *)(out + row * f.cols) + byte) = v; });
+  }
+}
+
+// Workgroups of `tiles` tiles: as many for each XCD.
+int grid_of(int64_t tiles) { return (int)plan::round_up(tiles, kXcdQueues); }
+
+hipError_t logit_parts(const LogitParts &f, int tile, hipStream_t s) {
+  const int grid = grid_of(f.tiles_p * (f.rows / tile) * f.split);
+  if (tile == 32) linear_parts_kernel<32><<<grid, 512, 0, s>>>(f);
+  else if (tile == 64) linear_parts_kernel<64><<<grid, 512, 0, s>>>(f);
+  else if (tile == 128) linear_parts_kernel<128><<<grid, 512, 0, s>>>(f);
+  else linear_parts_kernel<256><<<grid, 512, 0, s>>>(f);
+  return hipGetLastError();
+}
+
 // ----------------------------------------------------------------- forward --
 
 struct FwdTiles {
@@ -143,6 +232,35 @@ __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void
     }
     f.part[at.p * f.panel + q0 + tok] = r;
   }
+}
+
+// The same of logits in parts: a wave a token and tile, a lane four of its logits.
+__global__ __launch_bounds__(256) void linear_logp_stats_kernel(FwdTiles f, LogitParts z) {
+  const int lane = threadIdx.x & 63;
+  const int64_t unit = (int64_t)blockIdx.x * 4 + (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tok = (int)(unit / f.tiles_p), tile = (int)(unit - (int64_t)tok * f.tiles_p);
+  if (tok >= f.n) return;
+  const int v = tile * plan::kTileP + 4 * lane;
+  const f32x4 raw = z.at(tok, v);
+  const float c = f.a.scale * kLog2e;
+  const int64_t y = f.a.logp ? f.a.targets[tok] : -1;
+  float a[4], m = kLowest, s = 0.f, u = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    a[i] = v + i < f.a.vocab ? raw[i] : kNegInf;
+    if (v + i == y && y < f.a.vocab) f.at_target[tok] = a[i];
+    m = fmaxf(m, a[i]);
+  }
+  m = wave_max(m);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float d = (a[i] - m) * c, e = fast_exp2(d);
+    s += e;
+    u = fmaf(e, fmaxf(d, -200.f), u);              // (0 times infinity: 0; a NaN stays one in s)
+  }
+  s = group_sum<64>(s);
+  u = group_sum<64>(u);
+  if (lane == 0) f.part[tile * f.panel + tok] = make_float4(m, s, u, 0.f);
 }
 
 // The tiles of 16 tokens a workgroup: 64 strands of tiles, joined over the four of a
@@ -333,32 +451,6 @@ __global__ __launch_bounds__(1024) void linear_rows_gather_kernel(BwdTiles b) {
   for (int r = (int)blockIdx.x * 16 + wave; r < b.a.n_tokens; r += (int)gridDim.x * 16) gather_row(b, r, place[r]);
 }
 
-// 32 q's (one a lane pair) of 32 * NB p's, of a wave's sums, as rows of p: through
-// LDS (32 * 32 * NB elements of the wave's own), 16 bytes a lane.  put(row, byte,
-// 16 bytes) for rows below `rows`, elements below `cols`.
-template <int NB, bool F32, class Put>
-__device__ __forceinline__ void put_rows(const f32x16 *acc, char *lds, int rows, int cols, int lane_, Put put) {
-  const int lane = hidden(lane_);
-  constexpr int CH = NB * (F32 ? 8 : 4), PER = F32 ? 4 : 8;
-  const int l32 = lane & 31, h = lane >> 5;
-#pragma unroll
-  for (int mb = 0; mb < NB; ++mb)
-#pragma unroll
-    for (int gq = 0; gq < 4; ++gq) {
-      const f32x4 v = {acc[mb][4 * gq], acc[mb][4 * gq + 1], acc[mb][4 * gq + 2], acc[mb][4 * gq + 3]};
-      const int c = F32 ? 8 * mb + 2 * gq + h : 4 * mb + gq;
-      char *p = lds + 16 * (l32 * CH + (c ^ (l32 & (CH - 1))));
-      if constexpr (F32) *(f32x4 *)p = v;
-      else *(bf16x4 *)(p + 8 * h) = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
-    }
-#pragma unroll
-  for (int j = 0; j < CH / 2; ++j) {
-    const int row = (64 * j + lane) / CH, c = (64 * j + lane) % CH;
-    const f32x4 v = *(const f32x4 *)(lds + 16 * (row * CH + (c ^ (row & (CH - 1)))));
-    if (row < rows && c * PER < cols) put(row, 16 * c, v);
-  }
-}
-
 // dl of a piece.
 template <int NQ>
 __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void linear_dl_kernel(BwdTiles b, int tiles_p) {
@@ -401,6 +493,25 @@ __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void
     char *out = b.dl + 2 * ((int64_t)r0 * b.f.piece + vw);
     put_rows<P::BP, false>(x.acc[q], smem + x.wave * (2048 * P::BP), 32, 32 * P::BP, x.lane,
                            [&](int row, int byte, f32x4 v) { *(f32x4 *)(out + (int64_t)row * 2 * b.f.piece + byte) = v; });
+  }
+}
+
+// dl of a piece from logits in parts: eight columns a thread.
+__global__ __launch_bounds__(256) void linear_dl_parts_kernel(BwdTiles b, LogitParts z) {
+  const int vecs = b.f.piece / 8;
+  const int64_t all = (int64_t)*b.count * vecs;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const int r = (int)(i / vecs), v = (int)(i - (int64_t)r * vecs) * 8;
+    const float4 k = b.coef[r];
+    const int y = b.target[r] - v;
+    const f32x4 lo = z.at(r, v), hi = z.at(r, v + 4);
+    float o[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float d = ((e < 4 ? lo[e & 3] : hi[e & 3]) * b.a.scale - k.x) * kLog2e;
+      o[e] = fast_exp2(fminf(d, 0.f)) * (k.z != 0.f ? k.y + k.z * fmaxf(d, -200.f) : k.y) + (e == y ? k.w : 0.f);
+    }
+    *(u32x4 *)(b.dl + 2 * ((int64_t)r * b.f.piece + v)) = pack<bf16>(o);
   }
 }
 
@@ -523,9 +634,6 @@ __global__ __launch_bounds__(256) void linear_zero_kernel(char *dw, int64_t row_
     for (int i = (int)threadIdx.x; i < vecs; i += 256) *(u32x4 *)(dw + v * row_bytes + 16 * i) = u32x4{};
 }
 
-// Workgroups of `tiles` tiles: as many for each XCD.
-int grid_of(int64_t tiles) { return (int)plan::round_up(tiles, kXcdQueues); }
-
 template <int NQ>
 hipError_t fwd_tiles(const FwdTiles &f, hipStream_t s) {
   linear_logp_tiles_kernel<NQ><<<grid_of((int64_t)f.tiles_p * f.tiles_q), 512, 0, s>>>(f);
@@ -572,7 +680,7 @@ hipError_t join_sums(const BwdTiles &b, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_linear_logp_fwd(const LinearArgs &a, hipStream_t s) {
-  const plan::LinearFwd p = plan::linear_fwd(a.n_tokens, a.vocab);
+  const plan::LinearFwd p = plan::linear_fwd(a.n_tokens, a.dim, a.vocab);
   FwdTiles f{};
   f.a = a;
   f.panel = p.panel;
@@ -583,7 +691,17 @@ hipError_t launch_linear_logp_fwd(const LinearArgs &a, hipStream_t s) {
     f.t0 = t0;
     f.n = (int)(a.n_tokens - t0 < p.panel ? a.n_tokens - t0 : p.panel);
     f.tiles_q = (int)plan::ceil_div(f.n, p.tile);
-    hipError_t e = p.tile == 32 ? fwd_tiles<32>(f, s) : p.tile == 64 ? fwd_tiles<64>(f, s) : p.tile == 128 ? fwd_tiles<128>(f, s) : fwd_tiles<256>(f, s);
+    hipError_t e;
+    if (p.split > 1) {
+      const LogitParts z = {a.w, a.x, a.w_stride, a.x_stride, nullptr, f.n, a.vocab, a.dim, p.split, f.tiles_p, p.panel,
+                            p.tiles_p * plan::kTileP, (float *)(a.ws + p.z_off)};
+      e = logit_parts(z, p.tile, s);
+      if (e != hipSuccess) return e;
+      linear_logp_stats_kernel<<<(int)plan::ceil_div(f.n * p.tiles_p, 4), 256, 0, s>>>(f, z);
+      e = hipGetLastError();
+    } else {
+      e = p.tile == 32 ? fwd_tiles<32>(f, s) : p.tile == 64 ? fwd_tiles<64>(f, s) : p.tile == 128 ? fwd_tiles<128>(f, s) : fwd_tiles<256>(f, s);
+    }
     if (e != hipSuccess) return e;
     linear_logp_join_kernel<<<(f.n + kJoinTokens - 1) / kJoinTokens, kJoinTokens * kJoinStrands, 0, s>>>(f);
     e = hipGetLastError();
@@ -631,7 +749,17 @@ hipError_t launch_linear_logp_bwd(const LinearArgs &a, hipStream_t s) {
     b.n_v = a.vocab - b.v0 < b.f.piece ? a.vocab - b.v0 : b.f.piece;
     b.first = p == 0;
     b.last = p == b.f.pieces - 1;
-    e = b.f.tile == 32 ? dl_tiles<32>(b, s) : b.f.tile == 64 ? dl_tiles<64>(b, s) : b.f.tile == 128 ? dl_tiles<128>(b, s) : dl_tiles<256>(b, s);
+    if (b.f.split_z > 1) {
+      const LogitParts z = {a.w, b.x, a.w_stride, b.f.dim, b.count, 0, a.vocab, a.dim, b.f.split_z, b.f.piece / plan::kTileP, b.f.rows,
+                            b.f.piece, (float *)(a.ws + b.f.z_off)};
+      e = logit_parts(z, b.f.tile, s);
+      if (e != hipSuccess) return e;
+      const int64_t want = plan::ceil_div(b.f.rows * (b.f.piece / 8), 256);
+      linear_dl_parts_kernel<<<(int)(want < 8192 ? want : 8192), 256, 0, s>>>(b, z);
+      e = hipGetLastError();
+    } else {
+      e = b.f.tile == 32 ? dl_tiles<32>(b, s) : b.f.tile == 64 ? dl_tiles<64>(b, s) : b.f.tile == 128 ? dl_tiles<128>(b, s) : dl_tiles<256>(b, s);
+    }
     if (e == hipSuccess) e = b.f.tile_x == 64 ? grads<64>(b, s) : grads<256>(b, s);
     if (e == hipSuccess && a.dw && b.f.split_w > 1) e = join_sums<false>(b, s);
     if (e == hipSuccess && a.dx && b.last && b.sums_x) e = join_sums<true>(b, s);

@@ -146,7 +146,7 @@ extern "C" {
 size_t nsp_linear_logp_fwd_workspace(int64_t n_tokens, int32_t dim, int32_t vocab) {
   if (check_linear_sizes(n_tokens, dim, vocab) != NSP_OK || n_tokens == 0) return 0;
   set_error(NSP_OK, nullptr);
-  return nsp::plan::linear_fwd(n_tokens, vocab).bytes;
+  return nsp::plan::linear_fwd(n_tokens, dim, vocab).bytes;
 }
 
 nsp_status nsp_linear_logp_fwd(int64_t n_tokens, int32_t dim, int32_t vocab, const nsp_rows *x, const nsp_rows *w,
@@ -160,7 +160,7 @@ nsp_status nsp_linear_logp_fwd(int64_t n_tokens, int32_t dim, int32_t vocab, con
   NSP_TRY(check_array(targets, 8, some && logp, "targets"));
   NSP_TRY(check_array(entropy, 4, false, "entropy"));
   if (!some) return set_error(NSP_OK, nullptr);
-  NSP_TRY(check_workspace(workspace, ws_bytes, nsp::plan::linear_fwd(n_tokens, vocab).bytes));
+  NSP_TRY(check_workspace(workspace, ws_bytes, nsp::plan::linear_fwd(n_tokens, dim, vocab).bytes));
   a.logp = logp;
   a.lse = lse;
   a.entropy = entropy;

@@ -40,13 +40,27 @@ constexpr int64_t linear_panel(int64_t tiles_p) {
   return n;
 }
 
+// Parts of the logits' sums over dim, where their tiles are too few: of 512 k at least,
+// and three at least, since they are written and read once more.  (us whole and in parts,
+// forward: 8 x 4400 of 9040 rows 48 and 24, 1 x 4096 of 4000 29 and 15, 600 x 8192 of 2000 73
+// and 36, 1486 x 2176 of 1285 29 and 28; backward: 4 x 4616 of 2740 72 and 39, 16 x 4472 of
+// 14375 118 and 94.  In two parts: 1000 x 2048 of 4000 forward 28 and 34, 2000 x 1024 of 1000
+// backward 59 and 63)
+constexpr int linear_logit_split(int64_t tiles, int dim) {
+  int64_t s = kUnits / tiles;
+  const int64_t most = dim / 512;
+  s = s < most ? s : most;
+  return (int)(s < 3 ? 1 : s > 16 ? 16 : s);
+}
+
 struct LinearFwd {
   int tile;
+  int split;                   // parts of the logits' sums
   int64_t panel;               // tokens, a multiple of the tile or all of them
   int64_t tiles_p;
-  size_t part_off, target_off, bytes;
+  size_t part_off, target_off, z_off, bytes;
 };
-constexpr LinearFwd linear_fwd(int64_t n_tokens, int vocab) {
+constexpr LinearFwd linear_fwd(int64_t n_tokens, int dim, int vocab) {
   LinearFwd f{};
   f.tile = linear_tile(n_tokens, vocab);
   f.tiles_p = ceil_div(vocab, kTileP);
@@ -54,7 +68,10 @@ constexpr LinearFwd linear_fwd(int64_t n_tokens, int vocab) {
   if (n_tokens < f.panel) f.panel = round_up(n_tokens, f.tile);
   f.part_off = 0;
   f.target_off = pad256((size_t)f.tiles_p * f.panel * 16);
-  f.bytes = f.target_off + pad256((size_t)f.panel * 4);
+  f.z_off = f.target_off + pad256((size_t)f.panel * 4);
+  // (more than one part: one panel)
+  f.split = n_tokens > 0 ? linear_logit_split(f.tiles_p * ceil_div(n_tokens, f.tile), dim) : 1;
+  f.bytes = f.z_off + (f.split > 1 ? (size_t)f.split * f.panel * f.tiles_p * kTileP * 4 : 0);
   return f;
 }
 
@@ -76,8 +93,8 @@ struct LinearBwd {
   int piece;                   // vocabulary rows of a piece, in whole tiles
   int pieces;
   int dim;                     // elements between gathered rows: whole 128-byte lines
-  int split_x, split_w;        // parts of dx's and dw's sums
-  size_t count_off, order_off, place_off, coef_off, target_off, x_off, dl_off, sum_x_off, sum_w_off, bytes;
+  int split_z, split_x, split_w;   // parts of the logits', dx's and dw's sums
+  size_t count_off, order_off, place_off, coef_off, target_off, x_off, dl_off, z_off, sum_x_off, sum_w_off, bytes;
 };
 // The gradient of the logits is kept for one piece of the vocabulary at a time,
 // some 2^28 elements of it (512 MB): large enough that adding dx's float32 sums
@@ -110,6 +127,11 @@ constexpr LinearBwd linear_bwd(int64_t n_tokens, int dim, int vocab) {
   if (f.pieces > 1 || f.split_x > 1) at += pad256((size_t)f.split_x * f.rows * dim * 4);
   f.sum_w_off = at;
   if (f.split_w > 1) at += pad256((size_t)f.split_w * f.piece * dim * 4);
+  // the logits' parts are read before those sums begin (more than one part: one piece)
+  f.z_off = f.sum_x_off;
+  f.split_z = n_tokens > 0 ? linear_logit_split(f.rows / f.tile * (f.piece / kTileP), dim) : 1;
+  const size_t z_end = f.z_off + (f.split_z > 1 ? (size_t)f.split_z * f.rows * f.piece * 4 : 0);
+  at = at > z_end ? at : z_end;
   f.bytes = n_tokens > 0 ? at : 0;
   return f;
 }

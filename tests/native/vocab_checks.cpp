@@ -59,18 +59,23 @@ static int64_t spread(int64_t lo, int64_t hi) {
 static int64_t pick(int64_t n) { return (int64_t)(g_rng() % (uint64_t)n); }
 
 static void linear_plans(int64_t T, int dim, int V) {
-  const plan::LinearFwd f = plan::linear_fwd(T, V);
+  const plan::LinearFwd f = plan::linear_fwd(T, dim, V);
   CHECK(f.tile == 32 || f.tile == 64 || f.tile == 128 || f.tile == 256);
   CHECK(f.panel >= T || f.panel == plan::linear_panel(f.tiles_p));
   CHECK(f.panel % f.tile == 0 && f.tiles_p * plan::kTileP >= V);
   CHECK((f.tiles_p * (f.panel / f.tile) + 8) * 512 < int64_t(1) << 32);   // threads of a launch
-  CHECK(f.target_off >= (size_t)(f.tiles_p * f.panel * 16) && f.bytes >= f.target_off + (size_t)f.panel * 4);
+  CHECK(f.target_off >= (size_t)(f.tiles_p * f.panel * 16) && f.z_off >= f.target_off + (size_t)f.panel * 4);
+  CHECK(f.split >= 1 && (f.split == 1 || (T <= f.panel && dim / f.split >= 512)));
+  CHECK(f.bytes >= f.z_off + (f.split > 1 ? (size_t)f.split * f.panel * f.tiles_p * plan::kTileP * 4 : 0));
+  CHECK(f.split * f.tiles_p * (f.panel / f.tile) <= (f.split > 1 ? plan::kUnits : INT32_MAX - 8));
   const plan::LinearBwd b = plan::linear_bwd(T, dim, V);
   CHECK(b.rows >= T && b.rows % b.tile == 0 && b.rows < T + b.tile);
   CHECK(b.piece % plan::kTileP == 0 && b.pieces >= 1);
   CHECK((int64_t)b.piece * b.pieces >= V && (int64_t)b.piece * (b.pieces - 1) < V);
   CHECK(b.dim >= dim && b.dim % 64 == 0);
   CHECK(b.split_x >= 1 && b.split_x <= 64 && b.split_w >= 1 && b.split_w <= 64);
+  CHECK(b.split_z == 1 || (b.pieces == 1 && dim / b.split_z >= 512));
+  CHECK(b.z_off >= b.dl_off + (size_t)b.rows * b.piece * 2 && b.bytes >= b.z_off + (b.split_z > 1 ? (size_t)b.split_z * b.rows * b.piece * 4 : 0));
   // a part of 256 k at least
   CHECK(b.split_x == 1 || b.piece / b.split_x >= 256);
   CHECK(b.split_w == 1 || T / b.split_w >= 256);

@@ -134,6 +134,54 @@ def test_gradient(T, dim, V):
         _check_bwd(x, w, yy, o, gg, dx, dw, 0.8)
 
 
+# wide rows, few tiles of logits: sums in parts over dim
+WIDE = [(1, 1024, 1), (7, 1032, 300), (33, 2056, 600), (70, 4104, 100), (130, 1536, 513), (300, 2048, 1000), (513, 1096, 257), (24, 8192, 3001)]
+
+
+@pytest.mark.parametrize("T,dim,V", WIDE)
+def test_wide_rows_of_few_tiles(T, dim, V):
+    rng, x, w, y = _inputs(T, dim, V, T + dim)
+    off = torch.from_numpy(rng.random(T) < 0.2).cuda()
+    o = _forward(x, w, y, 0.8)
+    _check_fwd(x, w, y, o, 0.8)
+    again = _forward(x, w, y, 0.8)
+    assert all(torch.equal(o[n], again[n]) for n in o)
+    g = [torch.from_numpy(rng.standard_normal(T).astype(np.float32)).cuda().masked_fill(off, 0.0) for _ in range(3)]
+    for use, dtype in (((1, 0, 0), BF), ((1, 1, 1), F)):
+        gg = [t if u else None for t, u in zip(g, use)]
+        dx, dw = _backward(x, w, y, o, gg, 0.8, dtype)
+        dx2, dw2 = _backward(x, w, y, o, gg, 0.8, dtype)
+        torch.cuda.synchronize()
+        assert torch.equal(dx, dx2) and torch.equal(dw, dw2)
+        _check_bwd(x, w, y, o, gg, dx, dw, 0.8)
+
+
+def test_wide_rows_that_are_lost():
+    """As in test_rows_that_are_lost, with sums in parts."""
+    rng, x, w, y = _inputs(50, 2048, 400, 12)
+    y = y.clamp(0, 399)
+    o = _forward(x, w, y)
+    bad = x.clone()
+    bad[7, 3], bad[20, 1500] = NAN, float("inf")
+    o2 = _forward(bad, w, y)
+    lost = torch.zeros(50, dtype=torch.bool, device="cuda")
+    lost[[7, 20]] = True
+    for n in o:
+        assert o2[n][lost].isnan().all() and torch.equal(o2[n][~lost], o[n][~lost]), n
+    g = torch.ones(50, device="cuda")
+    dx, dw = _backward(bad, w, y, o2, (g, None, None))
+    assert dx[lost].isnan().all() and not dx[~lost].isnan().any() and dw.isnan().all()
+    # logits of -inf alone
+    big = torch.full((1, 2048), 3e38, dtype=BF, device="cuda")
+    o3 = _forward(big, torch.full_like(w, -1.0), y[:1].contiguous())
+    assert o3["lse"].item() == -math.inf and o3["entropy"].item() == 0 and o3["logp"].item() == -math.inf
+    # some of them
+    wneg = torch.zeros_like(w)
+    wneg[:200] = -1.0
+    o4 = _forward(big, wneg, torch.tensor([3], device="cuda"))
+    assert abs(o4["lse"].item() - math.log(200)) < 1e-5 and abs(o4["entropy"].item() - math.log(200)) < 1e-5 and o4["logp"].item() == -math.inf
+
+
 def test_gradient_against_differences():
     """Differences of the forward along a direction, by steps of x that bf16 holds: x on
     a grid of 2^-4 below 4, steps of 2^-4.  The third-order term is below

@@ -168,7 +168,7 @@ def test_workspace_sizes():
         f, b = nsp.nsp_linear_logp_fwd_workspace(T, dim, V), nsp.nsp_linear_logp_bwd_workspace(T, dim, V)
         assert f % 256 == 0 and b % 256 == 0
         rows = min(T + 256, 32768)
-        assert 0 < f <= 16 * rows * (V // 256 + 1) + 4 * rows + 512
+        assert 0 < f <= 16 * rows * (V // 256 + 1) + 4 * rows + 512 + 256 * 256 * 256 * 4
         pieces = max(1 << 29, 8192 * (T + 256)) + 512 * (T + 256)
         sums = 4 * (T + 256) * dim + 256 * 256 * 256 * 4
         assert 0 < b <= 2 * (T + 256) * (dim + 64) + 28 * (T + 256) + pieces + 2 * sums + (1 << 20), (T, dim, V, b)
