@@ -742,8 +742,13 @@ hipError_t launch_linear_logp_bwd(const LinearArgs &a, hipStream_t s) {
     e = hipGetLastError();
   }
   if (e != hipSuccess) return e;
-  b.sums_x = b.f.pieces > 1 || b.f.split_x > 1;
   b.tiles_dim = (int)plan::ceil_div(a.dim, plan::kTileP);
+  if (a.dx && a.dw) {
+    const int64_t x = b.tiles_dim * plan::ceil_div(a.n_tokens, b.f.tile_x), w = b.tiles_dim * (b.f.piece / plan::kTileP) * b.f.split_w;
+    if (x * b.f.split_x <= plan::kUnits)
+      b.f.split_x = plan::linear_split_beside(b.f.split_x, x, b.f.piece, w, plan::ceil_div(a.n_tokens, b.f.split_w));
+  }
+  b.sums_x = b.f.pieces > 1 || b.f.split_x > 1;
   for (int p = 0; p < b.f.pieces; ++p) {
     b.v0 = p * b.f.piece;
     b.n_v = a.vocab - b.v0 < b.f.piece ? a.vocab - b.v0 : b.f.piece;

@@ -82,6 +82,24 @@ constexpr int linear_split(int64_t tiles, int64_t n_k) {
   s = s < most ? s : most;
   return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
 }
+// Parts of dx's sums where its tiles (n_x a part) run before n_w tiles of dw in one launch:
+// those up to `most` that let the compute units end soonest.  A tile takes its
+// stages of 64 k and some 4 to store.  (Calls with `most` and with these, us: 777 x 1000 x
+// 50021, where 16 parts leave a fourth turn of 16 tiles of dw, 295 and 291; 64 x 1024 x
+// 32000 56 and 49; 300 x 2048 x 4000 58 and 52; 300 x 1024 x 50000 152 and 153.)
+constexpr int linear_split_beside(int most, int64_t n_x, int64_t k_x, int64_t n_w, int64_t k_w) {
+  int best = most;
+  int64_t least = INT64_MAX;
+  for (int s = most; s >= 1 && 2 * s >= most; --s) {
+    const int64_t x = ceil_div(ceil_div(k_x, s), 64) + 4, w = ceil_div(k_w, 64) + 4, idle = kUnits - n_x * s;
+    const int64_t beside = idle * (x / w), left = n_w > beside ? n_w - beside : 0, end = x + ceil_div(left, kUnits) * w;
+    if (end < least) {
+      least = end;
+      best = s;
+    }
+  }
+  return best;
+}
 // Tokens that one workgroup finds the rows of, which then every workgroup of the
 // gathering does for itself.
 constexpr int kLinearFew = 1024;

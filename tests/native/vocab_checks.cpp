@@ -82,6 +82,11 @@ static void linear_plans(int64_t T, int dim, int V) {
   const int64_t cols = plan::ceil_div(dim, plan::kTileP);
   CHECK((b.piece / plan::kTileP * (b.rows / b.tile) + 8) * 512 < int64_t(1) << 32);
   CHECK(cols * plan::ceil_div(b.rows, b.tile_x) * b.split_x + cols * (b.piece / plan::kTileP) * b.split_w < INT32_MAX - 16);
+  const int64_t n_x = cols * plan::ceil_div(T, b.tile_x);
+  if (n_x * b.split_x <= plan::kUnits) {
+    const int beside = plan::linear_split_beside(b.split_x, n_x, b.piece, cols * (b.piece / plan::kTileP) * b.split_w, plan::ceil_div(T, b.split_w));
+    CHECK(beside >= 1 && beside <= b.split_x);
+  }
   // one after another, none over the next
   const size_t off[] = {b.count_off, b.order_off, b.place_off, b.coef_off, b.target_off, b.x_off, b.dl_off, b.sum_x_off, b.sum_w_off, b.bytes};
   const size_t need[] = {4, (size_t)b.rows * 4, (size_t)T * 4, (size_t)b.rows * 16, (size_t)b.rows * 4, (size_t)T * b.dim * 2,

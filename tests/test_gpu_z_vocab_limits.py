@@ -273,3 +273,17 @@ def test_embedding_gradient_with_and_without_a_sort(T, dim, wt, dt):
         if one >= 0:
             want[one] = dy.double().sum(0)
         assert torch.equal(wide[:, :dim], want.to(wt)) and bool((wide[:, dim:] == 7).all())
+
+
+@pytest.mark.parametrize("T,dim", [(1, 1 << 20), (2, 1 << 20), (20, 70001), (32, 40000), (33, 40000)])
+def test_embedding_of_widest_rows(T, dim):
+    """Few tokens of wide rows: with and without a sort, one chunk and two."""
+    V = 5
+    ids, dy, w = _ids(T, V), _whole(T, dim).float(), _whole(V, dim)
+    ids[T // 2:] = 3
+    dw = torch.full((V, dim), float("nan"), device="cuda")
+    nsp.nsp_embedding_bwd(ids, dy, dw, _ws(nsp.nsp_embedding_bwd_workspace(T, dim, V)))
+    assert torch.equal(dw.double(), _count(ids, dy, V))
+    y = _e(T, dim)
+    nsp.nsp_embedding_fwd(ids, w, y, scale=2.0)
+    assert torch.equal(y, 2 * w[ids].float())
