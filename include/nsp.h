@@ -725,9 +725,10 @@ nsp_status nsp_linear_logp_fwd(int64_t n_tokens, int32_t dim, int32_t vocab, con
  *     da_v = scale (g_logp (1[v = target] - p_v) + g_lse p_v
  *                   - g_entropy p_v (z_v - lse + entropy))
  *     dx[t] = sum_v da[t][v] w[v],   dw[v] = sum_t da[t][v] x[t]
- * da is rounded to bf16 (half a step of it, 2^-8, an element) for the matrix
- * cores; sums are float32, rounded once to grad_dtype.  A token whose gradients are
- * all 0 (an ignored target takes g_logp as 0), or whose lse is -inf, takes no part,
+ * da is rounded to bf16 (half a step of it, 2^-8, an element; in calls of up to 128
+ * tokens to two of them, 2^-16) for the matrix cores; sums are float32, rounded once
+ * to grad_dtype.  A token whose gradients are all 0 (an ignored target takes g_logp
+ * as 0), or whose lse is -inf, takes no part,
  * whatever its row of x holds, and has dx = 0.  An lse of NaN or +inf makes the
  * token's dx and all of dw NaN.
  *   lse         the forward's; entropy too, needed with g_entropy

@@ -19,8 +19,9 @@
 //     dl = scale (k0 p + k1 p ln p + 1[target]) of the piece's logits, bf16
 //     dw[piece] = dl^T x,   dx += dl w[piece]
 // dl is rounded to bf16 (half a step, 2^-8 of each term at most, as independent
-// signs: next to the result's own rounding), which the matrix instructions take;
-// sums are float32, over pieces too.
+// signs: next to the result's own rounding), which the matrix instructions take; of up to
+// 128 tokens, where those roundings do not average and the weight's bytes are the time,
+// the rest goes in as a second row.  Sums are float32, over pieces too.
 #include "gemm_tile.hpp"
 #include "row_common.hpp"
 #include "vocab_internal.hpp"
@@ -346,9 +347,9 @@ struct BwdTiles {
   int *place;                  // [tokens]: a token's row, -1: it has no gradient
   float4 *coef;                // [rows]: lse, k0, k1, the target's
   int *target;                 // [rows], -1: none
-  char *x;                     // gathered rows [rows][f.dim]
-  char *dl;                    // [rows][piece]
-  float *sum_x, *sum_w;        // [split][rows][dim], [split][piece][dim]
+  char *x;                     // gathered rows [copies][rows][f.dim]; second copies follow the last first
+  char *dl;                    // [copies][rows][piece], likewise
+  float *sum_x, *sum_w;        // [split][copies][rows][dim], [split][piece][dim]
   int v0, n_v;                 // the piece
   bool first, last;            // of the pieces
   bool sums_x;                 // dx goes by float32 sums
@@ -399,13 +400,17 @@ __device__ __forceinline__ int count_before(bool some, int (&sums)[16], int &n) 
   return before;
 }
 
-// A token's hidden row to its place; dx of a token without one is zero.
-__device__ __forceinline__ void gather_row(const BwdTiles &b, int64_t t, int row) {
+// A token's hidden row to its place, and to another where that is not the same; dx of a
+// token without one is zero.
+__device__ __forceinline__ void gather_row(const BwdTiles &b, int64_t t, int row, int another) {
   const LinearArgs &a = b.a;
   const int lane = threadIdx.x & 63;
   if (row >= 0) {
     const u32x4 *from = (const u32x4 *)(a.x + 2 * t * a.x_stride);
     u32x4 *to = (u32x4 *)(b.x + 2 * (int64_t)row * b.f.dim);
+    for (int i = lane; i < a.dim / 8; i += 64) to[i] = from[i];
+    if (another == row) return;
+    to = (u32x4 *)(b.x + 2 * (int64_t)another * b.f.dim);
     for (int i = lane; i < a.dim / 8; i += 64) to[i] = from[i];
   } else if (a.dx) {
     u32x4 *to = (u32x4 *)(a.dx + (a.g_f32 ? 4 : 2) * t * a.dx_stride);
@@ -430,7 +435,7 @@ __global__ __launch_bounds__(1024) void linear_rows_kernel(BwdTiles b) {
 
 __global__ __launch_bounds__(256) void linear_gather_kernel(BwdTiles b) {
   const int wave = (int)threadIdx.x >> 6;
-  for (int64_t t = (int64_t)blockIdx.x * 4 + wave; t < b.a.n_tokens; t += (int64_t)gridDim.x * 4) gather_row(b, t, b.place[t]);
+  for (int64_t t = (int64_t)blockIdx.x * 4 + wave; t < b.a.n_tokens; t += (int64_t)gridDim.x * 4) gather_row(b, t, b.place[t], b.place[t]);
 }
 
 // Both, of up to kLinearFew tokens: every workgroup finds all places for itself.
@@ -448,7 +453,13 @@ __global__ __launch_bounds__(1024) void linear_rows_gather_kernel(BwdTiles b) {
   }
   __syncthreads();
   const int wave = (int)threadIdx.x >> 6;
-  for (int r = (int)blockIdx.x * 16 + wave; r < b.a.n_tokens; r += (int)gridDim.x * 16) gather_row(b, r, place[r]);
+  for (int r = (int)blockIdx.x * 16 + wave; r < b.a.n_tokens; r += (int)gridDim.x * 16) gather_row(b, r, place[r], place[r] + (b.f.copies > 1 ? n : 0));
+}
+
+// What rounding to bf16 leaves of x.
+__device__ __forceinline__ float left_of(float x) {
+  const float r = x - (float)(bf16)x;
+  return fabsf(r) < -kNegInf ? r : 0.f;          // (an infinity and a NaN are whole)
 }
 
 // dl of a piece.
@@ -490,16 +501,29 @@ __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void
 #pragma unroll
         for (int i = 0; i < 16; ++i) x.acc[q][p][i] += 32 * p + p_of(i, h) == y ? k.w : 0.f;
     }
-    char *out = b.dl + 2 * ((int64_t)r0 * b.f.piece + vw);
-    put_rows<P::BP, false>(x.acc[q], smem + x.wave * (2048 * P::BP), 32, 32 * P::BP, x.lane,
-                           [&](int row, int byte, f32x4 v) { *(f32x4 *)(out + (int64_t)row * 2 * b.f.piece + byte) = v; });
+    const auto put = [&](int64_t first, int rows) {
+      char *out = b.dl + 2 * (first * b.f.piece + vw);
+      put_rows<P::BP, false>(x.acc[q], smem + x.wave * (2048 * P::BP), rows, 32 * P::BP, x.lane,
+                             [&](int row, int byte, f32x4 v) { *(f32x4 *)(out + (int64_t)row * 2 * b.f.piece + byte) = v; });
+    };
+    if (NQ > plan::kLinearTwice || b.f.copies == 1) {
+      put(r0, 32);
+    } else {                                       // two rows a token
+      put(r0, n - r0);
+#pragma unroll
+      for (int p = 0; p < P::BP; ++p)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x.acc[q][p][i] = left_of(x.acc[q][p][i]);
+      put((int64_t)n + r0, n - r0);
+    }
   }
 }
 
 // dl of a piece from logits in parts: eight columns a thread.
 __global__ __launch_bounds__(256) void linear_dl_parts_kernel(BwdTiles b, LogitParts z) {
   const int vecs = b.f.piece / 8;
-  const int64_t all = (int64_t)*b.count * vecs;
+  const int n = *b.count;
+  const int64_t all = (int64_t)n * vecs;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
     const int r = (int)(i / vecs), v = (int)(i - (int64_t)r * vecs) * 8;
     const float4 k = b.coef[r];
@@ -512,6 +536,11 @@ __global__ __launch_bounds__(256) void linear_dl_parts_kernel(BwdTiles b, LogitP
       o[e] = fast_exp2(fminf(d, 0.f)) * (k.z != 0.f ? k.y + k.z * fmaxf(d, -200.f) : k.y) + (e == y ? k.w : 0.f);
     }
     *(u32x4 *)(b.dl + 2 * ((int64_t)r * b.f.piece + v)) = pack<bf16>(o);
+    if (b.f.copies > 1) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = left_of(o[e]);
+      *(u32x4 *)(b.dl + 2 * ((int64_t)(n + r) * b.f.piece + v)) = pack<bf16>(o);
+    }
   }
 }
 
@@ -551,7 +580,7 @@ typedef Product<kAcross, kAcross, 256, 256, 2, 4> DwTile;
 template <int NQ>
 __device__ __forceinline__ void dx_tile(const BwdTiles &b, int id, char *smem) {
   typedef typename DxTile<NQ>::P P;
-  const int n = *b.count, dim = b.a.dim;
+  const int n = *b.count * b.f.copies, dim = b.a.dim;
   tile::Place at;
   if (!at.find(id, b.tiles_dim, (n + NQ - 1) / NQ, b.f.split_x, kGroup)) return;
   P x;
@@ -562,7 +591,7 @@ __device__ __forceinline__ void dx_tile(const BwdTiles &b, int id, char *smem) {
         typename P::LoadQ(b.dl, b.f.piece, q0, n, k0, n_k, x.wave, x.lane), n_k);
   const auto row = [&](int es) { return [=, &b](int r) { return b.a.dx + (int64_t)b.order[r] * b.a.dx_stride * es; }; };
   if (b.sums_x) {
-    float *sums = b.sum_x + (int64_t)at.part * b.f.rows * dim;
+    float *sums = b.sum_x + (int64_t)at.part * b.f.copies * b.f.rows * dim;
     put_product<P, kSums>(x, smem, p0, q0, n, dim, !b.first, [&](int r) { return (char *)(sums + (int64_t)r * dim); });
   } else if (b.a.g_f32) {
     put_product<P, kF32>(x, smem, p0, q0, n, dim, false, row(4));
@@ -577,7 +606,7 @@ __device__ __forceinline__ void dw_tile(const BwdTiles &b, int id, char *smem) {
   tile::Place at;
   if (!at.find(id, b.tiles_dim, (int)plan::ceil_div(b.n_v, P::NQ), b.f.split_w, kGroup)) return;
   P x;
-  const int n = *b.count;
+  const int n = *b.count * b.f.copies;
   const int len = (int)plan::round_up(plan::ceil_div(n, b.f.split_w), tile::kStep);
   const int k0 = at.part * len, n_k = max(0, min(n - k0, len));
   const int p0 = at.p * P::NP, q0 = at.q * P::NQ;
@@ -606,21 +635,23 @@ __global__ __launch_bounds__(512, 2) void linear_grads_kernel(BwdTiles b) {
 // The parts' sums, in order, as rows of the gradient.
 template <bool F32, bool DX>
 __global__ __launch_bounds__(256) void linear_sums_kernel(BwdTiles b) {
-  const int rows = DX ? *b.count : b.n_v, dim = b.a.dim, parts = DX ? b.f.split_x : b.f.split_w;
-  const int64_t per = (DX ? b.f.rows : (int64_t)b.f.piece) * dim;
+  const int rows = DX ? *b.count : b.n_v, dim = b.a.dim, parts = DX ? b.f.split_x : b.f.split_w, copies = DX ? b.f.copies : 1;
+  const int64_t per = (DX ? (int64_t)b.f.copies * b.f.rows : (int64_t)b.f.piece) * dim;
   const float *sums = DX ? b.sum_x : b.sum_w;
   const int vecs = dim / 4;
   const int64_t n = (int64_t)rows * vecs;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
     const int r = (int)(i / vecs), c = (int)(i - (int64_t)r * vecs) * 4;
-    const float *from = sums + (int64_t)r * dim + c;
-    f32x4 sum = *(const f32x4 *)from;
-    for (int p0 = 1; p0 < parts; p0 += 8) {
-      f32x4 v[8];
+    f32x4 sum = {};
+    for (int k = 0; k < copies; ++k) {
+      const float *from = sums + ((int64_t)k * rows + r) * dim + c;
+      for (int p0 = 0; p0 < parts; p0 += 8) {
+        f32x4 v[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = p0 + j < parts ? *(const f32x4 *)(from + (p0 + j) * per) : f32x4{};
+        for (int j = 0; j < 8; ++j) v[j] = p0 + j < parts ? *(const f32x4 *)(from + (p0 + j) * per) : f32x4{};
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum += v[j];
+        for (int j = 0; j < 8; ++j) sum += v[j];
+      }
     }
     char *row = DX ? b.a.dx + (int64_t)b.order[r] * b.a.dx_stride * (F32 ? 4 : 2) : b.a.dw + (int64_t)(b.v0 + r) * b.a.dw_stride * (F32 ? 4 : 2);
     if constexpr (F32) *(f32x4 *)(row + 4 * c) = sum;
@@ -658,7 +689,7 @@ hipError_t launch_grads(const BwdTiles &b, hipStream_t s) {
 // us apart, 20 together; where both fill them the two together are 1% slower.)
 template <int NQ>
 hipError_t grads(BwdTiles b, hipStream_t s) {
-  b.grid_x = b.a.dx ? grid_of(b.tiles_dim * plan::ceil_div(b.f.rows, NQ) * b.f.split_x) : 0;
+  b.grid_x = b.a.dx ? grid_of(b.tiles_dim * plan::ceil_div(b.f.copies * b.f.rows, NQ) * b.f.split_x) : 0;
   b.grid_w = b.a.dw ? grid_of(b.tiles_dim * plan::ceil_div(b.n_v, DwTile::NQ) * b.f.split_w) : 0;
   if (b.grid_x <= plan::kUnits || b.grid_w == 0) return launch_grads<NQ>(b, s);
   BwdTiles w = b;
@@ -744,11 +775,11 @@ hipError_t launch_linear_logp_bwd(const LinearArgs &a, hipStream_t s) {
   if (e != hipSuccess) return e;
   b.tiles_dim = (int)plan::ceil_div(a.dim, plan::kTileP);
   if (a.dx && a.dw) {
-    const int64_t x = b.tiles_dim * plan::ceil_div(a.n_tokens, b.f.tile_x), w = b.tiles_dim * (b.f.piece / plan::kTileP) * b.f.split_w;
+    const int64_t x = b.tiles_dim * plan::ceil_div(b.f.copies * a.n_tokens, b.f.tile_x), w = b.tiles_dim * (b.f.piece / plan::kTileP) * b.f.split_w;
     if (x * b.f.split_x <= plan::kUnits)
-      b.f.split_x = plan::linear_split_beside(b.f.split_x, x, b.f.piece, w, plan::ceil_div(a.n_tokens, b.f.split_w));
+      b.f.split_x = plan::linear_split_beside(b.f.split_x, x, b.f.piece, w, plan::ceil_div(b.f.copies * a.n_tokens, b.f.split_w));
   }
-  b.sums_x = b.f.pieces > 1 || b.f.split_x > 1;
+  b.sums_x = b.f.pieces > 1 || b.f.split_x > 1 || b.f.copies > 1;
   for (int p = 0; p < b.f.pieces; ++p) {
     b.v0 = p * b.f.piece;
     b.n_v = a.vocab - b.v0 < b.f.piece ? a.vocab - b.v0 : b.f.piece;

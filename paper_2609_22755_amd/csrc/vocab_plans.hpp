@@ -104,7 +104,16 @@ constexpr int linear_split_beside(int most, int64_t n_x, int64_t k_x, int64_t n_
 // gathering does for itself.
 constexpr int kLinearFew = 1024;
 
+// Tokens up to which the gradient of the logits goes into the products as two bf16
+// numbers, itself and what its rounding leaves, as twice the rows.  Its roundings average
+// over many tokens; over few they show (relative 2-norms of bf16 gradients 0.0017 instead of
+// 0.0022 to 0.0026, what the result's own rounding makes being 0.0017).  (us with one row and
+// two: 4 x 4616 x 2740 39 and 42, 25 x 384 x 29140 33 and 40, 64 x 1024 x 32000 50 and 64, 100
+// x 704 x 12000 42 and 52.)
+constexpr int kLinearTwice = 128;
+
 struct LinearBwd {
+  int copies;                  // rows of a token
   int tile;                    // tokens of a tile of logits
   int tile_x;                  // tokens of a tile of dx
   int64_t rows;                // tokens, in whole tiles
@@ -120,6 +129,7 @@ struct LinearBwd {
 // 6 T dim piece operations: 2% at pieces of 32768).
 constexpr LinearBwd linear_bwd(int64_t n_tokens, int dim, int vocab) {
   LinearBwd f{};
+  f.copies = n_tokens <= kLinearTwice ? 2 : 1;
   f.tile = linear_tile(n_tokens, vocab);
   f.rows = round_up(n_tokens, f.tile);
   f.dim = (int)round_up(dim, 64);
@@ -131,7 +141,7 @@ constexpr LinearBwd linear_bwd(int64_t n_tokens, int dim, int vocab) {
   f.pieces = (int)ceil_div(all, f.piece);
   const int64_t cols = ceil_div(dim, kTileP);
   f.tile_x = n_tokens <= 64 ? 64 : 256;
-  f.split_x = linear_split(cols * ceil_div(n_tokens, f.tile_x), f.piece);
+  f.split_x = linear_split(cols * ceil_div(f.copies * n_tokens, f.tile_x), f.piece);
   f.split_w = linear_split(cols * (f.piece / kTileP), n_tokens);
   size_t at = 0;
   f.count_off = at, at += 256;
@@ -139,10 +149,10 @@ constexpr LinearBwd linear_bwd(int64_t n_tokens, int dim, int vocab) {
   f.place_off = at, at += pad256((size_t)f.rows * 4);
   f.coef_off = at, at += pad256((size_t)f.rows * 16);
   f.target_off = at, at += pad256((size_t)f.rows * 4);
-  f.x_off = at, at += pad256((size_t)f.rows * f.dim * 2);
-  f.dl_off = at, at += pad256((size_t)f.rows * f.piece * 2);
+  f.x_off = at, at += pad256((size_t)f.copies * f.rows * f.dim * 2);
+  f.dl_off = at, at += pad256((size_t)f.copies * f.rows * f.piece * 2);
   f.sum_x_off = at;
-  if (f.pieces > 1 || f.split_x > 1) at += pad256((size_t)f.split_x * f.rows * dim * 4);
+  if (f.pieces > 1 || f.split_x > 1 || f.copies > 1) at += pad256((size_t)f.split_x * f.copies * f.rows * dim * 4);
   f.sum_w_off = at;
   if (f.split_w > 1) at += pad256((size_t)f.split_w * f.piece * dim * 4);
   // the logits' parts are read before those sums begin (more than one part: one piece)

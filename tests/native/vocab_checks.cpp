@@ -75,22 +75,22 @@ static void linear_plans(int64_t T, int dim, int V) {
   CHECK(b.dim >= dim && b.dim % 64 == 0);
   CHECK(b.split_x >= 1 && b.split_x <= 64 && b.split_w >= 1 && b.split_w <= 64);
   CHECK(b.split_z == 1 || (b.pieces == 1 && dim / b.split_z >= 512));
-  CHECK(b.z_off >= b.dl_off + (size_t)b.rows * b.piece * 2 && b.bytes >= b.z_off + (b.split_z > 1 ? (size_t)b.split_z * b.rows * b.piece * 4 : 0));
+  CHECK(b.z_off >= b.dl_off + (size_t)b.copies * b.rows * b.piece * 2 && b.bytes >= b.z_off + (b.split_z > 1 ? (size_t)b.split_z * b.rows * b.piece * 4 : 0));
   // a part of 256 k at least
   CHECK(b.split_x == 1 || b.piece / b.split_x >= 256);
   CHECK(b.split_w == 1 || T / b.split_w >= 256);
   const int64_t cols = plan::ceil_div(dim, plan::kTileP);
   CHECK((b.piece / plan::kTileP * (b.rows / b.tile) + 8) * 512 < int64_t(1) << 32);
-  CHECK(cols * plan::ceil_div(b.rows, b.tile_x) * b.split_x + cols * (b.piece / plan::kTileP) * b.split_w < INT32_MAX - 16);
-  const int64_t n_x = cols * plan::ceil_div(T, b.tile_x);
+  CHECK(cols * plan::ceil_div(b.copies * b.rows, b.tile_x) * b.split_x + cols * (b.piece / plan::kTileP) * b.split_w < INT32_MAX - 16);
+  const int64_t n_x = cols * plan::ceil_div(b.copies * T, b.tile_x);
   if (n_x * b.split_x <= plan::kUnits) {
     const int beside = plan::linear_split_beside(b.split_x, n_x, b.piece, cols * (b.piece / plan::kTileP) * b.split_w, plan::ceil_div(T, b.split_w));
     CHECK(beside >= 1 && beside <= b.split_x);
   }
   // one after another, none over the next
   const size_t off[] = {b.count_off, b.order_off, b.place_off, b.coef_off, b.target_off, b.x_off, b.dl_off, b.sum_x_off, b.sum_w_off, b.bytes};
-  const size_t need[] = {4, (size_t)b.rows * 4, (size_t)T * 4, (size_t)b.rows * 16, (size_t)b.rows * 4, (size_t)T * b.dim * 2,
-                         (size_t)b.rows * b.piece * 2, b.pieces > 1 || b.split_x > 1 ? (size_t)b.split_x * T * dim * 4 : 0,
+  const size_t need[] = {4, (size_t)b.rows * 4, (size_t)T * 4, (size_t)b.rows * 16, (size_t)b.rows * 4, (size_t)b.copies * T * b.dim * 2,
+                         (size_t)b.copies * b.rows * b.piece * 2, b.pieces > 1 || b.split_x > 1 || b.copies > 1 ? (size_t)b.split_x * b.copies * b.rows * dim * 4 : 0,
                          b.split_w > 1 ? (size_t)b.split_w * (V < b.piece ? V : b.piece) * dim * 4 : 0};
   for (int i = 0; i < 9; ++i) CHECK(off[i] % 256 == 0 && off[i] + need[i] <= off[i + 1]);
 }

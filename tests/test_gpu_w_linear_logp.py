@@ -182,6 +182,25 @@ def test_wide_rows_that_are_lost():
     assert abs(o4["lse"].item() - math.log(200)) < 1e-5 and abs(o4["entropy"].item() - math.log(200)) < 1e-5 and o4["logp"].item() == -math.inf
 
 
+@pytest.mark.parametrize("T,dim,V", [(1, 64, 700), (31, 72, 500), (33, 264, 1000), (64, 64, 3000), (65, 1032, 300), (127, 136, 1000), (128, 2048, 300)])
+def test_gradients_of_few_tokens(T, dim, V):
+    """Up to 128 tokens the gradient of the logits is kept to 2^-16 of itself (twice half a step
+    of bf16); p's own errors, 2^-21 (1 + |z| + |lse|) and the logits', are below that at these
+    sizes.  The sizes' sum of dx and dw is at most 4 times the result (a target's against the
+    others'): relative 2-norms of float32 gradients within 4 (2^-16 + 2^-16) < 2^-12, a fifth
+    of what one rounding to bf16 leaves.  All weights alike, so that its errors are too."""
+    rng, x, w, y = _inputs(T, dim, V, 5 * T)
+    y = y.clamp(0, V - 1)
+    o = _forward(x, w, y)
+    g = torch.full((T,), -1.0 / 3.0, device="cuda")
+    dx, dw = _backward(x, w, y, o, (g, None, None), dtype=F)
+    want_dx, want_dw, _ = O.linear_logp_backward(as64(x), as64(w), y.cpu().numpy(), as64(o["lse"]), as64(o["entropy"]), as64(g))
+    for name, got, want in (("dx", dx, want_dx), ("dw", dw, want_dw)):
+        off = float(np.linalg.norm(as64(got) - want) / np.linalg.norm(want))
+        print(f"[rows] {name}: {off:.2e}", flush=True)
+        assert off <= 2.0 ** -12, (name, off)
+
+
 def test_gradient_against_differences():
     """Differences of the forward along a direction, by steps of x that bf16 holds: x on
     a grid of 2^-4 below 4, steps of 2^-4.  The third-order term is below
