@@ -689,7 +689,8 @@ nsp_status nsp_token_logp_bwd(nsp_dtype dtype, int64_t n_tokens, int32_t vocab, 
  * logits of one piece of the vocabulary (512 MB at most, but 8192 bytes a token from
  * 65536 tokens on), and float32 sums: 4 n_tokens dim bytes with more than one piece,
  * and up to 256 tiles of 256 KB each of dx and of dw where few tiles are split.
- * Calls whose logits make few tiles: up to 256 such tiles of them too. */
+ * Calls whose logits make few tiles: up to 256 such tiles of them too.  Calls of up
+ * to 128 tokens count them twice, but in the forward. */
 size_t nsp_linear_logp_fwd_workspace(int64_t n_tokens, int32_t dim, int32_t vocab);
 size_t nsp_linear_logp_bwd_workspace(int64_t n_tokens, int32_t dim, int32_t vocab);
 
@@ -728,9 +729,8 @@ nsp_status nsp_linear_logp_fwd(int64_t n_tokens, int32_t dim, int32_t vocab, con
  * da is rounded to bf16 (half a step of it, 2^-8, an element; in calls of up to 128
  * tokens to two of them, 2^-16) for the matrix cores; sums are float32, rounded once
  * to grad_dtype.  A token whose gradients are all 0 (an ignored target takes g_logp
- * as 0), or whose lse is -inf, takes no part,
- * whatever its row of x holds, and has dx = 0.  An lse of NaN or +inf makes the
- * token's dx and all of dw NaN.
+ * as 0), or whose lse is -inf, takes no part, whatever its row of x holds, and has
+ * dx = 0.  An lse of NaN or +inf makes the token's dx and all of dw NaN.
  *   lse         the forward's; entropy too, needed with g_entropy
  *   dx, dw      [n_tokens] and [vocab] rows of dim elements of grad_dtype (16-byte
  *               aligned, strides multiples of 16 bytes); either may be NULL (not

@@ -6,7 +6,8 @@
 //
 // Bound by HBM: the forward reads the logits once, the backward reads and writes
 // them once; what the alternatives cost (12 bytes and a few operations each) has to
-// hide behind that.
+// hide behind that.  bf16, 4096 x 151643 with 64 alternatives: 192 us (6.5 TB/s);
+// backward 8192 x 131072 with 20: 695 (6.2).
 //
 // Forward: the running sums of the log probabilities' pass (logit_sums.hpp)
 // without its weighted one; a workgroup takes a row, or a part of one where there
