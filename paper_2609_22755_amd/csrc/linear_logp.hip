@@ -481,7 +481,7 @@ __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void
 #pragma unroll
   for (int q = 0; q < P::BQ; ++q) {
     const int r0 = q0 + x.q0() + 32 * q, r = r0 + l32;
-    // (rows from n on and columns from n_v on are read by nobody)
+    // (rows from n on are read by nobody)
     const float4 k = r < n ? b.coef[r] : make_float4(0.f, 0.f, 0.f, 0.f);
     const int y = r < n ? b.target[r] - b.v0 - vw : -1;
     const auto each = [&](auto slope) {
@@ -500,6 +500,15 @@ __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void
       for (int p = 0; p < P::BP; ++p)
 #pragma unroll
         for (int i = 0; i < 16; ++i) x.acc[q][p][i] += 32 * p + p_of(i, h) == y ? k.w : 0.f;
+    }
+    // Columns from n_v on: dx's loads take eight at a time, so some of them meet zeros in the
+    // place of w's rows, and what their logit of 0 comes to need not be finite.
+    if (v0 + P::NP > b.n_v) {
+#pragma unroll
+      for (int p = 0; p < P::BP; ++p)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (vw + 32 * p + p_of(i, h) >= b.n_v) x.acc[q][p][i] = 0.f;
     }
     const auto put = [&](int64_t first, int rows) {
       char *out = b.dl + 2 * (first * b.f.piece + vw);
@@ -534,6 +543,7 @@ __global__ __launch_bounds__(256) void linear_dl_parts_kernel(BwdTiles b, LogitP
     for (int e = 0; e < 8; ++e) {
       const float d = ((e < 4 ? lo[e & 3] : hi[e & 3]) * b.a.scale - k.x) * kLog2e;
       o[e] = fast_exp2(fminf(d, 0.f)) * (k.z != 0.f ? k.y + k.z * fmaxf(d, -200.f) : k.y) + (e == y ? k.w : 0.f);
+      if (v + e >= b.n_v) o[e] = 0.f;              // (as above)
     }
     *(u32x4 *)(b.dl + 2 * ((int64_t)r * b.f.piece + v)) = pack<bf16>(o);
     if (b.f.copies > 1) {
