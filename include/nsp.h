@@ -687,7 +687,7 @@ nsp_status nsp_token_logp_bwd(nsp_dtype dtype, int64_t n_tokens, int32_t vocab, 
  * 32768 tokens at most (fewer from 2^19 vocabulary rows on: 1 GB, or 4096 tokens).
  * Backward: the hidden rows gathered (2 n_tokens dim bytes), the gradient of the
  * logits of one piece of the vocabulary (512 MB at most, but 8192 bytes a token from
- * 65536 tokens on), and float32 sums: 4 n_tokens dim bytes with more than one piece,
+ * 65536 tokens on; gradients of either type fit), and float32 sums: 4 n_tokens dim bytes with more than one piece,
  * and up to 256 tiles of 256 KB each of dx and of dw where few tiles are split.
  * Calls whose logits make few tiles: up to 256 such tiles of them too.  Calls of up
  * to 128 tokens count them twice, but in the forward. */
@@ -726,9 +726,12 @@ nsp_status nsp_linear_logp_fwd(int64_t n_tokens, int32_t dim, int32_t vocab, con
  *     da_v = scale (g_logp (1[v = target] - p_v) + g_lse p_v
  *                   - g_entropy p_v (z_v - lse + entropy))
  *     dx[t] = sum_v da[t][v] w[v],   dw[v] = sum_t da[t][v] x[t]
- * da is rounded to bf16 (half a step of it, 2^-8, an element; in calls of up to 128
- * tokens to two of them, 2^-16) for the matrix cores; sums are float32, rounded once
- * to grad_dtype.  A token whose gradients are all 0 (an ignored target takes g_logp
+ * da is rounded to bf16 for the matrix cores: with float32 gradients, and in calls of
+ * up to 128 tokens, to two bf16 numbers (2^-16 of an element); with bf16 gradients of
+ * more tokens to one (half a step, 2^-8: their relative 2-norm is off by 0.0022 to 0.0026,
+ * where rounding the results alone leaves 0.0017).  float32 gradients take the products of
+ * dx and dw twice (8192 x 4096 x 131072: 1.7 times as long).  Sums are float32, rounded
+ * once to grad_dtype.  A token whose gradients are all 0 (an ignored target takes g_logp
  * as 0), or whose lse is -inf, takes no part, whatever its row of x holds, and has
  * dx = 0.  An lse of NaN or +inf makes the token's dx and all of dw NaN.
  *   lse         the forward's; entropy too, needed with g_entropy

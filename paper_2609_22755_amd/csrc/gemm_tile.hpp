@@ -178,13 +178,20 @@ struct Product {
   // The sums over n_k k's; every wave of the workgroup.  Nothing is in flight
   // afterwards and every wave is past its last read.
   __device__ __forceinline__ void run(char *smem, LoadP lp, LoadQ lq, int n_k) {
-    constexpr int IP = LoadP::PER_WAVE, IQ = LoadQ::PER_WAVE;
-    const Reader<LP, BP> rp(0, p0(), lane);
-    const Reader<LQ, BQ> rq(kAtQ, q0(), lane);
+    clear();
+    add(smem, lp, lq, n_k);
+  }
+  __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int q = 0; q < BQ; ++q)
 #pragma unroll
       for (int p = 0; p < BP; ++p) acc[q][p] = f32x16{};
+  }
+  // The same, added to what is there.
+  __device__ __forceinline__ void add(char *smem, LoadP lp, LoadQ lq, int n_k) {
+    constexpr int IP = LoadP::PER_WAVE, IQ = LoadQ::PER_WAVE;
+    const Reader<LP, BP> rp(0, p0(), lane);
+    const Reader<LQ, BQ> rq(kAtQ, q0(), lane);
     const auto at_p = [&](int stage) { return smem + stage % kRingP * kBytesP; };
     const auto at_q = [&](int stage) { return smem + kAtQ + stage % kRingQ * kBytesQ; };
     const auto read_q = [&](Operands &x, int stage, int kb) {

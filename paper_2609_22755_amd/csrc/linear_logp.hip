@@ -18,10 +18,10 @@
 // gathered into rows side by side; then, piece by piece of the vocabulary,
 //     dl = scale (k0 p + k1 p ln p + 1[target]) of the piece's logits, bf16
 //     dw[piece] = dl^T x,   dx += dl w[piece]
-// dl is rounded to bf16 (half a step, 2^-8 of each term at most, as independent
-// signs: next to the result's own rounding), which the matrix instructions take; of up to
-// 128 tokens, where those roundings do not average and the weight's bytes are the time,
-// the rest goes in as a second row.  Sums are float32, over pieces too.
+// dl is rounded to bf16 (half a step, 2^-8 of each term at most), which the matrix
+// instructions take; for float32 gradients, and of up to 128 tokens, what that rounding
+// leaves goes in as a second number (2^-16; vocab_plans.hpp has what either costs).  Sums are
+// float32, over pieces too.
 #include "gemm_tile.hpp"
 #include "row_common.hpp"
 #include "vocab_internal.hpp"
@@ -348,7 +348,7 @@ struct BwdTiles {
   float4 *coef;                // [rows]: lse, k0, k1, the target's
   int *target;                 // [rows], -1: none
   char *x;                     // gathered rows [copies][rows][f.dim]; second copies follow the last first
-  char *dl;                    // [copies][rows][piece], likewise
+  char *dl;                    // [numbers][rows][piece]; copies likewise, second numbers of one copy from `rows` on
   float *sum_x, *sum_w;        // [split][copies][rows][dim], [split][piece][dim]
   int v0, n_v;                 // the piece
   bool first, last;            // of the pieces
@@ -515,15 +515,14 @@ __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void
       put_rows<P::BP, false>(x.acc[q], smem + x.wave * (2048 * P::BP), rows, 32 * P::BP, x.lane,
                              [&](int row, int byte, f32x4 v) { *(f32x4 *)(out + (int64_t)row * 2 * b.f.piece + byte) = v; });
     };
-    if (NQ > plan::kLinearTwice || b.f.copies == 1) {
-      put(r0, 32);
-    } else {                                       // two rows a token
-      put(r0, n - r0);
+    const bool pairs = NQ <= plan::kLinearTwice && b.f.copies > 1;   // two rows a token
+    put(r0, pairs ? n - r0 : 32);
+    if (b.f.numbers > 1) {
 #pragma unroll
       for (int p = 0; p < P::BP; ++p)
 #pragma unroll
         for (int i = 0; i < 16; ++i) x.acc[q][p][i] = left_of(x.acc[q][p][i]);
-      put((int64_t)n + r0, n - r0);
+      put((pairs ? n : b.f.rows) + r0, pairs ? n - r0 : 32);
     }
   }
 }
@@ -546,10 +545,10 @@ __global__ __launch_bounds__(256) void linear_dl_parts_kernel(BwdTiles b, LogitP
       if (v + e >= b.n_v) o[e] = 0.f;              // (as above)
     }
     *(u32x4 *)(b.dl + 2 * ((int64_t)r * b.f.piece + v)) = pack<bf16>(o);
-    if (b.f.copies > 1) {
+    if (b.f.numbers > 1) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] = left_of(o[e]);
-      *(u32x4 *)(b.dl + 2 * ((int64_t)(n + r) * b.f.piece + v)) = pack<bf16>(o);
+      *(u32x4 *)(b.dl + 2 * (((b.f.copies > 1 ? n : b.f.rows) + r) * b.f.piece + v)) = pack<bf16>(o);
     }
   }
 }
@@ -587,7 +586,8 @@ struct DxTile<64> { typedef Product<kAcross, kAlong, 256, 64, 4, 2> P; };
 // dw: p: columns, q: the piece's vocabulary rows, k: gathered rows.
 typedef Product<kAcross, kAcross, 256, 256, 2, 4> DwTile;
 
-template <int NQ>
+// ALONG: times that a product goes over its k's, each time with the next numbers of dl.
+template <int NQ, int ALONG>
 __device__ __forceinline__ void dx_tile(const BwdTiles &b, int id, char *smem) {
   typedef typename DxTile<NQ>::P P;
   const int n = *b.count * b.f.copies, dim = b.a.dim;
@@ -597,8 +597,11 @@ __device__ __forceinline__ void dx_tile(const BwdTiles &b, int id, char *smem) {
   const int len = (int)plan::round_up(plan::ceil_div(b.f.piece, b.f.split_x), tile::kStep);
   const int k0 = at.part * len, n_k = max(0, min(b.n_v - k0, len));
   const int p0 = at.p * P::NP, q0 = at.q * NQ;
-  x.run(smem, typename P::LoadP(b.a.w, b.a.w_stride, p0, dim, b.v0 + k0, n_k, x.wave, x.lane),
-        typename P::LoadQ(b.dl, b.f.piece, q0, n, k0, n_k, x.wave, x.lane), n_k);
+  x.clear();
+#pragma unroll
+  for (int i = 0; i < ALONG; ++i)
+    x.add(smem, typename P::LoadP(b.a.w, b.a.w_stride, p0, dim, b.v0 + k0, n_k, x.wave, x.lane),
+          typename P::LoadQ(b.dl + i * (2 * b.f.rows * b.f.piece), b.f.piece, q0, n, k0, n_k, x.wave, x.lane), n_k);
   const auto row = [&](int es) { return [=, &b](int r) { return b.a.dx + (int64_t)b.order[r] * b.a.dx_stride * es; }; };
   if (b.sums_x) {
     float *sums = b.sum_x + (int64_t)at.part * b.f.copies * b.f.rows * dim;
@@ -610,6 +613,7 @@ __device__ __forceinline__ void dx_tile(const BwdTiles &b, int id, char *smem) {
   }
 }
 
+template <int ALONG>
 __device__ __forceinline__ void dw_tile(const BwdTiles &b, int id, char *smem) {
   typedef DwTile P;
   const int dim = b.a.dim;
@@ -620,7 +624,11 @@ __device__ __forceinline__ void dw_tile(const BwdTiles &b, int id, char *smem) {
   const int len = (int)plan::round_up(plan::ceil_div(n, b.f.split_w), tile::kStep);
   const int k0 = at.part * len, n_k = max(0, min(n - k0, len));
   const int p0 = at.p * P::NP, q0 = at.q * P::NQ;
-  x.run(smem, P::LoadP(b.x, b.f.dim, p0, dim, k0, n_k, x.wave, x.lane), P::LoadQ(b.dl, b.f.piece, q0, b.n_v, k0, n_k, x.wave, x.lane), n_k);
+  x.clear();
+#pragma unroll
+  for (int i = 0; i < ALONG; ++i)
+    x.add(smem, P::LoadP(b.x, b.f.dim, p0, dim, k0, n_k, x.wave, x.lane),
+          P::LoadQ(b.dl + i * (2 * b.f.rows * b.f.piece), b.f.piece, q0, b.n_v, k0, n_k, x.wave, x.lane), n_k);
   const auto row = [&](int es) { return [=, &b](int r) { return b.a.dw + (int64_t)(b.v0 + r) * b.a.dw_stride * es; }; };
   if (b.f.split_w > 1) {
     float *sums = b.sum_w + (int64_t)at.part * b.f.piece * dim;
@@ -633,13 +641,13 @@ __device__ __forceinline__ void dw_tile(const BwdTiles &b, int id, char *smem) {
 }
 
 // dx's tiles, then dw's, of a piece.
-template <int NQ>
+template <int NQ, int ALONG>
 __global__ __launch_bounds__(512, 2) void linear_grads_kernel(BwdTiles b) {
   constexpr int kX = DxTile<NQ>::P::kLds;
   __shared__ __attribute__((aligned(1024))) char smem[kX > DwTile::kLds ? kX : DwTile::kLds];
   const int id = (int)blockIdx.x;
-  if (id < b.grid_x) dx_tile<NQ>(b, id, smem);
-  else dw_tile(b, id - b.grid_x, smem);
+  if (id < b.grid_x) dx_tile<NQ, ALONG>(b, id, smem);
+  else dw_tile<ALONG>(b, id - b.grid_x, smem);
 }
 
 // The parts' sums, in order, as rows of the gradient.
@@ -688,24 +696,24 @@ hipError_t dl_tiles(const BwdTiles &b, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <int NQ>
+template <int NQ, int ALONG>
 hipError_t launch_grads(const BwdTiles &b, hipStream_t s) {
   const int grid = b.grid_x + b.grid_w;
-  if (grid > 0) linear_grads_kernel<NQ><<<grid, 512, 0, s>>>(b);
+  if (grid > 0) linear_grads_kernel<NQ, ALONG><<<grid, 512, 0, s>>>(b);
   return hipGetLastError();
 }
 
 // In one launch, where dx alone would leave compute units idle.  (100 x 704 x 12000: 33
 // us apart, 20 together; where both fill them the two together are 1% slower.)
-template <int NQ>
+template <int NQ, int ALONG>
 hipError_t grads(BwdTiles b, hipStream_t s) {
   b.grid_x = b.a.dx ? grid_of(b.tiles_dim * plan::ceil_div(b.f.copies * b.f.rows, NQ) * b.f.split_x) : 0;
   b.grid_w = b.a.dw ? grid_of(b.tiles_dim * plan::ceil_div(b.n_v, DwTile::NQ) * b.f.split_w) : 0;
-  if (b.grid_x <= plan::kUnits || b.grid_w == 0) return launch_grads<NQ>(b, s);
+  if (b.grid_x <= plan::kUnits || b.grid_w == 0) return launch_grads<NQ, ALONG>(b, s);
   BwdTiles w = b;
   w.grid_x = b.grid_w = 0;
-  const hipError_t e = launch_grads<NQ>(w, s);
-  return e == hipSuccess ? launch_grads<NQ>(b, s) : e;
+  const hipError_t e = launch_grads<NQ, ALONG>(w, s);
+  return e == hipSuccess ? launch_grads<NQ, ALONG>(b, s) : e;
 }
 
 template <bool DX>
@@ -760,7 +768,8 @@ hipError_t launch_linear_logp_bwd(const LinearArgs &a, hipStream_t s) {
   }
   BwdTiles b{};
   b.a = a;
-  b.f = plan::linear_bwd(a.n_tokens, a.dim, a.vocab);
+  b.f = plan::linear_bwd(a.n_tokens, a.dim, a.vocab, a.g_f32);
+  const int along = b.f.numbers / b.f.copies;    // (more than 1: one copy, tiles of 256 tokens of dx)
   b.count = (int *)(a.ws + b.f.count_off);
   b.order = (int *)(a.ws + b.f.order_off);
   b.place = (int *)(a.ws + b.f.place_off);
@@ -787,7 +796,7 @@ hipError_t launch_linear_logp_bwd(const LinearArgs &a, hipStream_t s) {
   if (a.dx && a.dw) {
     const int64_t x = b.tiles_dim * plan::ceil_div(b.f.copies * a.n_tokens, b.f.tile_x), w = b.tiles_dim * (b.f.piece / plan::kTileP) * b.f.split_w;
     if (x * b.f.split_x <= plan::kUnits)
-      b.f.split_x = plan::linear_split_beside(b.f.split_x, x, b.f.piece, w, plan::ceil_div(b.f.copies * a.n_tokens, b.f.split_w));
+      b.f.split_x = plan::linear_split_beside(b.f.split_x, x, along * (int64_t)b.f.piece, w, plan::ceil_div(b.f.numbers * a.n_tokens, b.f.split_w));
   }
   b.sums_x = b.f.pieces > 1 || b.f.split_x > 1 || b.f.copies > 1;
   for (int p = 0; p < b.f.pieces; ++p) {
@@ -806,7 +815,7 @@ hipError_t launch_linear_logp_bwd(const LinearArgs &a, hipStream_t s) {
     } else {
       e = b.f.tile == 32 ? dl_tiles<32>(b, s) : b.f.tile == 64 ? dl_tiles<64>(b, s) : b.f.tile == 128 ? dl_tiles<128>(b, s) : dl_tiles<256>(b, s);
     }
-    if (e == hipSuccess) e = b.f.tile_x == 64 ? grads<64>(b, s) : grads<256>(b, s);
+    if (e == hipSuccess) e = along > 1 ? grads<256, 2>(b, s) : b.f.tile_x == 64 ? grads<64, 1>(b, s) : grads<256, 1>(b, s);
     if (e == hipSuccess && a.dw && b.f.split_w > 1) e = join_sums<false>(b, s);
     if (e == hipSuccess && a.dx && b.last && b.sums_x) e = join_sums<true>(b, s);
     if (e != hipSuccess) return e;

@@ -172,7 +172,7 @@ nsp_status nsp_linear_logp_fwd(int64_t n_tokens, int32_t dim, int32_t vocab, con
 size_t nsp_linear_logp_bwd_workspace(int64_t n_tokens, int32_t dim, int32_t vocab) {
   if (check_linear_sizes(n_tokens, dim, vocab) != NSP_OK || n_tokens == 0) return 0;
   set_error(NSP_OK, nullptr);
-  return nsp::plan::linear_bwd(n_tokens, dim, vocab).bytes;
+  return nsp::plan::linear_bwd_bytes(n_tokens, dim, vocab);
 }
 
 nsp_status nsp_linear_logp_bwd(nsp_dtype grad_dtype, int64_t n_tokens, int32_t dim, int32_t vocab, const nsp_rows *x,
@@ -200,7 +200,7 @@ nsp_status nsp_linear_logp_bwd(nsp_dtype grad_dtype, int64_t n_tokens, int32_t d
   NSP_TRY(check_array(targets, 8, some && g_logp, "targets"));
   NSP_TRY(check_array(entropy, 4, some && g_entropy, "entropy"));
   if (!dx && !dw) return set_error(NSP_OK, nullptr);
-  if (some) NSP_TRY(check_workspace(workspace, ws_bytes, nsp::plan::linear_bwd(n_tokens, dim, vocab).bytes));
+  if (some) NSP_TRY(check_workspace(workspace, ws_bytes, nsp::plan::linear_bwd_bytes(n_tokens, dim, vocab)));
   a.lse_in = lse;
   a.entropy_in = entropy;
   a.g_logp = g_logp;

@@ -104,16 +104,22 @@ constexpr int linear_split_beside(int most, int64_t n_x, int64_t k_x, int64_t n_
 // gathering does for itself.
 constexpr int kLinearFew = 1024;
 
-// Tokens up to which the gradient of the logits goes into the products as two bf16
-// numbers, itself and what its rounding leaves, as twice the rows.  Its roundings average
-// over many tokens; over few they show (relative 2-norms of bf16 gradients 0.0017 instead of
-// 0.0022 to 0.0026, what the result's own rounding makes being 0.0017).  (us with one row and
-// two: 4 x 4616 x 2740 39 and 42, 25 x 384 x 29140 33 and 40, 64 x 1024 x 32000 50 and 64, 100
-// x 704 x 12000 42 and 52.)
+// The gradient of the logits goes into the products as bf16, rounded once, or as two bf16
+// numbers, itself and what its rounding leaves (2^-16).  One rounding leaves some 0.0017 of a
+// gradient's 2-norm: a token's dx and a rare id's dw are a few terms, and there it does not
+// average.  Two numbers where the caller takes float32 gradients, of any number of tokens;
+// they are twice the products of dx and dw.  bf16 gradients, whose own rounding is 0.0017
+// too, take them up to so many tokens, where the weight's bytes are most of the time and the
+// second number is cheap (0.0017 instead of 0.0022 to 0.0026 in all; us with one number and two: 4 x
+// 4616 x 2740 39 and 42, 25 x 384 x 29140 33 and 40, 64 x 1024 x 32000 50 and 64, 100 x 704 x
+// 12000 42 and 52).  In such calls the second numbers are rows of their own beside the first,
+// one more tile's work at most; past them they go through the same tiles after the first
+// (along k), so that neither x nor dx's sums are there twice.
 constexpr int kLinearTwice = 128;
 
 struct LinearBwd {
   int copies;                  // rows of a token
+  int numbers;                 // bf16 numbers of an element of the logits' gradient
   int tile;                    // tokens of a tile of logits
   int tile_x;                  // tokens of a tile of dx
   int64_t rows;                // tokens, in whole tiles
@@ -127,15 +133,17 @@ struct LinearBwd {
 // some 2^28 elements of it (512 MB): large enough that adding dx's float32 sums
 // of one piece to the next costs little (a read and a write of T dim against
 // 6 T dim piece operations: 2% at pieces of 32768).
-constexpr LinearBwd linear_bwd(int64_t n_tokens, int dim, int vocab) {
+constexpr LinearBwd linear_bwd(int64_t n_tokens, int dim, int vocab, bool f32 = false) {
   LinearBwd f{};
   f.copies = n_tokens <= kLinearTwice ? 2 : 1;
+  f.numbers = f32 ? 2 : f.copies;
+  const int along = f.numbers / f.copies;        // times that a product goes over k
   f.tile = linear_tile(n_tokens, vocab);
   f.rows = round_up(n_tokens, f.tile);
   f.dim = (int)round_up(dim, 64);
   const int64_t all = round_up(vocab, kTileP);
-  int64_t piece = (int64_t(1) << 28) / (f.rows > 0 ? f.rows : 1) / kTileP * kTileP;
-  piece = piece < 4096 ? 4096 : piece;
+  int64_t piece = (int64_t(1) << 28) / (f.rows > 0 ? along * f.rows : 1) / kTileP * kTileP;
+  piece = piece < 4096 / along ? 4096 / along : piece;
   f.pieces = (int)(piece >= all ? 1 : ceil_div(all, piece));
   f.piece = (int)round_up(ceil_div(all, f.pieces), kTileP);
   f.pieces = (int)ceil_div(all, f.piece);
@@ -150,7 +158,7 @@ constexpr LinearBwd linear_bwd(int64_t n_tokens, int dim, int vocab) {
   f.coef_off = at, at += pad256((size_t)f.rows * 16);
   f.target_off = at, at += pad256((size_t)f.rows * 4);
   f.x_off = at, at += pad256((size_t)f.copies * f.rows * f.dim * 2);
-  f.dl_off = at, at += pad256((size_t)f.copies * f.rows * f.piece * 2);
+  f.dl_off = at, at += pad256((size_t)f.numbers * f.rows * f.piece * 2);
   f.sum_x_off = at;
   if (f.pieces > 1 || f.split_x > 1 || f.copies > 1) at += pad256((size_t)f.split_x * f.copies * f.rows * dim * 4);
   f.sum_w_off = at;
@@ -162,6 +170,11 @@ constexpr LinearBwd linear_bwd(int64_t n_tokens, int dim, int vocab) {
   at = at > z_end ? at : z_end;
   f.bytes = n_tokens > 0 ? at : 0;
   return f;
+}
+// Of gradients of either type.
+constexpr size_t linear_bwd_bytes(int64_t n_tokens, int dim, int vocab) {
+  const size_t a = linear_bwd(n_tokens, dim, vocab, false).bytes, b = linear_bwd(n_tokens, dim, vocab, true).bytes;
+  return a > b ? a : b;
 }
 
 // --------------------------------------------------------------- embedding --
