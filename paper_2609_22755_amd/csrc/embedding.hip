@@ -375,6 +375,7 @@ __global__ __launch_bounds__(kSortThreads) void embedding_move_kernel(SortArgs a
   for (int r = 0; r < kRounds; ++r) {
     if (first + 64 * r + lane >= a.n_tokens) continue;
     const uint32_t to = counts[wave][(x.key[r] >> a.shift) & (n_bins - 1)] + x.rank[r];
+    if (to >= (uint32_t)a.n_tokens) continue;    // (only where something else writes the workspace meanwhile)
     a.key_out[to] = x.key[r];
     a.token_out[to] = x.token[r];
   }
@@ -499,6 +500,8 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs s, int bits)
   const bool there = c0 < a.dim;
   const int lo = chunk * a.f.chunk, hi = min(lo + a.f.chunk, a.n_tokens);
   const Y *dy = (const Y *)a.y.data + col;
+  // (a row of dy also where something else writes the workspace meanwhile)
+  const auto row_at = [&](int at) { return dy + (int64_t)min(s.token[at], (uint32_t)a.n_tokens - 1) * a.y.ts; };
   float acc[N] = {};
   uint32_t id = s.key[lo];
   bool open = lo > 0 && s.key[lo - 1] == id;       // the id's rows began before the chunk
@@ -526,7 +529,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs s, int bits)
       const int at = min(p + i, hi - 1);
       ids[i] = s.key[at];
       raw[i] = u32x4{};
-      if (a.dim >= N && there && p + i < hi && ids[i] < (uint32_t)a.vocab) raw[i] = load16(dy + (int64_t)s.token[at] * a.y.ts);
+      if (a.dim >= N && there && p + i < hi && ids[i] < (uint32_t)a.vocab) raw[i] = load16(row_at(at));
     }
   };
   fetch(lo);
@@ -545,7 +548,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs s, int bits)
       }
       float v[N];
       if (a.dim >= N) unpack<Y>(now[i], v);
-      else load_some(dy + (int64_t)s.token[p + i] * a.y.ts, there && id < (uint32_t)a.vocab ? cnt : 0, 0.f, v);
+      else load_some(row_at(p + i), there && id < (uint32_t)a.vocab ? cnt : 0, 0.f, v);
 #pragma unroll
       for (int e = 0; e < N; ++e) acc[e] += v[e];
     }
