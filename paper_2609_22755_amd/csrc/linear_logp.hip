@@ -83,6 +83,11 @@ __device__ __forceinline__ void put_rows(const f32x16 *acc, char *lds, int rows,
   }
 }
 
+// What is read back from the workspace as a number of rows or a row stays among the n
+// there are, also where something else writes the workspace meanwhile.
+__device__ __forceinline__ int rows_of(const int *count, int64_t n) { return (int)min((uint32_t)*count, (uint32_t)n); }
+__device__ __forceinline__ int64_t row_of(const int *order, int64_t at, int64_t n) { return min((uint32_t)order[at], (uint32_t)n - 1); }
+
 // ------------------------------------------------- logits of few tiles --
 
 // Sums of a part of dim, in float32: [part][rows][cols], for calls whose tiles are fewer than
@@ -91,7 +96,7 @@ __device__ __forceinline__ void put_rows(const f32x16 *acc, char *lds, int rows,
 struct LogitParts {
   const char *w, *x;
   int64_t w_stride, x_stride;
-  const int *count;            // rows, null: n
+  const int *count;            // rows of the n, null: all
   int n, vocab, dim;
   int split, tiles_p;
   int64_t rows, cols;          // whole tiles
@@ -117,7 +122,7 @@ __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void
   typedef typename LogitTile<NQ>::P P;
   static_assert(P::kLds >= P::NW * 4096 * P::BP, "room for the rows that are stored");
   __shared__ __attribute__((aligned(1024))) char smem[P::kLds];
-  const int n = f.count ? *f.count : f.n;
+  const int n = f.count ? rows_of(f.count, f.n) : f.n;
   tile::Place at;
   if (!at.find(blockIdx.x, f.tiles_p, (n + NQ - 1) / NQ, f.split, kGroup)) return;
   P x;
@@ -350,6 +355,8 @@ struct BwdTiles {
   char *x;                     // gathered rows [copies][rows][f.dim]; second copies follow the last first
   char *dl;                    // [numbers][rows][piece]; copies likewise, second numbers of one copy from `rows` on
   float *sum_x, *sum_w;        // [split][copies][rows][dim], [split][piece][dim]
+  __device__ __forceinline__ int rows() const { return rows_of(count, a.n_tokens); }
+  __device__ __forceinline__ int64_t token(int r) const { return row_of(order, r, a.n_tokens); }
   int v0, n_v;                 // the piece
   bool first, last;            // of the pieces
   bool sums_x;                 // dx goes by float32 sums
@@ -435,7 +442,10 @@ __global__ __launch_bounds__(1024) void linear_rows_kernel(BwdTiles b) {
 
 __global__ __launch_bounds__(256) void linear_gather_kernel(BwdTiles b) {
   const int wave = (int)threadIdx.x >> 6;
-  for (int64_t t = (int64_t)blockIdx.x * 4 + wave; t < b.a.n_tokens; t += (int64_t)gridDim.x * 4) gather_row(b, t, b.place[t], b.place[t]);
+  for (int64_t t = (int64_t)blockIdx.x * 4 + wave; t < b.a.n_tokens; t += (int64_t)gridDim.x * 4) {
+    const int row = (int)min((int64_t)b.place[t], b.a.n_tokens - 1);
+    gather_row(b, t, row, row);
+  }
 }
 
 // Both, of up to kLinearFew tokens: every workgroup finds all places for itself.
@@ -468,7 +478,7 @@ __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void
   typedef typename LogitTile<NQ>::P P;
   static_assert(P::kLds >= 512 * 32 * P::BP, "room for the rows that are stored");
   __shared__ __attribute__((aligned(1024))) char smem[P::kLds];
-  const int n = *b.count;
+  const int n = b.rows();
   tile::Place at;
   if (!at.find(blockIdx.x, tiles_p, (n + NQ - 1) / NQ, 1, kGroup)) return;
   P x;
@@ -530,7 +540,7 @@ __global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void
 // dl of a piece from logits in parts: eight columns a thread.
 __global__ __launch_bounds__(256) void linear_dl_parts_kernel(BwdTiles b, LogitParts z) {
   const int vecs = b.f.piece / 8;
-  const int n = *b.count;
+  const int n = b.rows();
   const int64_t all = (int64_t)n * vecs;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
     const int r = (int)(i / vecs), v = (int)(i - (int64_t)r * vecs) * 8;
@@ -590,7 +600,7 @@ typedef Product<kAcross, kAcross, 256, 256, 2, 4> DwTile;
 template <int NQ, int ALONG>
 __device__ __forceinline__ void dx_tile(const BwdTiles &b, int id, char *smem) {
   typedef typename DxTile<NQ>::P P;
-  const int n = *b.count * b.f.copies, dim = b.a.dim;
+  const int n = b.rows() * b.f.copies, dim = b.a.dim;
   tile::Place at;
   if (!at.find(id, b.tiles_dim, (n + NQ - 1) / NQ, b.f.split_x, kGroup)) return;
   P x;
@@ -602,7 +612,7 @@ __device__ __forceinline__ void dx_tile(const BwdTiles &b, int id, char *smem) {
   for (int i = 0; i < ALONG; ++i)
     x.add(smem, typename P::LoadP(b.a.w, b.a.w_stride, p0, dim, b.v0 + k0, n_k, x.wave, x.lane),
           typename P::LoadQ(b.dl + i * (2 * b.f.rows * b.f.piece), b.f.piece, q0, n, k0, n_k, x.wave, x.lane), n_k);
-  const auto row = [&](int es) { return [=, &b](int r) { return b.a.dx + (int64_t)b.order[r] * b.a.dx_stride * es; }; };
+  const auto row = [&](int es) { return [=, &b](int r) { return b.a.dx + b.token(r) * b.a.dx_stride * es; }; };
   if (b.sums_x) {
     float *sums = b.sum_x + (int64_t)at.part * b.f.copies * b.f.rows * dim;
     put_product<P, kSums>(x, smem, p0, q0, n, dim, !b.first, [&](int r) { return (char *)(sums + (int64_t)r * dim); });
@@ -620,7 +630,7 @@ __device__ __forceinline__ void dw_tile(const BwdTiles &b, int id, char *smem) {
   tile::Place at;
   if (!at.find(id, b.tiles_dim, (int)plan::ceil_div(b.n_v, P::NQ), b.f.split_w, kGroup)) return;
   P x;
-  const int n = *b.count * b.f.copies;
+  const int n = b.rows() * b.f.copies;
   const int len = (int)plan::round_up(plan::ceil_div(n, b.f.split_w), tile::kStep);
   const int k0 = at.part * len, n_k = max(0, min(n - k0, len));
   const int p0 = at.p * P::NP, q0 = at.q * P::NQ;
@@ -653,7 +663,7 @@ __global__ __launch_bounds__(512, 2) void linear_grads_kernel(BwdTiles b) {
 // The parts' sums, in order, as rows of the gradient.
 template <bool F32, bool DX>
 __global__ __launch_bounds__(256) void linear_sums_kernel(BwdTiles b) {
-  const int rows = DX ? *b.count : b.n_v, dim = b.a.dim, parts = DX ? b.f.split_x : b.f.split_w, copies = DX ? b.f.copies : 1;
+  const int rows = DX ? b.rows() : b.n_v, dim = b.a.dim, parts = DX ? b.f.split_x : b.f.split_w, copies = DX ? b.f.copies : 1;
   const int64_t per = (DX ? (int64_t)b.f.copies * b.f.rows : (int64_t)b.f.piece) * dim;
   const float *sums = DX ? b.sum_x : b.sum_w;
   const int vecs = dim / 4;
@@ -671,7 +681,7 @@ __global__ __launch_bounds__(256) void linear_sums_kernel(BwdTiles b) {
         for (int j = 0; j < 8; ++j) sum += v[j];
       }
     }
-    char *row = DX ? b.a.dx + (int64_t)b.order[r] * b.a.dx_stride * (F32 ? 4 : 2) : b.a.dw + (int64_t)(b.v0 + r) * b.a.dw_stride * (F32 ? 4 : 2);
+    char *row = DX ? b.a.dx + b.token(r) * b.a.dx_stride * (F32 ? 4 : 2) : b.a.dw + (int64_t)(b.v0 + r) * b.a.dw_stride * (F32 ? 4 : 2);
     if constexpr (F32) *(f32x4 *)(row + 4 * c) = sum;
     else *(uint2 *)(row + 2 * c) = make_uint2(pack_bf16(sum[0], sum[1]), pack_bf16(sum[2], sum[3]));
   }
@@ -805,7 +815,7 @@ hipError_t launch_linear_logp_bwd(const LinearArgs &a, hipStream_t s) {
     b.first = p == 0;
     b.last = p == b.f.pieces - 1;
     if (b.f.split_z > 1) {
-      const LogitParts z = {a.w, b.x, a.w_stride, b.f.dim, b.count, 0, a.vocab, a.dim, b.f.split_z, b.f.piece / plan::kTileP, b.f.rows,
+      const LogitParts z = {a.w, b.x, a.w_stride, b.f.dim, b.count, (int)a.n_tokens, a.vocab, a.dim, b.f.split_z, b.f.piece / plan::kTileP, b.f.rows,
                             b.f.piece, (float *)(a.ws + b.f.z_off)};
       e = logit_parts(z, b.f.tile, s);
       if (e != hipSuccess) return e;
