@@ -726,7 +726,8 @@ nsp_status nsp_linear_logp_fwd(int64_t n_tokens, int32_t dim, int32_t vocab, con
  *     da_v = scale (g_logp (1[v = target] - p_v) + g_lse p_v
  *                   - g_entropy p_v (z_v - lse + entropy))
  *     dx[t] = sum_v da[t][v] w[v],   dw[v] = sum_t da[t][v] x[t]
- * da is rounded to bf16 for the matrix cores: with float32 gradients, and in calls of
+ * with p = exp(z - lse) of the lse given, at most 1 (an lse of a part of the vocabulary
+ * cuts the gradient there).  da is rounded to bf16 for the matrix cores: with float32 gradients, and in calls of
  * up to 128 tokens, to two bf16 numbers (2^-16 of an element); with bf16 gradients of
  * more tokens to one (half a step, 2^-8: their relative 2-norm is off by 0.0022 to 0.0026,
  * where rounding the results alone leaves 0.0017).  float32 gradients take the products of
@@ -758,7 +759,8 @@ size_t nsp_distill_fwd_workspace(int64_t n_tokens, int32_t vocab);
 /*
  * Divergence of a row of logits from a teacher's top alternatives (Kullback and
  * Leibler's, from the teacher's side), as nsp_token_logp_fwd gives them of
- * the teacher's logits.  For row t, alternatives i_k = index[t][k] with log
+ * the teacher's logits.  The logits are stored ones: of a long step, those of some rows
+ * at a time (each row is for itself).  For row t, alternatives i_k = index[t][k] with log
  * probabilities t_k = teacher_logp[t][k]:
  *     q_k  = exp(t_k - c),  c = 0 (NSP_DISTILL_GIVEN: what the alternatives leave
  *            of 1 counts for nothing) or log sum_k exp(t_k) (NSP_DISTILL_NORMALIZED)
@@ -788,8 +790,8 @@ nsp_status nsp_distill_fwd(nsp_dtype dtype, int64_t n_tokens, int32_t vocab, con
  * Gradient of the loss with respect to the logits, from g_loss (float32
  * [n_tokens]; a token's weight):
  *     dlogits_v = scale g_loss (p_v sum_k q_k - sum of the q_k with i_k = v)
- * in float32, rounded once, with p = exp(z - lse) of the lse given.  A row with
- * g_loss 0, without alternatives or with an lse of -inf has gradient 0, whatever its
+ * in float32, rounded once, with p = exp(z - lse) of the lse given, at most 1 (an lse
+ * of a part of the vocabulary cuts the gradient there).  A row with g_loss 0, without alternatives or with an lse of -inf has gradient 0, whatever its
  * logits; another with an lse of NaN or +inf has NaN.
  *   dlogits     rows of `vocab` elements of dtype, d_row_stride (>= vocab, unless
  *               one row) apart; in place allowed; what lies between the rows is

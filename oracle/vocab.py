@@ -76,7 +76,7 @@ def distill(logits, index, teacher, normalized=False, scale=1.0):
 
 
 def distill_backward(logits, index, teacher, lse, g, normalized=False, scale=1.0):
-    """Gradient of the logits for the lse given."""
+    """Gradient of the logits for the lse given (p at most 1)."""
     raw = np.asarray(logits, np.float64)
     T, V = raw.shape
     q, _, there = weights(index, teacher, V, normalized)
@@ -87,7 +87,7 @@ def distill_backward(logits, index, teacher, lse, g, normalized=False, scale=1.0
         if np.isnan(q[t]).any():
             out[t] = np.nan
             continue
-        out[t] = np.exp(raw[t] * scale - float(lse[t])) * q[t].sum()
+        out[t] = np.exp(np.minimum(raw[t] * scale - float(lse[t]), 0.0)) * q[t].sum()
         np.subtract.at(out[t], index[t, there[t]], q[t, there[t]])
         out[t] *= float(g[t])
     return out * scale
