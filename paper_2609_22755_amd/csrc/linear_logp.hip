@@ -50,10 +50,6 @@ struct LogitTile<64> { typedef Product<kAlong, kAlong, 256, 64, 4, 2> P; };
 template <>
 struct LogitTile<32> { typedef Product<kAlong, kAlong, 256, 32, 8, 1> P; };
 
-// Workgroups of a compute unit by what their stages leave of its LDS.
-template <class P>
-constexpr int kWavesPerSimd = P::kLds > 80 * 1024 ? 2 : 4;
-
 // The p of element i of a block, from the block's first.
 __device__ __forceinline__ int p_of(int i, int h) { return 8 * (i >> 2) + 4 * h + (i & 3); }
 
@@ -118,7 +114,7 @@ struct LogitParts {
 };
 
 template <int NQ>
-__global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void linear_parts_kernel(LogitParts f) {
+__global__ __launch_bounds__(512, 2) void linear_parts_kernel(LogitParts f) {
   typedef typename LogitTile<NQ>::P P;
   static_assert(P::kLds >= P::NW * 4096 * P::BP, "room for the rows that are stored");
   __shared__ __attribute__((aligned(1024))) char smem[P::kLds];
@@ -164,7 +160,7 @@ struct FwdTiles {
 };
 
 template <int NQ>
-__global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void linear_logp_tiles_kernel(FwdTiles f) {
+__global__ __launch_bounds__(512, 2) void linear_logp_tiles_kernel(FwdTiles f) {
   typedef typename LogitTile<NQ>::P P;
   __shared__ __attribute__((aligned(1024))) char smem[P::kLds];
   tile::Place at;
@@ -474,7 +470,7 @@ __device__ __forceinline__ float left_of(float x) {
 
 // dl of a piece.
 template <int NQ>
-__global__ __launch_bounds__(512, kWavesPerSimd<typename LogitTile<NQ>::P>) void linear_dl_kernel(BwdTiles b, int tiles_p) {
+__global__ __launch_bounds__(512, 2) void linear_dl_kernel(BwdTiles b, int tiles_p) {
   typedef typename LogitTile<NQ>::P P;
   static_assert(P::kLds >= 512 * 32 * P::BP, "room for the rows that are stored");
   __shared__ __attribute__((aligned(1024))) char smem[P::kLds];
