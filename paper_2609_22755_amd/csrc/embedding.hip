@@ -605,8 +605,8 @@ __global__ __launch_bounds__(64 * kJoinWaves) void embedding_join_kernel(SumArgs
 // Zeros in `rows` rows of `bytes` bytes, a vector a thread: a workgroup that stores
 // once and ends keeps the chip writing in the order of the addresses (1 GB: 6.9 TB/s by
 // 4 KB a workgroup, 5.5 to 6.1 by 8 to 256 KB).  lanes: of a row, up to 256.
-constexpr int kFillThreads = 256, kFillBytes = 16 * kFillThreads;
-constexpr int64_t kFillGrid = 1 << 23;           // (a launch holds less than 2^32 threads)
+using plan::kFillBytes;
+using plan::kFillThreads;
 
 __global__ __launch_bounds__(kFillThreads) void embedding_fill_kernel(char *dw, int64_t rows, int64_t bytes, int64_t row_bytes, int64_t strips, int lanes) {
   if (rows == 1) {                               // side by side: cut at lines
@@ -639,6 +639,7 @@ constexpr int kFewWaves = 4;
 template <class W, class Y>
 __global__ __launch_bounds__(64 * kFewWaves) void embedding_few_kernel(EmbedArgs a, int strips) {
   constexpr int N = kVec<Y>, kIds = plan::kEmbedFew / 64 / kFewWaves;
+  static_assert(64 * kFewWaves * kIds == plan::kEmbedFew, "a place for every token");
   __shared__ float sums[kFewWaves - 1][N][64];
   __shared__ int earlier[kFewWaves];
   const int lane = threadIdx.x & 63, wave = (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -731,14 +732,9 @@ template <class W, class Y>
 hipError_t bwd(const EmbedArgs &a, hipStream_t s) {
   const plan::EmbedBwd &f = a.f;
   if (plan::embed_few(a.n_tokens, a.dim, (int)sizeof(Y))) {   // (also of none)
-    const int64_t bytes = a.dim * (int64_t)sizeof(W), row_bytes = a.w.ts * (int64_t)sizeof(W);
-    const bool whole = a.vocab == 1 || row_bytes == bytes;
-    const int64_t rows = whole ? 1 : a.vocab, each = whole ? a.vocab * bytes : bytes;
-    const int64_t strips = plan::ceil_div(each + (whole ? 127 : 0), kFillBytes);
-    int lanes = 1;
-    while (lanes < kFillThreads && 16 * lanes < bytes) lanes *= 2;
-    const int64_t grid = plan::ceil_div(rows, kFillThreads / lanes) * strips;
-    embedding_fill_kernel<<<(int)(grid < kFillGrid ? grid : kFillGrid), kFillThreads, 0, s>>>(a.w.data, rows, each, row_bytes, strips, lanes);
+    const int64_t row_bytes = a.w.ts * (int64_t)sizeof(W);
+    const plan::EmbedFill z = plan::embed_fill(a.vocab, a.dim * (int64_t)sizeof(W), row_bytes);
+    embedding_fill_kernel<<<z.grid, kFillThreads, 0, s>>>(a.w.data, z.rows, z.bytes, row_bytes, z.strips, z.lanes);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.n_tokens == 0) return e;
     const int sum_strips = (int)plan::ceil_div(a.dim, 64 * kVec<Y>);

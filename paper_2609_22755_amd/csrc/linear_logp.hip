@@ -774,7 +774,7 @@ hipError_t launch_linear_logp_bwd(const LinearArgs &a, hipStream_t s) {
   }
   BwdTiles b{};
   b.a = a;
-  b.f = plan::linear_bwd(a.n_tokens, a.dim, a.vocab, a.g_f32);
+  b.f = plan::linear_bwd_call(a.n_tokens, a.dim, a.vocab, a.g_f32, a.dx != nullptr, a.dw != nullptr);
   const int along = b.f.numbers / b.f.copies;    // (more than 1: one copy, tiles of 256 tokens of dx)
   b.count = (int *)(a.ws + b.f.count_off);
   b.order = (int *)(a.ws + b.f.order_off);
@@ -799,11 +799,6 @@ hipError_t launch_linear_logp_bwd(const LinearArgs &a, hipStream_t s) {
   }
   if (e != hipSuccess) return e;
   b.tiles_dim = (int)plan::ceil_div(a.dim, plan::kTileP);
-  if (a.dx && a.dw) {
-    const int64_t x = b.tiles_dim * plan::ceil_div(b.f.copies * a.n_tokens, b.f.tile_x), w = b.tiles_dim * (b.f.piece / plan::kTileP) * b.f.split_w;
-    if (x * b.f.split_x <= plan::kUnits)
-      b.f.split_x = plan::linear_split_beside(b.f.split_x, x, along * (int64_t)b.f.piece, w, plan::ceil_div(b.f.numbers * a.n_tokens, b.f.split_w));
-  }
   b.sums_x = b.f.pieces > 1 || b.f.split_x > 1 || b.f.copies > 1;
   for (int p = 0; p < b.f.pieces; ++p) {
     b.v0 = p * b.f.piece;

@@ -171,6 +171,15 @@ constexpr LinearBwd linear_bwd(int64_t n_tokens, int dim, int vocab, bool f32 = 
   f.bytes = n_tokens > 0 ? at : 0;
   return f;
 }
+// As a call runs it: dx's parts fewer where its tiles run beside dw's.
+constexpr LinearBwd linear_bwd_call(int64_t n_tokens, int dim, int vocab, bool f32, bool dx, bool dw) {
+  LinearBwd f = linear_bwd(n_tokens, dim, vocab, f32);
+  const int64_t cols = ceil_div(dim, kTileP), x = cols * ceil_div(f.copies * n_tokens, f.tile_x);
+  if (dx && dw && x * f.split_x <= kUnits)
+    f.split_x = linear_split_beside(f.split_x, x, f.numbers / f.copies * (int64_t)f.piece, cols * (f.piece / kTileP) * f.split_w,
+                                    ceil_div(f.numbers * n_tokens, f.split_w));
+  return f;
+}
 // Of gradients of either type.
 constexpr size_t linear_bwd_bytes(int64_t n_tokens, int dim, int vocab) {
   const size_t a = linear_bwd(n_tokens, dim, vocab, false).bytes, b = linear_bwd(n_tokens, dim, vocab, true).bytes;
@@ -231,6 +240,28 @@ constexpr EmbedBwd embed_bwd(int64_t n_tokens, int dim, int vocab) {
   f.part_off = at;
   if (f.chunks > 1) at += pad256((size_t)f.chunks * 2 * dim * 4);
   f.bytes = at;
+  return f;
+}
+
+// Zeros in the rows of a table, a vector of 16 bytes a thread: rows side by side as one
+// row, cut at lines of 128 bytes; others `lanes` threads a row.
+constexpr int kFillThreads = 256, kFillBytes = 16 * kFillThreads;
+constexpr int64_t kFillGrid = 1 << 23;          // (a launch holds less than 2^32 threads)
+struct EmbedFill {
+  int64_t rows, bytes, strips; // of a row
+  int lanes;
+  int grid;
+};
+constexpr EmbedFill embed_fill(int vocab, int64_t bytes, int64_t row_bytes) {
+  EmbedFill f{};
+  const bool whole = vocab == 1 || row_bytes == bytes;
+  f.rows = whole ? 1 : vocab;
+  f.bytes = whole ? vocab * bytes : bytes;
+  f.strips = ceil_div(f.bytes + (whole ? 127 : 0), kFillBytes);
+  f.lanes = 1;
+  while (f.lanes < kFillThreads && 16 * f.lanes < bytes) f.lanes *= 2;
+  const int64_t grid = ceil_div(f.rows, kFillThreads / f.lanes) * f.strips;
+  f.grid = (int)(grid < kFillGrid ? grid : kFillGrid);
   return f;
 }
 
