@@ -685,12 +685,12 @@ nsp_status nsp_token_logp_bwd(nsp_dtype dtype, int64_t n_tokens, int32_t vocab, 
 /* Bytes of device workspace of nsp_linear_logp_fwd and _bwd (0 for invalid
  * sizes and no tokens).  Forward: 16 bytes a token and 256 vocabulary rows, of
  * 32768 tokens at most (fewer from 2^19 vocabulary rows on: 1 GB, or 4096 tokens).
- * Backward: the hidden rows gathered (2 n_tokens dim bytes), the gradient of the
- * logits of one piece of the vocabulary (512 MB at most, but 8192 bytes a token from
- * 65536 tokens on; gradients of either type fit), and float32 sums: 4 n_tokens dim bytes with more than one piece,
- * and up to 256 tiles of 256 KB each of dx and of dw where few tiles are split.
- * Calls whose logits make few tiles: up to 256 such tiles of them too.  Calls of up
- * to 128 tokens count them twice, but in the forward. */
+ * Backward (gradients of either type): the hidden rows gathered (2 n_tokens dim
+ * bytes), the gradient of the logits of one piece of the vocabulary (512 MB at most,
+ * but 8192 bytes a token from 65536 tokens on), and float32 sums: 4 n_tokens dim bytes
+ * with more than one piece, and up to 256 tiles of 256 KB each of dx and of dw where
+ * few tiles are split.  Calls whose logits make few tiles: up to 256 such tiles of them
+ * too.  Calls of up to 128 tokens count them twice, but in the forward. */
 size_t nsp_linear_logp_fwd_workspace(int64_t n_tokens, int32_t dim, int32_t vocab);
 size_t nsp_linear_logp_bwd_workspace(int64_t n_tokens, int32_t dim, int32_t vocab);
 
@@ -727,12 +727,12 @@ nsp_status nsp_linear_logp_fwd(int64_t n_tokens, int32_t dim, int32_t vocab, con
  *                   - g_entropy p_v (z_v - lse + entropy))
  *     dx[t] = sum_v da[t][v] w[v],   dw[v] = sum_t da[t][v] x[t]
  * with p = exp(z - lse) of the lse given, at most 1 (an lse of a part of the vocabulary
- * cuts the gradient there).  da is rounded to bf16 for the matrix cores: with float32 gradients, and in calls of
- * up to 128 tokens, to two bf16 numbers (2^-16 of an element); with bf16 gradients of
- * more tokens to one (half a step, 2^-8: their relative 2-norm is off by 0.0022 to 0.0026,
- * where rounding the results alone leaves 0.0017).  float32 gradients take the products of
- * dx and dw twice (8192 x 4096 x 131072: 1.7 times as long).  Sums are float32, rounded
- * once to grad_dtype.  A token whose gradients are all 0 (an ignored target takes g_logp
+ * cuts the gradient there).  da is rounded to bf16 for the matrix cores: with float32
+ * gradients, and in calls of up to 128 tokens, to two bf16 numbers (2^-16 of an
+ * element); with bf16 gradients of more tokens to one (half a step, 2^-8: their relative
+ * 2-norm is off by 0.0022 to 0.0026, where rounding the results alone leaves 0.0017).
+ * float32 gradients of more than 128 tokens take the products of dx and dw twice (8192 x
+ * 4096 x 131072: 1.7 times as long).  Sums are float32, rounded once to grad_dtype.  A token whose gradients are all 0 (an ignored target takes g_logp
  * as 0), or whose lse is -inf, takes no part, whatever its row of x holds, and has
  * dx = 0.  An lse of NaN or +inf makes the token's dx and all of dw NaN.
  *   lse         the forward's; entropy too, needed with g_entropy
@@ -791,8 +791,9 @@ nsp_status nsp_distill_fwd(nsp_dtype dtype, int64_t n_tokens, int32_t vocab, con
  * [n_tokens]; a token's weight):
  *     dlogits_v = scale g_loss (p_v sum_k q_k - sum of the q_k with i_k = v)
  * in float32, rounded once, with p = exp(z - lse) of the lse given, at most 1 (an lse
- * of a part of the vocabulary cuts the gradient there).  A row with g_loss 0, without alternatives or with an lse of -inf has gradient 0, whatever its
- * logits; another with an lse of NaN or +inf has NaN.
+ * of a part of the vocabulary cuts the gradient there).  A row with g_loss 0, without
+ * alternatives or with an lse of -inf has gradient 0, whatever its logits; another with
+ * an lse of NaN or +inf has NaN.
  *   dlogits     rows of `vocab` elements of dtype, d_row_stride (>= vocab, unless
  *               one row) apart; in place allowed; what lies between the rows is
  *               left as it is
@@ -827,7 +828,8 @@ size_t nsp_embedding_bwd_workspace(int64_t n_tokens, int32_t dim, int32_t vocab)
  * Gradient of the table: dw[v] = scale * sum of dy[t] over the tokens t of id v,
  * in float32, in a fixed order (the tokens' own, in chunks), rounded once to
  * w_dtype; every row of dw is written, those of ids without a token with zeros.
- * dy of tokens outside the vocabulary is not read.
+ * dy of tokens outside the vocabulary is not read.  An id of most of the tokens
+ * (padding inside the vocabulary) makes the call slower; outside it costs nothing.
  *   dy          [n_tokens] rows of dim elements of dtype;  dw: [vocab] rows of
  *               w_dtype, apart from dy
  *   workspace   nsp_embedding_bwd_workspace bytes, 256-byte aligned

@@ -7,7 +7,7 @@
 // Bound by HBM: the forward reads the logits once, the backward reads and writes
 // them once; what the alternatives cost (12 bytes and a few operations each) has to
 // hide behind that.  bf16, 4096 x 151643 with 64 alternatives: 192 us (6.5 TB/s);
-// backward 8192 x 131072 with 20: 695 (6.2).
+// backward 8192 x 131072 with 64: 693 (6.2).
 //
 // Forward: the running sums of the log probabilities' pass (logit_sums.hpp)
 // without its weighted one; a workgroup takes a row, or a part of one where there
@@ -306,7 +306,9 @@ template <class T>
 hipError_t bwd(const DistillArgs &a, hipStream_t s) {
   // (us at one, two and four turns. 8192 x 131072 bf16, 8 alternatives: 679, 691, 742;
   // 20: 700, 680, 736; 64: 760, 692, 738; 256: 1413, 878, 809.  777 x 50021 float32, 20:
-  // 55, 57, 65; 64: 59, 62, 68; 256: 108, 80, 84)
+  // 55, 57, 65; 64: 59, 62, 68; 256: 108, 80, 84.  Of few rows the weighing of the alternatives is
+  // the time, and their number alone may decide: 24 x 131072 bf16 at one turn and as here, 64: 7.4
+  // and 7.8; 256: 16.1 and 17.4; one row, 256: 17.4 and 16.6)
   return a.top * kVec<T> <= 128 ? bwd_turns<T, 1>(a, s) : a.top <= 128 ? bwd_turns<T, 2>(a, s) : bwd_turns<T, 4>(a, s);
 }
 

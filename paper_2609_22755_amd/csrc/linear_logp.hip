@@ -5,7 +5,7 @@
 // Bound by the matrix cores: 2 T dim V operations forward, three times that
 // backward (the logits are made again, dx and dw are a product each).  4096 x 4096 x
 // 151643 forward 3.74 ms (1361 TFLOP/s); 8192 x 4096 x 131072, a tenth of the tokens
-// ignored, backward 18.0 ms (1318); a library's product of these sizes, its result stored
+// ignored, backward 18.0 to 18.6 ms (1318 to 1280), with float32 gradients 31.5; a library's product of these sizes, its result stored
 // to memory, 1366 to 1486 (NT).  The clock under this load is 1.6 to 1.7 GHz: power bounds
 // both.  24 rows of 131072 x 4096, a read of the weight: 177 us (6.1 TB/s).
 //

@@ -130,9 +130,12 @@ struct LinearBwd {
   size_t count_off, order_off, place_off, coef_off, target_off, x_off, dl_off, z_off, sum_x_off, sum_w_off, bytes;
 };
 // The gradient of the logits is kept for one piece of the vocabulary at a time,
-// some 2^28 elements of it (512 MB): large enough that adding dx's float32 sums
+// some 2^28 numbers of it (512 MB): large enough that adding dx's float32 sums
 // of one piece to the next costs little (a read and a write of T dim against
-// 6 T dim piece operations: 2% at pieces of 32768).
+// 6 T dim piece operations: 2% at pieces of 32768).  From 65536 tokens on pieces stay at 4096
+// rows, so that the memory grows with the tokens only; the sums are 8% there (4096 x 131072 of
+// 8192 tokens 1330 TFLOP/s, of 65536 1244, of 262144 1225).  Two numbers an element: half
+// the piece.
 constexpr LinearBwd linear_bwd(int64_t n_tokens, int dim, int vocab, bool f32 = false) {
   LinearBwd f{};
   f.copies = n_tokens <= kLinearTwice ? 2 : 1;
@@ -195,11 +198,15 @@ constexpr int kSortWhole = 16384;               // tokens that one workgroup sor
 constexpr int kSortBits = 9;                    // most of a digit
 
 // Few tokens, of at most so many bytes of dy: a kernel of zeros and one that finds each
-// id's tokens itself.  (us, with and without a sort, tables in HBM.  Gained: 24 x 4096 of
-// 131072 rows 199 and 160, a fill alone 156; 70 x 1393 float32 of 69335 74 and 63; 400 x 512
-// of 3000 15.4 and 8.3; 1000 x 512 of 3000 16.7 and 9.7; 2000 x 512 18.0 and 13.4; 1000 x
-// 1024 float32 of 32000 33.2 and 29.5.  Lost, the sort hides beside the zeros of a large
-// table: 1000 x 2048 bf16 of 32000 32.8 and 34.8, 1500 x 1024 33.1 and 38.5)
+// id's tokens itself.  (us with a sort and without, three tables in turn, ids spread over the
+// logarithm of the vocabulary.  Taken without: 24 x 4096 of 131072 rows 197 and 160, the zeros
+// 159; 70 x 1393 float32 of 69335 75 and 61; 400 x 512 of 3000 15.0 and 7.0; 1000 x 512 of 3000
+// 16.3 and 9.1; 2000 x 512 of 3000 18.6 and 13.5, of 32000 21.1 and 20.9; 1000 x 1024 float32 of
+// 32000 32.7 and 30.2; 1000 x 2048 bf16 of 3000 17.7 and 11.4, of 131072 102 and 91, and between
+// them, of 32000, where the sort hides beside the zeros, even: 33.5 and 33.8; 24 x 65536 of 5000 130
+// and 103.  Taken with: 1500 x 1024 bf16 of 32000 20.7 and 21.5; 2000 x 1024 21.9 and 25.3; 2000 x 512
+// float32 21.4 and 19.3.)  Where most tokens have one id the workgroup of that id adds them
+// all: 2000 x 512 of 3000 rows, half of them one id's 63 us, all of them 174.
 constexpr int kEmbedFew = 2048;
 constexpr bool embed_few(int64_t n_tokens, int dim, int es) {
   return n_tokens <= kEmbedFew && n_tokens * dim * es <= (n_tokens <= 1024 ? 4 << 20 : 2 << 20);
